@@ -337,6 +337,132 @@ typedef struct vf_stats {
 int vf_index_stats(const vf_index *index, vf_stats *out);
 
 /*
+ * Operators of a query encoder: the head that turns an upstream embedding into a vector of the table's space and
+ * into the labels to filter by, its training step, and its form for one query.
+ *
+ * Conventions, beside those above
+ *   - dtype: VF_F32, VF_BF16 or VF_F16, one type for all matrices and vectors of a call that are not declared
+ *     float here.  Products, sums, softmax statistics and moments are held in float32; an output is rounded once.
+ *   - Matrices are row-major; ld* is the distance of two rows in elements (>= the row's length), so that a matrix may
+ *     be a slice of a wider one.  Any alignment of an element is accepted; rows that start on 16 bytes are the fastest.
+ *     Offsets are 64 bits wide; every extent (m, n, k, d, v) is below 2^31.
+ *   - Nothing is allocated and nothing waits: work is enqueued on hip_stream and may be captured.  Where a call needs
+ *     device memory of its own it takes it as `workspace` (16-byte aligned); the *_workspace function says how much (0: none,
+ *     NULL is fine), and the memory is free again once the call's work has completed.
+ *   - Results do not depend on what else runs: no floating-point atomics, every sum in a fixed order.
+ *   - Outputs must not overlap inputs or each other, but for the cases named below.
+ */
+#define VF_BF16 2
+#define VF_F16 3
+#define VF_ACT_NONE 0
+#define VF_ACT_RELU 1
+#define VF_ACT_GELU 2 /* z Phi(z), Phi the normal distribution function */
+#define VF_ACT_SILU 3 /* z / (1 + exp(-z)) */
+
+/*
+ * y = act(z) + residual, z = x w^T + bias.
+ *   x [m][k], w [n][k], bias [n] or NULL, residual [m][n] or NULL, y [m][n]; z [m][n] or NULL: the pre-activation, which
+ *   vf_linear_backward reads.  y may be the residual's own memory (same ld).  k = 0: z = bias.
+ */
+int vf_linear(int32_t dtype, int64_t m, int64_t n, int64_t k, const void *x, int64_t ldx, const void *w, int64_t ldw,
+              const void *bias, int32_t activation, const void *residual, int64_t ldr, void *y, int64_t ldy, void *z,
+              int64_t ldz, void *workspace, size_t workspace_bytes, void *hip_stream);
+/*
+ * Gradients of the same, from dy [m][n]: dz = dy act'(z); dx = dz w; dw = dz^T x; dbias = column sums of dz.  The
+ * residual's gradient is dy itself.  Each of dx [m][k], dw [n][k], dbias [n] may be NULL: it is left out, and what only
+ * it reads (w for dx, x for dw) may be NULL too.  z may be NULL for VF_ACT_NONE.  relu'(0) = 0.  dz is rounded to dtype as an
+ * operand of the two products (the column sums take it before that).
+ */
+int vf_linear_backward(int32_t dtype, int64_t m, int64_t n, int64_t k, const void *dy, int64_t lddy, const void *x,
+                       int64_t ldx, const void *w, int64_t ldw, const void *z, int64_t ldz, int32_t activation, void *dx,
+                       int64_t lddx, void *dw, int64_t lddw, void *dbias, void *workspace, size_t workspace_bytes,
+                       void *hip_stream);
+/* Bytes that vf_linear (backward = 0) or vf_linear_backward (1) of these sizes takes as workspace. */
+int vf_linear_workspace(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t activation, int32_t backward,
+                        size_t *bytes);
+
+/*
+ * y = (x - mean) rstd weight + bias per row of 1 <= d <= 2^24 elements; rstd = 1 / sqrt(variance + eps), the variance over d.
+ *   weight, bias [d] or NULL (1 and 0); mean, rstd float [m] or NULL.  y may be x's own memory (same ld).
+ */
+int vf_layer_norm(int32_t dtype, int64_t m, int64_t d, const void *x, int64_t ldx, const void *weight, const void *bias,
+                  double eps, void *y, int64_t ldy, float *mean, float *rstd, void *hip_stream);
+/*
+ * Its gradients.  With h = (x - mean) rstd and g = dy weight:  dx = rstd (g - avg(g) - h avg(g h)); dweight = column
+ * sums of dy h; dbias = column sums of dy.  Each of the three may be NULL.  dx may be dy's own memory (same ld).
+ */
+int vf_layer_norm_backward(int32_t dtype, int64_t m, int64_t d, const void *dy, int64_t lddy, const void *x, int64_t ldx,
+                           const float *mean, const float *rstd, const void *weight, void *dx, int64_t lddx,
+                           void *dweight, void *dbias, void *workspace, size_t workspace_bytes, void *hip_stream);
+int vf_layer_norm_workspace(int32_t dtype, int64_t m, int64_t d, size_t *bytes);
+
+/*
+ * Log probabilities over a vocabulary of v >= 1 labels, one row of logits per query.
+ *   targets  int32 [m] or NULL: the label whose log probability is asked for.  -1: none is (logp 0, no gradient);
+ *            any other value outside [0, v) gives logp NaN and no gradient
+ *   logp     float [m] (NULL without targets)      x_target - lse
+ *   entropy  float [m] or NULL                     -sum p log p
+ *   lse      float [m] or NULL                     log sum exp(x), which the gradient reads
+ *   top      0 .. VF_LOG_PROBS_MAX_TOP alternatives: top_ids int32 [m][top], top_logp float [m][top], the largest logits
+ *            first, ties to the lower label; -1 and -inf where fewer than `top` labels are left
+ * A logit of -inf is a masked label: probability 0, log probability -inf, never an alternative.  In a row of nothing else
+ * lse is -inf, logp of any label -inf, the entropy 0.  NaN or +inf anywhere in a row makes its lse, logp and entropy NaN (top_logp
+ * too); as alternatives NaN comes before +inf before numbers.
+ */
+#define VF_LOG_PROBS_MAX_TOP 64
+int vf_log_probs(int32_t dtype, int64_t m, int64_t v, const void *logits, int64_t ld, const int32_t *targets, int32_t top,
+                 float *logp, float *entropy, float *lse, int32_t *top_ids, float *top_logp, void *workspace,
+                 size_t workspace_bytes, void *hip_stream);
+/*
+ * dlogits_j = d_logp (1[j = target] - p_j) - d_entropy p_j (log p_j + entropy), [m][v] of dtype; lse (and entropy) as
+ * vf_log_probs left them.  d_logp and targets NULL: no such term; d_entropy and entropy NULL: no such term.  Rows without a label
+ * left get zeros.  dlogits may be the logits' own memory (same ld).
+ */
+int vf_log_probs_backward(int32_t dtype, int64_t m, int64_t v, const void *logits, int64_t ld, const float *lse,
+                          const int32_t *targets, const float *d_logp, const float *entropy, const float *d_entropy,
+                          void *dlogits, int64_t ldd, void *hip_stream);
+int vf_log_probs_workspace(int32_t dtype, int64_t m, int64_t v, int32_t top, size_t *bytes);
+
+/*
+ * One AdamW step over many tensors at once.  Per element, in float32 and in this order of operations:
+ *   g = grad grad_scale;  m = m beta1 + g (1 - beta1);  v = v beta2 + (g g) (1 - beta2)
+ *   w = w (1 - lr weight_decay) - lr (m c1) / (sqrt(v) c2 + eps),  c1 = 1 / (1 - beta1^step), c2 = 1 / sqrt(1 - beta2^step)
+ * where w is the master if there is one, else the parameter; a parameter with a master receives w rounded to its type.
+ *
+ *   state_bits 32  m, v: float [n]
+ *   state_bits 8   m: int8 [n], v: uint8 [n], m_scale, v_scale: float [ceil(n / VF_ADAMW_BLOCK)], one scale per block.  Square-law codes:
+ *                  m = m_scale (c / 127) |c / 127|;  sqrt(v) = v_scale (c / 254)^2.  A block's scale is the largest |m| (sqrt(v)) in
+ *                  it, codes go to the nearest, ties to even; v > 0 has at least code 1.  All zero is the state before the first step.  A
+ *                  moment that is not finite is held as NaN by its own element (m code -128, v code 255) and leaves its block's
+ *                  scale alone.  The step itself takes m and v before they are rounded to codes.
+ *   skip           device int32 or NULL: nothing is changed if it is not 0 when the work runs (a found overflow)
+ * Parameters, masters, moments and scales of all tensors must not overlap.  n = 0 is fine.  At most 2^31 * VF_ADAMW_BLOCK elements in a call.
+ */
+#define VF_ADAMW_BLOCK 256
+typedef struct vf_adamw_tensor {
+    void *param;
+    const void *grad;
+    float *master;
+    void *m;
+    void *v;
+    float *m_scale;
+    float *v_scale;
+    int64_t n;
+    double weight_decay;
+    int32_t param_type, grad_type; /* VF_F32, VF_BF16, VF_F16 */
+    int32_t state_bits, reserved;  /* 32 or 8; reserved must be zero */
+} vf_adamw_tensor;
+typedef struct vf_adamw_params {
+    double lr, beta1, beta2, eps, grad_scale;
+    int64_t step; /* 1 for the first */
+} vf_adamw_params;
+int vf_adamw_step(const vf_adamw_tensor *tensors, int32_t n_tensors, const vf_adamw_params *params, const int32_t *skip,
+                  void *hip_stream);
+/* The moments as float32: m_out[i], v_out[i] float [n] of tensor i, either may be NULL (only n, m, v, scales and state_bits are read). */
+int vf_adamw_moments(const vf_adamw_tensor *tensors, int32_t n_tensors, float *const *m_out, float *const *v_out,
+                     void *hip_stream);
+
+/*
  * Experiment and test switches (not part of the paper's method): launch geometry, which kernels serve which
  * batch sizes, the error-bound scale of the float32 seed proofs.  With index == NULL the process-wide
  * defaults change, which indexes built afterwards start from (the build-time switches "build16",

@@ -14,7 +14,7 @@ import numpy as np
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libvecflow.so")
 
-VF_U8, VF_F32 = 0, 1
+VF_U8, VF_F32, VF_BF16, VF_F16 = 0, 1, 2, 3
 ARR = dict(S=0, O_HS=1, O_LS=2, M_HS=3, M_LS=4, G_HS=5, GO_LS=6, X_LS=7, BITSET=8)
 _ARR_DTYPE = dict(S=np.int64, O_HS=np.int64, O_LS=np.int64, M_HS=np.int32, M_LS=np.int32, G_HS=np.int32,
                   GO_LS=np.int64, X_LS=np.uint8, BITSET=np.uint32)
@@ -22,7 +22,10 @@ _ARR_DTYPE = dict(S=np.int64, O_HS=np.int64, O_LS=np.int64, M_HS=np.int32, M_LS=
 EXPORTED_SYMBOLS = ("vf_build_index", "vf_search", "vf_search_exact", "vf_index_export", "vf_index_stats",
                     "vf_index_free", "vf_last_error", "vf_profile_enable", "vf_profile_read", "vf_search_multi",
                     "vf_build_index_opt", "vf_tune", "vf_debug_route", "vf_search_noalloc", "vf_serve_begin", "vf_serve_submit",
-                    "vf_serve_poll", "vf_serve_end", "vf_serve_run", "vf_search_ex")
+                    "vf_serve_poll", "vf_serve_end", "vf_serve_run", "vf_search_ex",
+                    "vf_linear", "vf_linear_backward", "vf_linear_workspace", "vf_layer_norm", "vf_layer_norm_backward",
+                    "vf_layer_norm_workspace", "vf_log_probs", "vf_log_probs_backward", "vf_log_probs_workspace",
+                    "vf_adamw_step", "vf_adamw_moments")
 
 ALLOC_FN = C.CFUNCTYPE(C.c_void_p, C.c_size_t, C.c_void_p)
 FREE_FN = C.CFUNCTYPE(None, C.c_void_p, C.c_void_p)
@@ -59,6 +62,16 @@ class VfSearchParams(C.Structure):
 class VfServeParams(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("k", "itopk", "width", "iters", "n_seeds", "n_workers", "ring_slots", "waves_per_worker")] + \
                [(n, C.c_int64) for n in ("max_jobs", "idle_polls")]
+
+
+class VfAdamwTensor(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("param", "grad", "master", "m", "v", "m_scale", "v_scale")] + \
+               [("n", C.c_int64), ("weight_decay", C.c_double)] + \
+               [(n, C.c_int32) for n in ("param_type", "grad_type", "state_bits", "reserved")]
+
+
+class VfAdamwParams(C.Structure):
+    _fields_ = [(n, C.c_double) for n in ("lr", "beta1", "beta2", "eps", "grad_scale")] + [("step", C.c_int64)]
 
 
 class VecflowError(RuntimeError):
@@ -115,6 +128,21 @@ def load_library():
         L.vf_profile_enable.argtypes = [p, C.c_int]
         L.vf_profile_read.restype = C.c_int
         L.vf_profile_read.argtypes = [p, C.POINTER(VfProfile), p]
+        sz = C.c_size_t
+        for name, args in dict(
+                vf_linear=[i32, i64, i64, i64, p, i64, p, i64, p, i32, p, i64, p, i64, p, i64, p, sz, p],
+                vf_linear_backward=[i32, i64, i64, i64, p, i64, p, i64, p, i64, p, i64, i32, p, i64, p, i64, p, p, sz, p],
+                vf_linear_workspace=[i32, i64, i64, i64, i32, i32, C.POINTER(sz)],
+                vf_layer_norm=[i32, i64, i64, p, i64, p, p, C.c_double, p, i64, p, p, p],
+                vf_layer_norm_backward=[i32, i64, i64, p, i64, p, i64, p, p, p, p, i64, p, p, p, sz, p],
+                vf_layer_norm_workspace=[i32, i64, i64, C.POINTER(sz)],
+                vf_log_probs=[i32, i64, i64, p, i64, p, i32, p, p, p, p, p, p, sz, p],
+                vf_log_probs_backward=[i32, i64, i64, p, i64, p, p, p, p, p, p, i64, p],
+                vf_log_probs_workspace=[i32, i64, i64, i32, C.POINTER(sz)],
+                vf_adamw_step=[p, i32, C.POINTER(VfAdamwParams), p, p],
+                vf_adamw_moments=[p, i32, p, p, p]).items():
+            getattr(L, name).restype = C.c_int
+            getattr(L, name).argtypes = args
         L.vf_index_free.restype = None
         L.vf_index_free.argtypes = [p]
         L.vf_last_error.restype = C.c_char_p
@@ -470,3 +498,326 @@ def search_exact(index: Index, queries, qlabel_offsets, qlabel_ids, k, stream=No
                                           int(k), C.c_void_p(out_ids.data_ptr()), C.c_void_p(out_dists.data_ptr()),
                                           _stream_handle(stream)))
     return out_ids, out_dists
+
+
+# ---------------------------------------------------------------- operators of a query encoder
+#
+# Tensors are CUDA tensors of one device, the current one.  Matrices are 2-D with neighbouring columns (stride(1) == 1); rows may be
+# slices of a wider matrix.  Everything is enqueued on the current stream (or `stream`), where outputs and workspaces
+# are allocated too; nothing synchronises.
+
+ACTIVATIONS = dict(none=0, relu=1, gelu=2, silu=3)
+ADAMW_BLOCK = 256
+LOG_PROBS_MAX_TOP = 64
+
+_FLOAT_CODES = None       # torch dtype -> VF_*; filled on first use (torch is imported lazily here)
+
+
+def _float_code(t, what):
+    global _FLOAT_CODES
+    if _FLOAT_CODES is None:
+        import torch
+        _FLOAT_CODES = {torch.float32: VF_F32, torch.bfloat16: VF_BF16, torch.float16: VF_F16}
+    code = _FLOAT_CODES.get(t.dtype)
+    if code is None:
+        raise VecflowError(f"{what}: unsupported dtype {t.dtype}")
+    return code
+
+
+def _matrix(t, what, dtype, rows=None, cols=None):
+    """Distance of two rows of a matrix argument, which must have the dtype and sizes given."""
+    if not t.is_cuda or t.dim() != 2 or t.dtype != dtype:
+        raise VecflowError(f"{what} must be a 2-D CUDA tensor of {dtype}")
+    n, d = t.shape
+    if (rows is not None and n != rows) or (cols is not None and d != cols):
+        raise VecflowError(f"{what} must have shape [{n if rows is None else rows}, {d if cols is None else cols}], not {list(t.shape)}")
+    if d > 1 and t.stride(1) != 1:
+        raise VecflowError(f"{what} must have neighbouring columns (stride(1) == 1)")
+    if n <= 1:
+        return d
+    ld = t.stride(0)
+    if ld < d:
+        raise VecflowError(f"{what} must not have overlapping rows")
+    return ld
+
+
+def _vector(t, what, dtype, n):
+    """Address of a vector argument; None stays None."""
+    if t is None:
+        return None
+    if not t.is_cuda or t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise VecflowError(f"{what} must be a contiguous CUDA tensor [{n}] of {dtype}")
+    return t.data_ptr()
+
+
+class _on:
+    """The stream of a call: allocations are made on it, so that memory returns to the pool in its order."""
+
+    def __init__(self, stream, like):
+        import torch
+        self.torch = torch
+        self.device = like.device
+        if like.device.index != torch.cuda.current_device():
+            raise VecflowError("tensors must be on the current device")
+        self.stream = stream
+        self.handle = (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+
+    def empty(self, shape, dtype):
+        if self.stream is None:
+            return self.torch.empty(shape, dtype=dtype, device=self.device)
+        with self.torch.cuda.stream(self.stream):
+            return self.torch.empty(shape, dtype=dtype, device=self.device)
+
+    def workspace(self, nbytes):
+        """(tensor, address, bytes)"""
+        if nbytes == 0:
+            return None, None, 0
+        t = self.empty((nbytes,), self.torch.uint8)
+        return t, t.data_ptr(), nbytes
+
+
+def _size_of(fn, *args):
+    n = C.c_size_t(0)
+    _check(fn(*args, C.byref(n)))
+    return n.value
+
+
+def _activation(name):
+    if name not in ACTIVATIONS:
+        raise VecflowError(f"unknown activation {name!r}: one of {sorted(ACTIVATIONS)}")
+    return ACTIVATIONS[name]
+
+
+def linear(x, weight, bias=None, residual=None, activation="none", save=False, out=None, stream=None):
+    """act(x weight^T + bias) + residual for x [m, k], weight [n, k] (vf_linear).  save=True: (y, z) with the
+    pre-activation z that linear_backward reads.  `out` may be the residual's own memory."""
+    L = load_library()
+    code, T, act = _float_code(x, "x"), x.dtype, _activation(activation)
+    ldx = _matrix(x, "x", T)
+    m, k = x.shape
+    ldw = _matrix(weight, "weight", T, None, k)
+    n = weight.shape[0]
+    pb = _vector(bias, "bias", T, n)
+    on = _on(stream, x)
+    ldr = 0 if residual is None else _matrix(residual, "residual", T, m, n)
+    if out is None:
+        out = on.empty((m, n), T)
+    ldy = _matrix(out, "out", T, m, n)
+    z = on.empty((m, n), T) if save else None
+    _ws, pw, nw = on.workspace(_size_of(L.vf_linear_workspace, code, m, n, k, act, 0))
+    _check(L.vf_linear(code, m, n, k, x.data_ptr(), ldx, weight.data_ptr(), ldw, pb, act,
+                       None if residual is None else residual.data_ptr(), ldr, out.data_ptr(), ldy,
+                       z.data_ptr() if save else None, n, pw, nw, on.handle))
+    return (out, z) if save else out
+
+
+def linear_backward(dy, x, weight, z=None, activation="none", bias=True, dx=True, dweight=True, stream=None):
+    """Gradients (dx, dweight, dbias) of linear from dy [m, n] (vf_linear_backward); the residual's gradient is dy itself.
+    What is not asked for is None.  z: the pre-activation, needed for any activation but "none"."""
+    L = load_library()
+    code, T, act = _float_code(dy, "dy"), dy.dtype, _activation(activation)
+    lddy = _matrix(dy, "dy", T)
+    m, n = dy.shape
+    ldx = _matrix(x, "x", T, m)
+    k = x.shape[1]
+    ldw = _matrix(weight, "weight", T, n, k)
+    if act and z is None:
+        raise VecflowError(f"linear_backward needs z, the pre-activation, for activation {activation!r}")
+    ldz = _matrix(z, "z", T, m, n) if act else 0
+    on = _on(stream, dy)
+    gx = on.empty((m, k), T) if dx else None
+    gw = on.empty((n, k), T) if dweight else None
+    gb = on.empty((n,), T) if bias else None
+    _ws, pw, nw = on.workspace(_size_of(L.vf_linear_workspace, code, m, n, k, act, 1))
+    _check(L.vf_linear_backward(code, m, n, k, dy.data_ptr(), lddy, x.data_ptr(), ldx, weight.data_ptr(), ldw,
+                                z.data_ptr() if act else None, ldz, act, gx.data_ptr() if dx else None, k,
+                                gw.data_ptr() if dweight else None, k, gb.data_ptr() if bias else None, pw, nw, on.handle))
+    return gx, gw, gb
+
+
+def layer_norm(x, weight=None, bias=None, eps=1e-5, save=False, out=None, stream=None):
+    """(x - mean) / sqrt(variance + eps) weight + bias per row of x [m, d] (vf_layer_norm).  save=True: (y, mean, rstd).
+    `out` may be x's own memory."""
+    L = load_library()
+    code, T = _float_code(x, "x"), x.dtype
+    ldx = _matrix(x, "x", T)
+    m, d = x.shape
+    pg, pb = _vector(weight, "weight", T, d), _vector(bias, "bias", T, d)
+    on = _on(stream, x)
+    if out is None:
+        out = on.empty((m, d), T)
+    ldy = _matrix(out, "out", T, m, d)
+    stats = on.empty((2, m), on.torch.float32) if save else None
+    ps = stats.data_ptr() if save else None
+    _check(L.vf_layer_norm(code, m, d, x.data_ptr(), ldx, pg, pb, eps, out.data_ptr(), ldy, ps, ps + 4 * m if save else None,
+                           on.handle))
+    return (out, stats[0], stats[1]) if save else out
+
+
+def layer_norm_backward(dy, x, mean, rstd, weight=None, dx=True, dweight=True, dbias=True, out=None, stream=None):
+    """Gradients (dx, dweight, dbias) of layer_norm from dy [m, d] (vf_layer_norm_backward).  What is not asked for is
+    None.  `out`: where dx goes, dy's own memory if need be."""
+    L = load_library()
+    code, T = _float_code(dy, "dy"), dy.dtype
+    lddy = _matrix(dy, "dy", T)
+    m, d = dy.shape
+    ldx = _matrix(x, "x", T, m, d)
+    on = _on(stream, dy)
+    pm, pr = _vector(mean, "mean", on.torch.float32, m), _vector(rstd, "rstd", on.torch.float32, m)
+    pg = _vector(weight, "weight", T, d)
+    if dx and out is None:
+        out = on.empty((m, d), T)
+    ldo = _matrix(out, "out", T, m, d) if dx else 0
+    gw = on.empty((d,), T) if dweight else None
+    gb = on.empty((d,), T) if dbias else None
+    sums = dweight or dbias
+    _ws, pw, nw = on.workspace(_size_of(L.vf_layer_norm_workspace, code, m, d) if sums else 0)
+    _check(L.vf_layer_norm_backward(code, m, d, dy.data_ptr(), lddy, x.data_ptr(), ldx, pm, pr, pg,
+                                    out.data_ptr() if dx else None, ldo, gw.data_ptr() if dweight else None,
+                                    gb.data_ptr() if dbias else None, pw, nw, on.handle))
+    return out if dx else None, gw, gb
+
+
+def log_probs(logits, targets=None, top=0, stream=None):
+    """Log probabilities over the vocabulary of logits [m, v] (vf_log_probs): (logp, entropy, lse) or, with top > 0,
+    (logp, entropy, lse, top_ids, top_logp); float32 [m], int32 / float32 [m, top].  targets: int32 [m], -1 for none;
+    logp is None without them."""
+    L = load_library()
+    code = _float_code(logits, "logits")
+    ld = _matrix(logits, "logits", logits.dtype)
+    m, v = logits.shape
+    top = int(top)
+    if not 0 <= top <= LOG_PROBS_MAX_TOP:
+        raise VecflowError(f"top must be 0 .. {LOG_PROBS_MAX_TOP}")
+    on = _on(stream, logits)
+    f32, i32 = on.torch.float32, on.torch.int32
+    pt = _vector(targets, "targets", i32, m)
+    sums = on.empty((3, m), f32)
+    ps = sums.data_ptr()
+    ids = on.empty((m, top), i32) if top else None
+    tlp = on.empty((m, top), f32) if top else None
+    _ws, pw, nw = on.workspace(_size_of(L.vf_log_probs_workspace, code, m, v, top))
+    _check(L.vf_log_probs(code, m, v, logits.data_ptr(), ld, pt, top, ps if pt is not None else None, ps + 4 * m, ps + 8 * m,
+                          ids.data_ptr() if top else None, tlp.data_ptr() if top else None, pw, nw, on.handle))
+    logp, entropy, lse = sums.unbind(0)
+    if targets is None:
+        logp = None
+    return (logp, entropy, lse, ids, tlp) if top else (logp, entropy, lse)
+
+
+def log_probs_backward(logits, lse, targets=None, d_logp=None, entropy=None, d_entropy=None, out=None, stream=None):
+    """Gradient with respect to the logits from those of logp and entropy (vf_log_probs_backward); `out` may be the
+    logits' own memory."""
+    L = load_library()
+    code, T = _float_code(logits, "logits"), logits.dtype
+    ld = _matrix(logits, "logits", T)
+    m, v = logits.shape
+    on = _on(stream, logits)
+    f32 = on.torch.float32
+    if (targets is None) != (d_logp is None) or (entropy is None) != (d_entropy is None):
+        raise VecflowError("targets and d_logp go together, and entropy and d_entropy")
+    if out is None:
+        out = on.empty((m, v), T)
+    ldd = _matrix(out, "out", T, m, v)
+    _check(L.vf_log_probs_backward(code, m, v, logits.data_ptr(), ld, _vector(lse, "lse", f32, m),
+                                   _vector(targets, "targets", on.torch.int32, m), _vector(d_logp, "d_logp", f32, m),
+                                   _vector(entropy, "entropy", f32, m), _vector(d_entropy, "d_entropy", f32, m),
+                                   out.data_ptr(), ldd, on.handle))
+    return out
+
+
+def adamw_state(param, bits=32):
+    """Moments before the first step: (m, v) float32, or with bits=8 (m int8, v uint8, m_scale, v_scale)."""
+    import torch
+    n = param.numel()
+    if bits == 32:
+        return tuple(torch.zeros(n, dtype=torch.float32, device=param.device) for _ in range(2))
+    if bits != 8:
+        raise VecflowError("bits must be 32 or 8")
+    blocks = -(-n // ADAMW_BLOCK)
+    return (torch.zeros(n, dtype=torch.int8, device=param.device), torch.zeros(n, dtype=torch.uint8, device=param.device),
+            torch.zeros(blocks, dtype=torch.float32, device=param.device),
+            torch.zeros(blocks, dtype=torch.float32, device=param.device))
+
+
+def _flat(t, what, dtypes, n):
+    if not t.is_cuda or not t.is_contiguous() or t.dtype not in dtypes or t.numel() != n:
+        raise VecflowError(f"{what} must be a contiguous CUDA tensor of {n} elements of {' or '.join(map(str, dtypes))}")
+    return t.data_ptr()
+
+
+def _adamw_list(ms, vs, m_scales, v_scales):
+    """(array of VfAdamwTensor with the moments filled in, torch)"""
+    import torch
+    count = len(ms)
+    for other in (vs, m_scales, v_scales):
+        if other is not None and len(other) != count:
+            raise VecflowError("adamw: the lists must have one entry per tensor")
+    if (m_scales is None) != (v_scales is None):
+        raise VecflowError("adamw: m_scales and v_scales go together")
+    arr = (VfAdamwTensor * max(count, 1))()
+    for i in range(count):
+        n = ms[i].numel()
+        t = arr[i]
+        t.n = n
+        if ms[i].dtype == torch.float32:
+            t.state_bits, kinds = 32, ((torch.float32,), (torch.float32,))
+        else:
+            t.state_bits, kinds = 8, ((torch.int8,), (torch.uint8,))
+            if m_scales is None or m_scales[i] is None or v_scales[i] is None:
+                raise VecflowError(f"adamw: tensor {i}: moments in 8 bits need scales")
+            blocks = -(-n // ADAMW_BLOCK)
+            t.m_scale = _flat(m_scales[i], f"m_scales[{i}]", (torch.float32,), blocks)
+            t.v_scale = _flat(v_scales[i], f"v_scales[{i}]", (torch.float32,), blocks)
+        t.m = _flat(ms[i], f"ms[{i}]", kinds[0], n)
+        t.v = _flat(vs[i], f"vs[{i}]", kinds[1], n)
+    return arr, torch
+
+
+def adamw_step(params, grads, ms, vs, step, lr, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, grad_scale=1.0, masters=None,
+               m_scales=None, v_scales=None, skip=None, stream=None):
+    """One AdamW step over lists of tensors, in place (vf_adamw_step).  params: float32, bfloat16 or float16, with a
+    float32 master each if `masters` is given (entries may be None); ms, vs: the moments of adamw_state, in 8 bits with
+    their scales; weight_decay: one number or one per tensor; step counts from 1; skip: int32 CUDA tensor [1], the step
+    changes nothing if it is not 0 when the work runs."""
+    count = len(params)
+    if len(grads) != count or len(ms) != count or (masters is not None and len(masters) != count):
+        raise VecflowError("adamw: the lists must have one entry per tensor")
+    arr, torch = _adamw_list(ms, vs, m_scales, v_scales)
+    decay = weight_decay if isinstance(weight_decay, (list, tuple)) else [weight_decay] * count
+    if len(decay) != count:
+        raise VecflowError("adamw: weight_decay must be one number or one per tensor")
+    if count == 0:
+        return
+    floats = (torch.float32, torch.bfloat16, torch.float16)
+    for i in range(count):
+        t, n = arr[i], arr[i].n
+        t.param = _flat(params[i], f"params[{i}]", floats, n)
+        t.grad = _flat(grads[i], f"grads[{i}]", floats, n)
+        t.param_type, t.grad_type = _float_code(params[i], "params"), _float_code(grads[i], "grads")
+        if masters is not None and masters[i] is not None:
+            t.master = _flat(masters[i], f"masters[{i}]", (torch.float32,), n)
+        t.weight_decay = decay[i]
+    prm = VfAdamwParams(lr, betas[0], betas[1], eps, grad_scale, step)
+    on = _on(stream, params[0])
+    _check(load_library().vf_adamw_step(arr, count, C.byref(prm), _vector(skip, "skip", torch.int32, 1), on.handle))
+
+
+def adamw_moments(ms, vs, m_scales=None, v_scales=None, stream=None):
+    """The moments as float32 tensors: lists (m, v) (vf_adamw_moments)."""
+    arr, torch = _adamw_list(ms, vs, m_scales, v_scales)
+    count = len(ms)
+    if count == 0:
+        return [], []
+    on = _on(stream, ms[0])
+    total = [on.empty((sum(t.numel() for t in ms),), torch.float32) for _ in range(2)]
+    outs, ptrs = ([], []), ((C.c_void_p * count)(), (C.c_void_p * count)())
+    for which in (0, 1):
+        at, base = 0, total[which].data_ptr()
+        for i in range(count):
+            n = arr[i].n
+            outs[which].append(total[which][at:at + n])
+            ptrs[which][i] = base + 4 * at
+            at += n
+    _check(load_library().vf_adamw_moments(arr, count, ptrs[0], ptrs[1], on.handle))
+    return outs

@@ -1,0 +1,313 @@
+// One AdamW step over a list of tensors in few launches: the list travels as a kernel argument (48 tensors a launch), a
+// wave takes blocks of 256 elements, four neighbours a lane.  With moments in 8 bits a block shares a scale, so the wave that
+// holds it takes the largest moment without leaving its registers.  Bound by memory: every operand is read and written once.
+//
+// The operations are single float32 ones in the order that the header states (no fused multiply-add), divisions and square
+// roots rounded correctly: a plain evaluation gives the same bits, codes included.
+#include "vf_ops.h"
+
+namespace vf {
+
+constexpr int kBlock = VF_ADAMW_BLOCK;
+constexpr int kLaunchTensors = 48;   // 76 bytes each: the argument block of a kernel holds 4096
+
+struct AdamwItem {
+    void *param;
+    const void *grad;
+    float *master;
+    void *m, *v;
+    float *m_scale, *v_scale;
+    int64_t n;
+    float decay;        // 1 - lr weight_decay
+    int32_t types;      // parameter | gradient << 8
+};
+struct AdamwList {
+    AdamwItem item[kLaunchTensors];
+    uint32_t first[kLaunchTensors + 1];   // tensor i has the blocks first[i] .. first[i + 1]
+    int32_t n;
+};
+static_assert(sizeof(AdamwList) <= 3900, "the list must fit a kernel's argument block");
+
+struct AdamwScalars {
+    float beta1, one_beta1, beta2, one_beta2, c1, c2, eps, lr, grad_scale;
+};
+
+// Four neighbouring elements of a tensor as float32; n: how many there are.
+__device__ __forceinline__ void load4(const void *p, int type, int64_t at, int n, float (&o)[4])
+{
+    if (type == VF_F32) {
+        const float *q = (const float *)p + at;
+        if (n >= 4) { const float4v u = load_vec<float4v>(q); for (int j = 0; j < 4; ++j) o[j] = u[j]; }
+        else for (int j = 0; j < 4; ++j) o[j] = j < n ? q[j] : 0.f;
+    } else {
+        uint16_t u[4] = {0, 0, 0, 0};
+        const uint16_t *q = (const uint16_t *)p + at;
+        if (n >= 4) __builtin_memcpy(u, q, 8);
+        else for (int j = 0; j < 4; ++j) if (j < n) u[j] = q[j];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            o[j] = type == VF_BF16 ? __uint_as_float((uint32_t)u[j] << 16) : (float)__builtin_bit_cast(f16, u[j]);
+    }
+}
+__device__ __forceinline__ void store4(void *p, int type, int64_t at, int n, const float (&o)[4])
+{
+    if (type == VF_F32) {
+        float *q = (float *)p + at;
+        if (n >= 4) { float4v u = {o[0], o[1], o[2], o[3]}; store_vec(q, u); }
+        else for (int j = 0; j < 4; ++j) if (j < n) q[j] = o[j];
+    } else {
+        uint16_t u[4], *q = (uint16_t *)p + at;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            u[j] = type == VF_BF16 ? __builtin_bit_cast(uint16_t, (bf16)o[j]) : __builtin_bit_cast(uint16_t, (f16)o[j]);
+        if (n >= 4) __builtin_memcpy(q, u, 8);
+        else for (int j = 0; j < 4; ++j) if (j < n) q[j] = u[j];
+    }
+}
+
+// The moments that the codes of a block stand for.
+__device__ __forceinline__ float m_of(int8_t c, float scale)
+{
+    const float a = (float)c * (float)(1.0 / 127);
+    return c == -128 ? __uint_as_float(0x7FC00000u) : scale * (a * fabsf(a));
+}
+__device__ __forceinline__ float v_of(uint8_t c, float scale)
+{
+    const float b = (float)c * (float)(1.0 / 254), r = scale * (b * b);
+    return c == 255 ? __uint_as_float(0x7FC00000u) : r * r;
+}
+__device__ __forceinline__ void load4_codes(const void *p, int64_t at, int n, uint8_t (&c)[4])
+{
+    const uint8_t *q = (const uint8_t *)p + at;
+    if (n >= 4) __builtin_memcpy(c, q, 4);
+    else for (int j = 0; j < 4; ++j) c[j] = j < n ? q[j] : 0;
+}
+__device__ __forceinline__ void store4_codes(void *p, int64_t at, int n, const uint8_t (&c)[4])
+{
+    uint8_t *q = (uint8_t *)p + at;
+    if (n >= 4) __builtin_memcpy(q, c, 4);
+    else for (int j = 0; j < 4; ++j) if (j < n) q[j] = c[j];
+}
+
+// Code of x >= 0 under the block's scale, inv = 1 / scale.
+__device__ __forceinline__ float code_of(float x, float inv, float steps)
+{
+    return x > 0.f ? fminf(rintf(sqrtf(x * inv) * steps), steps) : 0.f;
+}
+__device__ __forceinline__ bool finite(float x) { return fabsf(x) <= kFltMax; }
+
+__device__ __forceinline__ int find_tensor(const AdamwList &l, uint32_t block)
+{
+    int lo = 0, hi = l.n - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (l.first[mid] <= block) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+}
+
+template <int BITS>
+__global__ __launch_bounds__(256) void adamw_kernel(const AdamwList l, const AdamwScalars c, const int32_t *skip)
+{
+    if (skip && *skip != 0) return;
+    const int lane = threadIdx.x & 63;
+    const uint32_t blocks = l.first[l.n];
+    for (uint32_t block = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)); block < blocks; block += gridDim.x * 4) {
+        const int i = find_tensor(l, block);
+        const AdamwItem &t = l.item[i];
+        const uint32_t b = block - l.first[i];
+        const int64_t at = (int64_t)b * kBlock + lane * 4;
+        const int n = (int)max((int64_t)0, min((int64_t)4, t.n - at));
+        const int ptype = t.types & 0xFF, gtype = t.types >> 8;
+        float p[4], g[4], m[4], v[4], root[4];
+        if (t.master) load4(t.master, VF_F32, at, n, p); else load4(t.param, ptype, at, n, p);
+        load4(t.grad, gtype, at, n, g);
+        if constexpr (BITS == 32) {
+            load4(t.m, VF_F32, at, n, m);
+            load4(t.v, VF_F32, at, n, v);
+        } else {
+            uint8_t cm[4], cv[4];
+            load4_codes(t.m, at, n, cm);
+            load4_codes(t.v, at, n, cv);
+            const float ms = t.m_scale[b], vs = t.v_scale[b];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { m[j] = m_of((int8_t)cm[j], ms); v[j] = v_of(cv[j], vs); }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float gj = g[j] * c.grad_scale;
+            m[j] = m[j] * c.beta1 + gj * c.one_beta1;
+            v[j] = v[j] * c.beta2 + (gj * gj) * c.one_beta2;
+            root[j] = sqrtf(v[j]);
+            p[j] = p[j] * t.decay - (m[j] * c.c1) / (root[j] * c.c2 + c.eps) * c.lr;
+        }
+        if (t.master) store4(t.master, VF_F32, at, n, p);
+        store4(t.param, ptype, at, n, p);
+        if constexpr (BITS == 32) {
+            store4(t.m, VF_F32, at, n, m);
+            store4(t.v, VF_F32, at, n, v);
+        } else {
+            float ms = 0.f, vs = 0.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (finite(m[j])) ms = fmaxf(ms, fabsf(m[j]));
+                if (finite(root[j])) vs = fmaxf(vs, root[j]);
+            }
+            ms = wave_max(ms);
+            vs = wave_max(vs);
+            const float mi = ms > 0.f ? 1.f / ms : 0.f, vi = vs > 0.f ? 1.f / vs : 0.f;
+            uint8_t cm[4], cv[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float a = code_of(fabsf(m[j]), mi, 127.f);
+                const float r = fmaxf(code_of(root[j], vi, 254.f), root[j] > 0.f ? 1.f : 0.f);
+                cm[j] = finite(m[j]) ? (uint8_t)(int8_t)(m[j] < 0.f ? -(int)a : (int)a) : (uint8_t)0x80;
+                cv[j] = finite(root[j]) ? (uint8_t)(int)r : (uint8_t)255;
+            }
+            store4_codes(t.m, at, n, cm);
+            store4_codes(t.v, at, n, cv);
+            if (lane == 0) { t.m_scale[b] = ms; t.v_scale[b] = vs; }
+        }
+    }
+}
+
+// master: where m goes, param: where v goes.
+template <int BITS> __global__ __launch_bounds__(256) void adamw_moments_kernel(const AdamwList l)
+{
+    const int lane = threadIdx.x & 63;
+    const uint32_t blocks = l.first[l.n];
+    for (uint32_t block = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)); block < blocks; block += gridDim.x * 4) {
+        const int i = find_tensor(l, block);
+        const AdamwItem &t = l.item[i];
+        const uint32_t b = block - l.first[i];
+        const int64_t at = (int64_t)b * kBlock + lane * 4;
+        const int n = (int)max((int64_t)0, min((int64_t)4, t.n - at));
+        float m[4], v[4];
+        if constexpr (BITS == 32) {
+            if (t.master) load4(t.m, VF_F32, at, n, m);
+            if (t.param) load4(t.v, VF_F32, at, n, v);
+        } else {
+            uint8_t cm[4], cv[4];
+            if (t.master) {
+                load4_codes(t.m, at, n, cm);
+                const float ms = t.m_scale[b];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) m[j] = m_of((int8_t)cm[j], ms);
+            }
+            if (t.param) {
+                load4_codes(t.v, at, n, cv);
+                const float vs = t.v_scale[b];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = v_of(cv[j], vs);
+            }
+        }
+        if (t.master) store4(t.master, VF_F32, at, n, m);
+        if (t.param) store4(t.param, VF_F32, at, n, v);
+    }
+}
+
+// Splits the tensors into launches of one width of moments and calls fn(list, bits) for each.
+template <class Fill, class Launch>
+static int each_launch(const vf_adamw_tensor *tensors, int32_t n_tensors, Fill &&fill, Launch &&launch)
+{
+    for (int bits : {32, 8}) {
+        AdamwList l;
+        l.n = 0;
+        l.first[0] = 0;
+        for (int32_t i = 0; i < n_tensors; ++i) {
+            const vf_adamw_tensor &t = tensors[i];
+            if (t.state_bits != bits || t.n == 0) continue;
+            if (l.n == kLaunchTensors) {
+                launch(l, bits);
+                l.n = 0;
+            }
+            fill(i, l.item[l.n]);
+            l.first[l.n + 1] = l.first[l.n] + (uint32_t)ceil_div(t.n, kBlock);
+            ++l.n;
+        }
+        if (l.n > 0) launch(l, bits);
+    }
+    VF_HIP(hipGetLastError());
+    return VF_OK;
+}
+
+// What both entry points ask of a tensor's moments, and that a launch's blocks can be counted in 31 bits.
+static int check_tensors(const vf_adamw_tensor *tensors, int32_t n_tensors)
+{
+    VF_REQUIRE(n_tensors >= 0, "adamw: n_tensors is negative");
+    VF_REQUIRE(n_tensors == 0 || tensors != nullptr, "adamw: tensors is NULL");
+    int64_t blocks = 0;
+    for (int32_t i = 0; i < n_tensors; ++i) {
+        const vf_adamw_tensor &t = tensors[i];
+        const std::string at = "adamw: tensor " + std::to_string(i);
+        VF_REQUIRE(t.n >= 0 && t.n <= (int64_t)INT32_MAX * kBlock, at + ": n out of range");
+        blocks += ceil_div(t.n, kBlock);
+        VF_REQUIRE(blocks <= INT32_MAX, "adamw: too many elements in one call");
+        VF_REQUIRE(t.reserved == 0, at + ": reserved must be zero");
+        VF_REQUIRE(t.state_bits == 32 || t.state_bits == 8, at + ": state_bits must be 32 or 8");
+        if (t.n == 0) continue;
+        VF_REQUIRE(t.m && t.v, at + ": m or v is NULL");
+        VF_REQUIRE(t.state_bits == 32 || (t.m_scale && t.v_scale), at + ": moments in 8 bits need scales");
+    }
+    return VF_OK;
+}
+
+static dim3 grid_of(const AdamwList &l)
+{
+    return dim3((unsigned)std::min<int64_t>(ceil_div((int64_t)l.first[l.n], 4), 256 * 8 * 2));
+}
+
+int adamw_step_impl(const vf_adamw_tensor *tensors, int32_t n_tensors, const vf_adamw_params *params, const int32_t *skip,
+                    hipStream_t s)
+{
+    if (int rc = check_tensors(tensors, n_tensors); rc != VF_OK) return rc;
+    VF_REQUIRE(params != nullptr, "adamw: params is NULL");
+    const vf_adamw_params &h = *params;
+    VF_REQUIRE(h.step >= 1, "adamw: step must be at least 1");
+    VF_REQUIRE(h.beta1 >= 0 && h.beta1 < 1 && h.beta2 >= 0 && h.beta2 < 1, "adamw: betas must lie in [0, 1)");
+    VF_REQUIRE(std::isfinite(h.lr) && h.eps >= 0 && std::isfinite(h.eps) && std::isfinite(h.grad_scale),
+               "adamw: lr, eps and grad_scale must be finite, eps not negative");
+    for (int32_t i = 0; i < n_tensors; ++i) {
+        const vf_adamw_tensor &t = tensors[i];
+        const std::string at = "adamw: tensor " + std::to_string(i);
+        VF_REQUIRE(is_float_type(t.param_type) && is_float_type(t.grad_type), at + ": types must be VF_F32, VF_BF16 or VF_F16");
+        VF_REQUIRE(t.n == 0 || (t.param && t.grad), at + ": param or grad is NULL");
+        VF_REQUIRE(std::isfinite(t.weight_decay), at + ": weight_decay must be finite");
+    }
+    AdamwScalars c;
+    c.beta1 = (float)h.beta1; c.one_beta1 = (float)(1 - h.beta1);
+    c.beta2 = (float)h.beta2; c.one_beta2 = (float)(1 - h.beta2);
+    c.c1 = (float)(1 / (1 - std::pow(h.beta1, (double)h.step)));
+    c.c2 = (float)std::sqrt(1 / (1 - std::pow(h.beta2, (double)h.step)));
+    c.eps = (float)h.eps; c.lr = (float)h.lr; c.grad_scale = (float)h.grad_scale;
+    return each_launch(
+        tensors, n_tensors,
+        [&](int32_t i, AdamwItem &o) {
+            const vf_adamw_tensor &t = tensors[i];
+            o = AdamwItem{t.param, t.grad, t.master, t.m, t.v, t.m_scale, t.v_scale, t.n,
+                          (float)(1 - h.lr * t.weight_decay), t.param_type | t.grad_type << 8};
+        },
+        [&](const AdamwList &l, int bits) {
+            if (bits == 32) adamw_kernel<32><<<grid_of(l), dim3(256), 0, s>>>(l, c, skip);
+            else adamw_kernel<8><<<grid_of(l), dim3(256), 0, s>>>(l, c, skip);
+        });
+}
+
+int adamw_moments_impl(const vf_adamw_tensor *tensors, int32_t n_tensors, float *const *m_out, float *const *v_out,
+                       hipStream_t s)
+{
+    if (int rc = check_tensors(tensors, n_tensors); rc != VF_OK) return rc;
+    VF_REQUIRE(n_tensors == 0 || m_out || v_out, "adamw: m_out and v_out are NULL");
+    return each_launch(
+        tensors, n_tensors,
+        [&](int32_t i, AdamwItem &o) {
+            const vf_adamw_tensor &t = tensors[i];
+            o = AdamwItem{v_out ? v_out[i] : nullptr, nullptr, m_out ? m_out[i] : nullptr, t.m, t.v, t.m_scale, t.v_scale, t.n, 0.f, 0};
+        },
+        [&](const AdamwList &l, int bits) {
+            if (bits == 32) adamw_moments_kernel<32><<<grid_of(l), dim3(256), 0, s>>>(l);
+            else adamw_moments_kernel<8><<<grid_of(l), dim3(256), 0, s>>>(l);
+        });
+}
+
+}  // namespace vf

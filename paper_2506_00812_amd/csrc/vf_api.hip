@@ -1,7 +1,7 @@
 // The C ABI declared in include/vecflow.h.  Every entry point runs its body under a guard, so that no C++
 // exception crosses the boundary; the work itself is in vf_index_build.hip (Alg. 1), vf_route.hip (routing and
 // grouping, host only) and vf_search.hip (Alg. 2).
-#include "vf_host.h"
+#include "vf_ops.h"
 
 using namespace vf;
 
@@ -223,4 +223,115 @@ extern "C" int vf_profile_read(vf_index *index, vf_profile *out, int32_t *per_qu
 extern "C" void vf_index_free(vf_index *index)
 {
     (void)guarded([&] { free_index(index); return VF_OK; });
+}
+
+// ---------------------------------------------------------------- operators of a query encoder
+
+extern "C" int vf_linear(int32_t dtype, int64_t m, int64_t n, int64_t k, const void *x, int64_t ldx, const void *w, int64_t ldw,
+                         const void *bias, int32_t activation, const void *residual, int64_t ldr, void *y, int64_t ldy,
+                         void *z, int64_t ldz, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    return guarded([&] {
+        LinearArgs a{};
+        a.dtype = dtype; a.act = activation; a.m = m; a.n = n; a.k = k;
+        a.x = x; a.ldx = ldx; a.w = w; a.ldw = ldw; a.bias = bias; a.residual = residual; a.ldr = ldr;
+        a.y = y; a.ldy = ldy; a.z = z; a.ldz = ldz;
+        a.workspace = workspace; a.workspace_bytes = workspace_bytes; a.stream = (hipStream_t)hip_stream;
+        return linear_impl(a);
+    });
+}
+
+extern "C" int vf_linear_backward(int32_t dtype, int64_t m, int64_t n, int64_t k, const void *dy, int64_t lddy, const void *x,
+                                  int64_t ldx, const void *w, int64_t ldw, const void *z, int64_t ldz, int32_t activation,
+                                  void *dx, int64_t lddx, void *dw, int64_t lddw, void *dbias, void *workspace,
+                                  size_t workspace_bytes, void *hip_stream)
+{
+    return guarded([&] {
+        LinearArgs a{};
+        a.dtype = dtype; a.act = activation; a.m = m; a.n = n; a.k = k;
+        a.dy = dy; a.lddy = lddy; a.x = x; a.ldx = ldx; a.w = w; a.ldw = ldw; a.z = const_cast<void *>(z); a.ldz = ldz;
+        a.dx = dx; a.lddx = lddx; a.dw = dw; a.lddw = lddw; a.dbias = dbias;
+        a.workspace = workspace; a.workspace_bytes = workspace_bytes; a.stream = (hipStream_t)hip_stream;
+        return linear_backward_impl(a);
+    });
+}
+
+extern "C" int vf_linear_workspace(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t activation, int32_t backward,
+                                   size_t *bytes)
+{
+    return guarded([&] { return linear_workspace_impl(dtype, m, n, k, activation, backward, bytes); });
+}
+
+extern "C" int vf_layer_norm(int32_t dtype, int64_t m, int64_t d, const void *x, int64_t ldx, const void *weight,
+                             const void *bias, double eps, void *y, int64_t ldy, float *mean, float *rstd, void *hip_stream)
+{
+    return guarded([&] {
+        NormArgs a{};
+        a.dtype = dtype; a.m = m; a.d = d; a.x = x; a.ldx = ldx; a.weight = weight; a.bias = bias; a.eps = eps;
+        a.y = y; a.ldy = ldy; a.mean = mean; a.rstd = rstd; a.stream = (hipStream_t)hip_stream;
+        return layer_norm_impl(a);
+    });
+}
+
+extern "C" int vf_layer_norm_backward(int32_t dtype, int64_t m, int64_t d, const void *dy, int64_t lddy, const void *x,
+                                      int64_t ldx, const float *mean, const float *rstd, const void *weight, void *dx,
+                                      int64_t lddx, void *dweight, void *dbias, void *workspace, size_t workspace_bytes,
+                                      void *hip_stream)
+{
+    return guarded([&] {
+        NormArgs a{};
+        a.dtype = dtype; a.m = m; a.d = d; a.dy = dy; a.lddy = lddy; a.x = x; a.ldx = ldx;
+        a.mean = const_cast<float *>(mean); a.rstd = const_cast<float *>(rstd); a.weight = weight;
+        a.y = dx; a.ldy = lddx; a.dweight = dweight; a.dbias = dbias;
+        a.workspace = workspace; a.workspace_bytes = workspace_bytes; a.stream = (hipStream_t)hip_stream;
+        return layer_norm_backward_impl(a);
+    });
+}
+
+extern "C" int vf_layer_norm_workspace(int32_t dtype, int64_t m, int64_t d, size_t *bytes)
+{
+    return guarded([&] { return layer_norm_workspace_impl(dtype, m, d, bytes); });
+}
+
+extern "C" int vf_log_probs(int32_t dtype, int64_t m, int64_t v, const void *logits, int64_t ld, const int32_t *targets,
+                            int32_t top, float *logp, float *entropy, float *lse, int32_t *top_ids, float *top_logp,
+                            void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    return guarded([&] {
+        LogProbArgs a{};
+        a.dtype = dtype; a.top = top; a.m = m; a.v = v; a.logits = logits; a.ld = ld; a.targets = targets;
+        a.logp = logp; a.entropy = entropy; a.lse = lse; a.top_ids = top_ids; a.top_logp = top_logp;
+        a.workspace = workspace; a.workspace_bytes = workspace_bytes; a.stream = (hipStream_t)hip_stream;
+        return log_probs_impl(a);
+    });
+}
+
+extern "C" int vf_log_probs_backward(int32_t dtype, int64_t m, int64_t v, const void *logits, int64_t ld, const float *lse,
+                                     const int32_t *targets, const float *d_logp, const float *entropy,
+                                     const float *d_entropy, void *dlogits, int64_t ldd, void *hip_stream)
+{
+    return guarded([&] {
+        LogProbArgs a{};
+        a.dtype = dtype; a.m = m; a.v = v; a.logits = logits; a.ld = ld; a.lse = const_cast<float *>(lse);
+        a.targets = targets; a.d_logp = d_logp; a.entropy = const_cast<float *>(entropy); a.d_entropy = d_entropy;
+        a.dlogits = dlogits; a.ldd = ldd; a.stream = (hipStream_t)hip_stream;
+        return log_probs_backward_impl(a);
+    });
+}
+
+extern "C" int vf_log_probs_workspace(int32_t dtype, int64_t m, int64_t v, int32_t top, size_t *bytes)
+{
+    return guarded([&] { return log_probs_workspace_impl(dtype, m, v, top, bytes); });
+}
+
+extern "C" int vf_adamw_step(const vf_adamw_tensor *tensors, int32_t n_tensors, const vf_adamw_params *params,
+                             const int32_t *skip, void *hip_stream)
+{
+    return guarded([&] { return adamw_step_impl(tensors, n_tensors, params, skip, (hipStream_t)hip_stream); });
+}
+
+extern "C" int vf_adamw_moments(const vf_adamw_tensor *tensors, int32_t n_tensors, float *const *m_out, float *const *v_out,
+                                void *hip_stream)
+{
+    return guarded([&] { return adamw_moments_impl(tensors, n_tensors, m_out, v_out, (hipStream_t)hip_stream); });
 }

@@ -1,0 +1,339 @@
+// Log probabilities over a vocabulary: one pass over the logits takes the running maximum m, S = sum exp(x - m), A = sum
+// exp(x - m) (x - m) and the largest entries of a row;  lse = m + log S,  logp = (x_t - m) - log S,  entropy = log S - A / S (a sum
+// of two terms that are not negative).  A changed maximum turns (S, A) into f S and f (A + (m - m') S) with f = exp(m - m').
+// Bound by memory where there are many rows.  A row is one wave's, one workgroup's, or (few rows) split into segments whose
+// (m, S, A, largest) a second kernel joins.
+#include "vf_ops.h"
+
+namespace vf {
+
+constexpr float kInf = __builtin_inff();
+
+// Orders values as whole numbers: NaN > +inf > ... > -inf, -0 = +0; with the complement of the label below it, a key orders
+// alternatives (larger first, ties to the lower label).  0: none.
+__device__ __forceinline__ uint32_t value_order(float x)
+{
+    if (x != x) return ~0u;
+    const uint32_t u = __float_as_uint(x + 0.f);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float order_value(uint32_t o)
+{
+    return __uint_as_float(o == ~0u ? 0x7FC00000u : o & 0x80000000u ? o & 0x7FFFFFFFu : ~o);
+}
+
+struct RowSums {
+    float m, s, a;
+};
+
+// The same sums from another origin m >= r.m.  A factor that vanishes (nothing was summed yet, or the origins are far apart: their
+// distance may be infinite) leaves nothing of a; s keeps a NaN.
+__device__ __forceinline__ void scale_to(RowSums &r, float m)
+{
+    if (r.m == m) return;
+    const float d = r.m - m, f = expf(d);
+    r.a = f > 0.f ? f * (r.a + d * r.s) : 0.f;
+    r.s = f * r.s;
+    r.m = m;
+}
+
+__device__ __forceinline__ RowSums wave_join(RowSums r)
+{
+    scale_to(r, wave_max(r.m));
+    r.s = wave_sum(r.s);
+    r.a = wave_sum(r.a);
+    return r;
+}
+
+// The largest keys of a wave: lane i holds the i-th largest of what was offered (all 64 are kept, `top` are asked for).
+struct WaveTop {
+    uint64_t key = 0, least = 0;
+    __device__ __forceinline__ void offer(bool mine, uint64_t k, int top)
+    {
+        const int lane = threadIdx.x & 63;
+        uint64_t mask = __ballot(mine && k > least);
+        while (mask) {
+            const int from = __builtin_ctzll(mask);
+            mask &= mask - 1;
+            const uint64_t in = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), from) << 32 |
+                                (uint32_t)__builtin_amdgcn_readlane((int)k, from);
+            if (in <= least) continue;
+            const int at = __popcll(__ballot(key > in));
+            const uint64_t up = __shfl_up(key, 1, 64);
+            key = lane < at ? key : lane == at ? in : up;
+            least = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(key >> 32), top - 1) << 32 |
+                    (uint32_t)__builtin_amdgcn_readlane((int)key, top - 1);
+        }
+    }
+};
+
+struct LogProbOut {
+    const int32_t *targets;
+    float *logp, *entropy, *lse;
+    int32_t *top_ids;
+    float *top_logp;
+};
+
+// What a row's sums and keys say, written by one wave.
+template <class T>
+__device__ __forceinline__ void finish_row(const LogProbOut &o, const T *x, int64_t row, int64_t v, int top, const RowSums &r, uint64_t key)
+{
+    const int lane = threadIdx.x & 63;
+    const bool empty = r.m == -kInf && r.s == 0.f;
+    const float log_s = logf(r.s);
+    if (lane == 0) {
+        if (o.lse) o.lse[row] = empty ? -kInf : r.m + log_s;
+        if (o.entropy) o.entropy[row] = empty ? 0.f : log_s - r.a / r.s;
+        if (o.targets) {
+            const int32_t t = o.targets[row];
+            float l = 0.f;
+            if (t != -1) {
+                if (t < 0 || t >= v) l = __uint_as_float(0x7FC00000u);
+                else l = empty ? -kInf : ((float)x[t] - r.m) - log_s;
+            }
+            o.logp[row] = l;
+        }
+    }
+    if (lane < top) {
+        o.top_ids[row * top + lane] = key ? (int32_t)~(uint32_t)key : -1;
+        o.top_logp[row * top + lane] = key ? (order_value((uint32_t)(key >> 32)) - r.m) - log_s : -kInf;
+    }
+}
+
+// Segment blockIdx.x % nseg of a row: TPR threads take its vectors in turn.  nseg > 1: the segment's sums and keys go to
+// part_sums [row][nseg] and part_keys [row][nseg][top].
+template <class T, int TPR, bool TOP>
+__global__ __launch_bounds__(256) void log_probs_kernel(int64_t m, int64_t v, const T *__restrict__ logits, int64_t ld, int nseg,
+                                                        int64_t seg, int top, LogProbOut out, float4 *__restrict__ part_sums,
+                                                        uint64_t *__restrict__ part_keys)
+{
+    constexpr int V = kVec<T>, RPB = 256 / TPR, W = TPR / 64;
+    __shared__ float lds_sums[4][3];
+    __shared__ uint64_t lds_keys[TOP && W > 1 ? 4 * 64 : 1];
+    const int t = threadIdx.x % TPR, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t items = m * nseg;
+    for (int64_t item = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR; item < items; item += (int64_t)gridDim.x * RPB) {
+        const int64_t row = nseg == 1 ? item : item / nseg, sg = nseg == 1 ? 0 : item - row * nseg;
+        const T *x = logits + row * ld;
+        const int64_t c0 = sg * seg, c1 = min(v, c0 + seg);
+        RowSums r = {-kInf, 0.f, 0.f};
+        WaveTop best;
+        for (int64_t base = c0; base < c1; base += TPR * V) {
+            const int64_t c = base + t * V;
+            float u[V];
+            float most = -kInf;
+            if (c < c1) {
+                const Vec<T> raw = load_part(x + c, (int)min((int64_t)V, c1 - c), (T)-kInf);
+#pragma unroll
+                for (int j = 0; j < V; ++j) u[j] = (float)raw[j];
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j) u[j] = -kInf;
+            }
+            bool odd = false;   // a NaN, which the maximum passes over
+#pragma unroll
+            for (int j = 0; j < V; ++j) { most = fmaxf(most, u[j]); odd |= u[j] != u[j]; }
+            if (most > r.m) scale_to(r, most);
+            const float origin = r.m == -kInf ? 0.f : r.m;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float d = u[j] - origin, e = expf(d);
+                r.s += e;
+                r.a += e > 0.f ? e * d : 0.f;
+            }
+            if constexpr (TOP) {
+                const uint32_t least = (uint32_t)(best.least >> 32);
+                if (__ballot(odd || (most > -kInf && value_order(most) >= least))) {
+#pragma unroll
+                    for (int j = 0; j < V; ++j)
+                        best.offer(u[j] != -kInf, (uint64_t)value_order(u[j]) << 32 | (uint32_t)~(uint32_t)(c + j), top);
+                }
+            }
+        }
+        r = wave_join(r);
+        if constexpr (W > 1) {
+            __syncthreads();
+            if (lane == 0) { lds_sums[wave][0] = r.m; lds_sums[wave][1] = r.s; lds_sums[wave][2] = r.a; }
+            if (TOP && lane < top) lds_keys[wave * 64 + lane] = best.key;
+            __syncthreads();
+            if (wave == 0) {
+                float most = -kInf;
+#pragma unroll
+                for (int w = 0; w < W; ++w) most = fmaxf(most, lds_sums[w][0]);
+                RowSums all = {most, 0.f, 0.f};
+#pragma unroll
+                for (int w = 0; w < W; ++w) {
+                    RowSums p = {lds_sums[w][0], lds_sums[w][1], lds_sums[w][2]};
+                    scale_to(p, most);
+                    all.s += p.s;
+                    all.a += p.a;
+                }
+                r = all;
+                if constexpr (TOP) {
+                    for (int w = 1; w < W; ++w) best.offer(lane < top, lane < top ? lds_keys[w * 64 + lane] : 0, top);
+                }
+            }
+        }
+        if (W == 1 || wave == 0) {
+            if (nseg == 1) {
+                finish_row(out, x, row, v, TOP ? top : 0, r, best.key);
+            } else {
+                if (lane == 0) part_sums[item] = make_float4(r.m, r.s, r.a, 0.f);
+                if (TOP && lane < top) part_keys[item * top + lane] = best.key;
+            }
+        }
+    }
+}
+
+// One wave per row joins the segments.
+template <class T>
+__global__ __launch_bounds__(64) void log_probs_join_kernel(int64_t m, int64_t v, const T *__restrict__ logits, int64_t ld, int nseg,
+                                                            int top, LogProbOut out, const float4 *__restrict__ part_sums,
+                                                            const uint64_t *__restrict__ part_keys)
+{
+    const int lane = threadIdx.x;
+    for (int64_t row = blockIdx.x; row < m; row += gridDim.x) {
+        RowSums r = {-kInf, 0.f, 0.f};
+        for (int i = lane; i < nseg; i += 64) {
+            const float4 p = part_sums[row * nseg + i];
+            RowSums q = {p.x, p.y, p.z};
+            const float most = fmaxf(r.m, q.m);
+            scale_to(r, most);
+            scale_to(q, most);
+            r.s += q.s;
+            r.a += q.a;
+        }
+        r = wave_join(r);
+        WaveTop best;
+        const int n = nseg * top;
+        for (int i = 0; i < n; i += 64) best.offer(i + lane < n, i + lane < n ? part_keys[row * n + i + lane] : 0, top);
+        finish_row(out, logits + row * ld, row, v, top, r, best.key);
+    }
+}
+
+// dlogits = d_logp (1[target] - p) - d_entropy p (log p + entropy), p = exp(x - lse).  Elementwise; bound by memory.
+template <class T>
+__global__ void log_probs_backward_kernel(int64_t m, int64_t v, const T *logits, int64_t ld, const float *__restrict__ lse,
+                                          const int32_t *__restrict__ targets, const float *__restrict__ d_logp,
+                                          const float *__restrict__ entropy, const float *__restrict__ d_entropy, T *dlogits, int64_t ldd)
+{
+    constexpr int V = kVec<T>;
+    const int64_t c = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) * V;
+    if (c >= v) return;
+    const int n = (int)min((int64_t)V, v - c);
+    for (int64_t row = (int64_t)blockIdx.y * blockDim.y + threadIdx.y; row < m; row += (int64_t)gridDim.y * blockDim.y) {
+        const float l = lse[row];
+        int32_t t = targets ? targets[row] : -1;
+        if (t < 0 || t >= v) t = -1;
+        const float dl = t >= 0 ? d_logp[row] : 0.f;
+        const float dh = d_entropy ? d_entropy[row] : 0.f, h = d_entropy ? entropy[row] : 0.f;
+        const Vec<T> x = load_part(logits + row * ld + c, n, (T)-kInf);
+        Vec<T> o;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const float lp = (float)x[j] - l, p = expf(lp);
+            float g = (t == c + j ? dl : 0.f) - dl * p;
+            g -= p > 0.f || p != p ? dh * (p * (lp + h)) : 0.f;
+            o[j] = (T)(l == -kInf ? 0.f : g);
+        }
+        store_part(dlogits + row * ldd + c, o, n);
+    }
+}
+
+// Threads per row and segments of a row.  Rows of up to 2,048 elements are a wave's; longer ones a workgroup's, in
+// segments where there are too few rows to fill the chip.
+struct LogProbPlan {
+    int tpr, nseg;
+    int64_t seg;
+};
+static LogProbPlan plan_of(int32_t dtype, int64_t m, int64_t v)
+{
+    LogProbPlan p{64, 1, v};
+    const int64_t lane_vecs = 16 / (int64_t)type_size(dtype);
+    if (v <= 2048) return p;
+    p.tpr = 256;
+    const int64_t unit = 256 * lane_vecs;
+    const int64_t want = std::min<int64_t>(ceil_div(1024, m), ceil_div(v, unit));
+    p.seg = ceil_div(ceil_div(v, want), unit) * unit;
+    p.nseg = (int)ceil_div(v, p.seg);
+    return p;
+}
+
+static int check_log_probs(int32_t dtype, int64_t m, int64_t v, int64_t top)
+{
+    VF_REQUIRE(is_float_type(dtype), "log probs: dtype must be VF_F32, VF_BF16 or VF_F16");
+    VF_REQUIRE(m >= 0 && m <= kMaxExtent, "log probs: m out of range");
+    VF_REQUIRE(v >= 1 && v <= kMaxExtent, "log probs: v must be at least 1 and below 2^31");
+    VF_REQUIRE(top >= 0 && top <= VF_LOG_PROBS_MAX_TOP, "log probs: top must be 0 .. VF_LOG_PROBS_MAX_TOP");
+    return VF_OK;
+}
+
+int log_probs_workspace_impl(int32_t dtype, int64_t m, int64_t v, int32_t top, size_t *bytes)
+{
+    VF_REQUIRE(bytes != nullptr, "log probs: bytes is NULL");
+    if (int rc = check_log_probs(dtype, m, v, top); rc != VF_OK) return rc;
+    *bytes = 0;
+    if (m == 0) return VF_OK;
+    const LogProbPlan p = plan_of(dtype, m, v);
+    if (p.nseg > 1) *bytes = (size_t)m * p.nseg * (16 + 8 * (size_t)top);
+    return VF_OK;
+}
+
+int log_probs_impl(const LogProbArgs &a)
+{
+    size_t need = 0;
+    if (int rc = log_probs_workspace_impl(a.dtype, a.m, a.v, a.top, &need); rc != VF_OK) return rc;
+    VF_REQUIRE(a.ld >= a.v, "log probs: ld is less than v");
+    VF_REQUIRE(a.m == 0 || a.logits != nullptr, "log probs: logits is NULL");
+    VF_REQUIRE(a.targets == nullptr || a.logp != nullptr || a.m == 0, "log probs: targets without logp");
+    VF_REQUIRE(a.top == 0 || a.m == 0 || (a.top_ids && a.top_logp), "log probs: top_ids or top_logp is NULL");
+    VF_REQUIRE(need == 0 || (a.workspace != nullptr && a.workspace_bytes >= need),
+               "log probs: the workspace must hold " + std::to_string(need) + " bytes");
+    if (a.m == 0) return VF_OK;
+    const LogProbPlan p = plan_of(a.dtype, a.m, a.v);
+    const LogProbOut out{a.targets, a.logp, a.entropy, a.lse, a.top_ids, a.top_logp};
+    float4 *sums = (float4 *)a.workspace;
+    uint64_t *keys = (uint64_t *)(sums + (p.nseg > 1 ? a.m * p.nseg : 0));
+    by_type(a.dtype, [&](auto *q) {
+        using T = std::remove_pointer_t<decltype(q)>;
+        const T *x = (const T *)a.logits;
+        const int64_t blocks = p.tpr == 64 ? ceil_div(a.m, 4) : a.m * p.nseg;
+        const dim3 grid((unsigned)std::min<int64_t>(blocks, 1 << 20)), block(256);
+        auto launch = [&](auto tpr, auto with_top) {
+            log_probs_kernel<T, tpr.value, with_top.value><<<grid, block, 0, a.stream>>>(a.m, a.v, x, a.ld, p.nseg, p.seg, a.top, out,
+                                                                                         sums, keys);
+        };
+        using W = std::integral_constant<int, 64>;
+        using G = std::integral_constant<int, 256>;
+        if (p.tpr == 64) { if (a.top) launch(W(), std::true_type()); else launch(W(), std::false_type()); }
+        else { if (a.top) launch(G(), std::true_type()); else launch(G(), std::false_type()); }
+        if (p.nseg > 1)
+            log_probs_join_kernel<T><<<dim3((unsigned)std::min<int64_t>(a.m, 1 << 20)), dim3(64), 0, a.stream>>>(
+                a.m, a.v, x, a.ld, p.nseg, a.top, out, sums, keys);
+    });
+    VF_HIP(hipGetLastError());
+    return VF_OK;
+}
+
+int log_probs_backward_impl(const LogProbArgs &a)
+{
+    if (int rc = check_log_probs(a.dtype, a.m, a.v, 0); rc != VF_OK) return rc;
+    VF_REQUIRE(a.ld >= a.v && a.ldd >= a.v, "log probs: ld or ldd is less than v");
+    VF_REQUIRE((a.targets == nullptr) == (a.d_logp == nullptr), "log probs: targets and d_logp go together");
+    VF_REQUIRE((a.entropy == nullptr) == (a.d_entropy == nullptr), "log probs: entropy and d_entropy go together");
+    if (a.m == 0) return VF_OK;
+    VF_REQUIRE(a.logits && a.lse && a.dlogits, "log probs: logits, lse or dlogits is NULL");
+    by_type(a.dtype, [&](auto *q) {
+        using T = std::remove_pointer_t<decltype(q)>;
+        const int64_t nv = ceil_div(a.v, kVec<T>);
+        const dim3 block = nv > 128 ? dim3(256, 1) : nv > 32 ? dim3(64, 4) : dim3(16, 16);
+        const int64_t across = ceil_div(nv, block.x);   // (a launch holds fewer than 2^32 threads)
+        const dim3 grid((unsigned)across, (unsigned)std::min<int64_t>({ceil_div(a.m, block.y), 65535, std::max<int64_t>(1, (1 << 20) / across)}));
+        log_probs_backward_kernel<T><<<grid, block, 0, a.stream>>>(a.m, a.v, (const T *)a.logits, a.ld, a.lse, a.targets, a.d_logp,
+                                                                   a.entropy, a.d_entropy, (T *)a.dlogits, a.ldd);
+    });
+    VF_HIP(hipGetLastError());
+    return VF_OK;
+}
+
+}  // namespace vf

@@ -1,0 +1,178 @@
+// What the kernels and the host code of the encoder operators share: element types, vector loads of any alignment,
+// wave and workgroup sums, activations.  Nothing here is part of the C ABI (see include/vecflow.h).
+#pragma once
+
+#include <cmath>
+#include <type_traits>
+
+#include "vf_host.h"
+
+#pragma clang fp contract(off)
+
+namespace vf {
+
+using bf16 = __bf16;
+using f16 = _Float16;
+
+template <class T> constexpr int kVec = 16 / (int)sizeof(T);   // elements of a 16-byte vector
+template <class T> using Vec = T __attribute__((ext_vector_type(16 / sizeof(T))));
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef float float16v __attribute__((ext_vector_type(16)));
+
+// Calls fn with a null pointer of the element type that dtype names.
+template <class F> void by_type(int32_t dtype, F &&fn)
+{
+    if (dtype == VF_F32) fn((float *)nullptr);
+    else if (dtype == VF_BF16) fn((bf16 *)nullptr);
+    else fn((f16 *)nullptr);
+}
+inline bool is_float_type(int32_t dtype) { return dtype == VF_F32 || dtype == VF_BF16 || dtype == VF_F16; }
+inline size_t type_size(int32_t dtype) { return dtype == VF_F32 ? 4 : 2; }
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+constexpr int64_t kMaxExtent = INT32_MAX;
+
+// A vector at an address that is aligned to an element only: one 16-byte load or store all the same (global memory
+// takes any alignment; rows cut out of a wider matrix start anywhere).
+template <class V, class T> __device__ __forceinline__ V load_vec(const T *p)
+{
+    V v;
+    __builtin_memcpy(&v, p, sizeof(V));
+    return v;
+}
+template <class V, class T> __device__ __forceinline__ void store_vec(T *p, V v) { __builtin_memcpy(p, &v, sizeof(V)); }
+
+// n elements (0 .. a whole vector) at p, the rest `fill`.
+template <class T> __device__ __forceinline__ Vec<T> load_part(const T *p, int n, T fill)
+{
+    if (n >= kVec<T>) return load_vec<Vec<T>>(p);
+    Vec<T> v;
+#pragma unroll
+    for (int i = 0; i < kVec<T>; ++i) v[i] = i < n ? p[i] : fill;
+    return v;
+}
+template <class T> __device__ __forceinline__ void store_part(T *p, Vec<T> v, int n)
+{
+    if (n >= kVec<T>) { store_vec(p, v); return; }
+#pragma unroll
+    for (int i = 0; i < kVec<T>; ++i)
+        if (i < n) p[i] = v[i];
+}
+
+// Sum over the 64 lanes of a wave, the same in every lane.
+__device__ __forceinline__ float wave_sum(float v)
+{
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d, 64);
+    return v;
+}
+__device__ __forceinline__ float wave_max(float v)
+{
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d, 64));
+    return v;
+}
+
+// The activations at infinite z are their limits (0 at -inf, where the products below would be NaN); NaN stays NaN.
+constexpr float kFltMax = 3.4028234663852886e38f;
+__device__ __forceinline__ float act_value(float z, int act)
+{
+    if (act == VF_ACT_NONE) return z;
+    if (act == VF_ACT_RELU) return z < 0.f ? 0.f : z;
+    const float u = z < -kFltMax ? -kFltMax : z;
+    if (act == VF_ACT_GELU) return 0.5f * u * (1.f + erff(u * 0.70710678118654752f));
+    return u / (1.f + expf(-u));
+}
+__device__ __forceinline__ float act_slope(float z, int act)
+{
+    if (act == VF_ACT_NONE) return 1.f;
+    if (act == VF_ACT_RELU) return z > 0.f ? 1.f : z != z ? z : 0.f;
+    const float u = z < -kFltMax ? -kFltMax : z > kFltMax ? kFltMax : z;
+    if (act == VF_ACT_GELU)
+        return 0.5f * (1.f + erff(u * 0.70710678118654752f)) + u * expf(-0.5f * u * u) * 0.39894228040143268f;
+    const float a = 1.f / (1.f + expf(-u));
+    return a * (1.f + u * (1.f - a));
+}
+
+// Column sums from partial rows part [parts][sums][d]: 64 columns and one of the sums per workgroup; parts = 0: zeros.
+template <class T>
+__global__ __launch_bounds__(1024) void join_parts_kernel(int parts, int64_t d, const float *__restrict__ part, T *out0, T *out1)
+{
+    __shared__ float comb[16][64];
+    const int t = threadIdx.x & 63, sub = threadIdx.x >> 6;
+    const int64_t c = (int64_t)blockIdx.x * 64 + t;
+    T *out = blockIdx.y == 0 ? out0 : out1;
+    if (out == nullptr) return;
+    float a = 0.f;
+    if (c < d)
+        for (int p = sub; p < parts; p += 16) a += part[((int64_t)p * gridDim.y + blockIdx.y) * d + c];
+    comb[sub][t] = a;
+    __syncthreads();
+    if (sub == 0 && c < d) {
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s += comb[i][t];
+        out[c] = (T)s;
+    }
+}
+template <class T> void launch_join_parts(int parts, int64_t d, int sums, const float *part, T *out0, T *out1, hipStream_t s)
+{
+    join_parts_kernel<T><<<dim3((unsigned)ceil_div(d, 64), (unsigned)sums), dim3(1024), 0, s>>>(parts, d, part, out0, out1);
+}
+
+// ---------------------------------------------------------------- entry points' bodies
+
+struct LinearArgs {
+    int32_t dtype, act;
+    int64_t m, n, k;
+    const void *x, *w, *bias, *residual, *dy;
+    int64_t ldx, ldw, ldr, lddy;
+    void *y, *z, *dx, *dw, *dbias;
+    int64_t ldy, ldz, lddx, lddw;
+    void *workspace;
+    size_t workspace_bytes;
+    hipStream_t stream;
+};
+int linear_impl(const LinearArgs &a);
+int linear_backward_impl(const LinearArgs &a);
+int linear_workspace_impl(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t act, int32_t backward, size_t *bytes);
+
+struct NormArgs {
+    int32_t dtype;
+    int64_t m, d;
+    const void *x, *dy, *weight, *bias;
+    int64_t ldx, lddy, ldy;
+    double eps;
+    void *y, *dweight, *dbias;   // y: the gradient dx in the backward pass
+    float *mean, *rstd;
+    void *workspace;
+    size_t workspace_bytes;
+    hipStream_t stream;
+};
+int layer_norm_impl(const NormArgs &a);
+int layer_norm_backward_impl(const NormArgs &a);
+int layer_norm_workspace_impl(int32_t dtype, int64_t m, int64_t d, size_t *bytes);
+
+struct LogProbArgs {
+    int32_t dtype, top;
+    int64_t m, v, ld, ldd;
+    const void *logits;
+    const int32_t *targets;
+    float *logp, *entropy, *lse;
+    int32_t *top_ids;
+    float *top_logp;
+    const float *d_logp, *d_entropy;
+    void *dlogits;
+    void *workspace;
+    size_t workspace_bytes;
+    hipStream_t stream;
+};
+int log_probs_impl(const LogProbArgs &a);
+int log_probs_backward_impl(const LogProbArgs &a);
+int log_probs_workspace_impl(int32_t dtype, int64_t m, int64_t v, int32_t top, size_t *bytes);
+
+int adamw_step_impl(const vf_adamw_tensor *tensors, int32_t n_tensors, const vf_adamw_params *params, const int32_t *skip,
+                    hipStream_t s);
+int adamw_moments_impl(const vf_adamw_tensor *tensors, int32_t n_tensors, float *const *m_out, float *const *v_out,
+                       hipStream_t s);
+
+}  // namespace vf

@@ -1,0 +1,184 @@
+"""AdamW over lists of tensors: bit for bit against single float32 operations in the stated order (numpy), and within their
+rounding (a few 2^-24 per operation, a step of the code for 8-bit moments) against the formulas in 64 bits."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2506_00812_amd import binding as vf
+
+pytestmark = pytest.mark.gpu
+F = np.float32
+B = 256
+
+
+def decode(cm, cv, ms, vs):
+    n = cm.size
+    a, b = cm.astype(F) * F(1 / 127), cv.astype(F) * F(1 / 254)
+    r = np.repeat(vs, B)[:n] * (b * b)
+    return np.repeat(ms, B)[:n] * (a * np.abs(a)), r * r
+
+
+def encode(x, steps):
+    """(codes of x >= 0, scales)"""
+    n = x.size
+    p = np.pad(x, (0, -n % B)).reshape(-1, B)
+    s = p.max(1)
+    inv = np.where(s > 0, F(1) / np.where(s > 0, s, F(1)), F(0)).astype(F)
+    c = np.minimum(np.rint(np.sqrt(p * inv[:, None]) * F(steps)), F(steps))
+    return c.reshape(-1)[:n], s
+
+
+def step(w, g, m, v, t, lr, b1, b2, eps, wd, gs=1.0):
+    g = g * F(gs)
+    m = m * F(b1) + g * F(1 - b1)
+    v = v * F(b2) + (g * g) * F(1 - b2)
+    root = np.sqrt(v)
+    w = w * F(1 - lr * wd) - (m * F(1 / (1 - b1 ** t))) / (root * F(math.sqrt(1 / (1 - b2 ** t))) + F(eps)) * F(lr)
+    return w, m, v, root
+
+
+def same(a, b, what):
+    a, b = np.asarray(a), np.asarray(b)
+    assert a.dtype == b.dtype and np.array_equal(a.view(np.uint8), b.view(np.uint8)), f"{what}: {np.flatnonzero(a != b)[:5]}"
+
+
+SIZES = [1, 2, 255, 256, 257, 1000, 4096, 12345, 0, 3]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_steps_bit_for_bit(bits, dtype):
+    rng = np.random.default_rng(3)
+    sizes = SIZES * 6                                            # more than one launch holds
+    W = [rng.standard_normal(n).astype(F) for n in sizes]
+    lead = [i % 3 for i in range(len(sizes))]                    # tensors that start anywhere
+    place = lambda a, i, T: torch.cat([torch.zeros(lead[i], dtype=T), torch.from_numpy(a).to(T)]).cuda()[lead[i]:]   # noqa: E731
+    master = dtype != torch.float32
+    p = [place(w, i, dtype) for i, w in enumerate(W)]
+    ws = [place(w, i, torch.float32) if i % 2 else None for i, w in enumerate(W)] if master else None
+    W = [w if not master or i % 2 else p[i].float().cpu().numpy() for i, w in enumerate(W)]
+    st = [vf.adamw_state(t, bits) for t in p]
+    M, V = [np.zeros(n, F) for n in sizes], [np.zeros(n, F) for n in sizes]
+    decay = [0.1 * (i % 2) for i in range(len(sizes))]
+    for t in (1, 2, 3):
+        G = [(rng.standard_normal(n) * 10.0 ** rng.integers(-4, 2, n)).astype(F) for n in sizes]
+        g = [place(x, i, dtype if i % 3 else torch.float32) for i, x in enumerate(G)]
+        G = [x.float().cpu().numpy() for x in g]
+        vf.adamw_step(p, g, [s[0] for s in st], [s[1] for s in st], step=t, lr=1e-2, betas=(0.9, 0.99), eps=1e-8, weight_decay=decay, masters=ws,
+                      grad_scale=0.5, m_scales=[s[2] for s in st] if bits == 8 else None, v_scales=[s[3] for s in st] if bits == 8 else None)
+        for i, n in enumerate(sizes):
+            W[i], M[i], V[i], root = step(W[i], G[i], M[i], V[i], t, 1e-2, 0.9, 0.99, 1e-8, decay[i], 0.5)
+            low = torch.from_numpy(W[i]).to(dtype)
+            same(p[i].cpu().view(torch.int16 if master else torch.int32).numpy(), low.view(torch.int16 if master else torch.int32).numpy(), f"parameter {i}")
+            if master and ws[i] is not None:
+                same(ws[i].cpu().numpy(), W[i], f"master {i}")
+            elif master:
+                W[i] = low.float().numpy()
+            if bits == 32:
+                same(st[i][0].cpu().numpy(), M[i], "m")
+                same(st[i][1].cpu().numpy(), V[i], "v")
+                continue
+            if n == 0:
+                continue
+            cm, ms = encode(np.abs(M[i]), 127)
+            cv, vs = encode(root, 254)
+            cm, cv = (cm * np.sign(M[i])).astype(np.int8), np.maximum(cv, root > 0).astype(np.uint8)
+            for k, x in enumerate((cm, cv, ms, vs)):
+                same(st[i][k].cpu().numpy(), x, f"state {k} of tensor {i}")
+            M[i], V[i] = decode(cm, cv, ms, vs)
+    out = vf.adamw_moments([s[0] for s in st], [s[1] for s in st], [s[2] for s in st] if bits == 8 else None, [s[3] for s in st] if bits == 8 else None)
+    for i in range(len(sizes)):
+        same(out[0][i].cpu().numpy(), M[i], "m read back")
+        same(out[1][i].cpu().numpy(), V[i], "v read back")
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_against_64_bits(bits):
+    """One step from zero moments: m = (1 - beta1) g, sqrt(v) = sqrt(1 - beta2) |g|.  A code is off by half a step: for x = s (c / K)^2 that
+    is at most s (c + 1/4) / K^2 <= sqrt(x s) / K + s / (4 K^2); the parameter's update takes the unrounded moments."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    n = 100_000
+    p = torch.randn(n, generator=g, device="cuda")
+    grad = torch.randn(n, generator=g, device="cuda") ** 3
+    st = vf.adamw_state(p, bits)
+    P, G = p.double(), grad.double()
+    vf.adamw_step([p], [grad], [st[0]], [st[1]], step=1, lr=1e-2, eps=1e-6, weight_decay=0.1, m_scales=[st[2]] if bits == 8 else None,
+                  v_scales=[st[3]] if bits == 8 else None)
+    want = P * (1 - 1e-3) - 1e-2 * G / (G.abs() + 1e-6)
+    assert ((p.double() - want).abs() <= 8 * 2.0 ** -24 * (P.abs() + 1e-2) + 1e-2 * 2.0 ** -20).all()
+    (m,), (v,) = vf.adamw_moments([st[0]], [st[1]], [st[2]] if bits == 8 else None, [st[3]] if bits == 8 else None)
+    for got, x, K in ((m.double(), 0.1 * G, 127), (v.double().sqrt(), math.sqrt(1e-3) * G.abs(), 254)):
+        tol = 2.0 ** -20 * x.abs()
+        if bits == 8:
+            s = torch.nn.functional.pad(x.abs(), (0, -n % B)).view(-1, B).amax(1).repeat_interleave(B)[:n]
+            tol = tol + (torch.sqrt(x.abs() * s) / K + s / (4 * K * K)) * 1.001
+            if K == 254:
+                tol = tol.maximum(s / (K * K) * 1.001)       # a v > 0 keeps at least the first code
+        assert ((got - x).abs() <= tol).all()
+
+
+def test_non_finite_gradients_stay_with_their_element():
+    n = 700
+    for bits in (32, 8):
+        p = torch.ones(n, device="cuda")
+        g = torch.full((n,), 0.1, device="cuda")
+        g[300], g[400], g[699] = math.nan, math.inf, -math.inf
+        st = vf.adamw_state(p, bits)
+        sc = dict(m_scales=[st[2]], v_scales=[st[3]]) if bits == 8 else {}
+        for t in (1, 2):
+            vf.adamw_step([p], [g], [st[0]], [st[1]], step=t, lr=0.1, **sc)
+        bad = torch.zeros(n, dtype=torch.bool, device="cuda")
+        bad[[300, 400, 699]] = True
+        assert torch.isfinite(p[~bad]).all() and torch.isnan(p[bad]).all()
+        (m,), (v,) = vf.adamw_moments([st[0]], [st[1]], sc.get("m_scales"), sc.get("v_scales"))
+        assert torch.allclose(m[~bad], torch.tensor(0.019, device="cuda"), rtol=0.02) and not torch.isfinite(m[bad]).any()
+        assert torch.isfinite(v[~bad]).all() and not torch.isfinite(v[bad]).any()
+
+
+def test_tiny_and_zero_gradients():
+    for scale in (0.0, 1e-30, 1e-40, 1e-44):
+        p = torch.ones(600, device="cuda")
+        st = vf.adamw_state(p, 8)
+        g = torch.full((600,), scale, device="cuda")
+        for t in (1, 2):
+            vf.adamw_step([p], [g], [st[0]], [st[1]], step=t, lr=0.1, eps=1e-8, m_scales=[st[2]], v_scales=[st[3]])
+        assert torch.isfinite(p).all() and (p <= 1).all() and (scale or (p == 1).all())
+        (m,), (v,) = vf.adamw_moments([st[0]], [st[1]], [st[2]], [st[3]])
+        assert torch.isfinite(m).all() and torch.isfinite(v).all() and (m >= 0).all()
+
+
+def test_skip_flag_and_stream():
+    p = torch.ones(1000, device="cuda")
+    g = torch.ones(1000, device="cuda")
+    m, v = vf.adamw_state(p)
+    flag = torch.ones(1, dtype=torch.int32, device="cuda")
+    vf.adamw_step([p], [g], [m], [v], step=1, lr=0.1, skip=flag)
+    assert (p == 1).all() and not m.any() and not v.any()
+    flag.zero_()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    vf.adamw_step([p], [g], [m], [v], step=1, lr=0.1, skip=flag, stream=s)
+    s.synchronize()
+    assert ((p - 0.9).abs() < 1e-6).all() and m.all()
+
+
+def test_refusals():
+    p, g = torch.ones(300, device="cuda"), torch.ones(300, device="cuda")
+    m, v = vf.adamw_state(p)
+    m8, v8, a, b = vf.adamw_state(p, 8)
+    ok = dict(step=1, lr=0.1)
+    bad = [lambda: vf.adamw_step([p], [g], [m], [v], step=0, lr=0.1), lambda: vf.adamw_step([p], [g[:9]], [m], [v], **ok),
+           lambda: vf.adamw_step([p], [], [m], [v], **ok), lambda: vf.adamw_step([p.double()], [g], [m], [v], **ok),
+           lambda: vf.adamw_step([p], [g], [m8], [v8], **ok), lambda: vf.adamw_step([p], [g], [m8], [v], m_scales=[a], v_scales=[b], **ok),
+           lambda: vf.adamw_step([p], [g], [m8], [v8], m_scales=[a[:1]], v_scales=[b], **ok),
+           lambda: vf.adamw_step([p], [g], [m], [v], betas=(1.0, 0.9), **ok), lambda: vf.adamw_step([p], [g], [m], [v], step=1, lr=math.nan),
+           lambda: vf.adamw_step([p], [g], [m], [v], eps=-1.0, **ok), lambda: vf.adamw_step([p], [g.cpu()], [m], [v], **ok),
+           lambda: vf.adamw_step([p], [g], [m], [v], weight_decay=[0.1, 0.2], **ok), lambda: vf.adamw_state(p, 16),
+           lambda: vf.adamw_step([p[::2]], [g[:150]], [m[:150]], [v[:150]], **ok)]
+    for f in bad:
+        with pytest.raises(vf.VecflowError):
+            f()
+    vf.adamw_step([], [], [], [], **ok)
