@@ -6,6 +6,7 @@
 //     dx        P = w  (along rows),   Q = dz (along c),     c = n
 //     dw        P = x  (along rows),   Q = dz (along rows),  c = m
 // P takes the matrix instruction's first operand, so that a lane's four accumulators are neighbours in a row of the output.
+#include "vf_device.h"
 #include "vf_ops.h"
 
 namespace vf {
@@ -38,34 +39,54 @@ template <class T> struct Epilogue {
     int64_t ldz;
 };
 
-// Writes n (1 .. 4) neighbouring outputs of row q from column p on.
-template <class T>
-__device__ __forceinline__ void finish4(const Epilogue<T> &e, int64_t q, int64_t p, int n, float4v a)
+// N neighbours of a row, n (1 .. N) of which exist.
+template <class T, int N> __device__ __forceinline__ void load_row(const T *p, int n, float (&o)[N])
 {
-    using V4 = T __attribute__((ext_vector_type(4)));
-    V4 out, pre, res;
-    if (e.residual && n == 4) res = load_vec<V4>(e.residual + q * e.ldr + p);
+    using V = T __attribute__((ext_vector_type(N)));
+    if (n == N) {
+        const V v = load_vec<V>(p);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (i >= n) break;
-        float z = a[i];
-        if (e.bias) z += (float)e.bias[p + i];
-        pre[i] = (T)z;
-        float y = act_value(z, e.act);
-        if (e.residual) y += n == 4 ? (float)res[i] : (float)e.residual[q * e.ldr + p + i];
-        out[i] = (T)y;
-    }
-    if (n == 4) {
-        if (e.z) store_vec(e.z + q * e.ldz + p, pre);
-        store_vec(e.y + q * e.ldy + p, out);
+        for (int i = 0; i < N; ++i) o[i] = (float)v[i];
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (i >= n) break;
-            if (e.z) e.z[q * e.ldz + p + i] = pre[i];
-            e.y[q * e.ldy + p + i] = out[i];
-        }
+        for (int i = 0; i < N; ++i) o[i] = i < n ? (float)p[i] : 0.f;
     }
+}
+template <class T, int N> __device__ __forceinline__ void store_row(T *p, int n, const float (&o)[N])
+{
+    using V = T __attribute__((ext_vector_type(N)));
+    V v;
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = (T)o[i];
+    if (n == N) {
+        store_vec(p, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < n) p[i] = v[i];
+    }
+}
+// The epilogue: outputs p .. p + n - 1 of row q.
+template <class T, int N> __device__ __forceinline__ void finish(const Epilogue<T> &e, int64_t q, int64_t p, int n, float (&v)[N])
+{
+    float u[N];
+    if (e.bias) {
+        load_row(e.bias + p, n, u);
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += u[i];
+    }
+    if (e.z) store_row(e.z + q * e.ldz + p, n, v);
+    if (e.act != VF_ACT_NONE)
+        by_act(e.act, [&](auto act) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = act_value<act.value>(v[i]);
+        });
+    if (e.residual) {
+        load_row(e.residual + q * e.ldr + p, n, u);
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += u[i];
+    }
+    store_row(e.y + q * e.ldy + p, n, v);
 }
 
 template <class T> struct Product {
@@ -167,10 +188,424 @@ __global__ __launch_bounds__(256) void product_kernel(Product<T> a, Epilogue<T> 
                 if (n == 4) store_vec(to, acc[i][j]);
                 else for (int u = 0; u < n; ++u) to[u] = acc[i][j][u];
             } else {
-                finish4(e, q, p, n, acc[i][j]);
+                float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+                finish(e, q, p, n, v);
             }
         }
     }
+}
+
+// ---------------------------------------------------------------- few rows
+
+// At most 16 FQ rows of Q (queries that are served one by one or in small batches): the work is one read of P, so no tile is shared and
+// nothing waits for another wave until the end.  A workgroup has 16 rows of P; its waves share the contraction in whole fragments, loaded
+// from memory straight into the matrix instruction's layout, several in flight, and add up through LDS.
+// One row, 4096 x 1024 in bfloat16 (8 MB of weights): 4.7 us; 64 x 64 tiles over a split contraction and their join took 13.
+template <class T, int FQ>
+__global__ __launch_bounds__(1024) void few_rows_kernel(Product<T> a, Epilogue<T> e)
+{
+    constexpr int V = kVec<T>, BC = 4 * V, AHEAD = FQ > 2 ? 2 : 4;
+    __shared__ __align__(16) float4v sums[16][FQ][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    const int64_t p0 = (int64_t)blockIdx.x * 16;
+    const T *P = a.P + min(p0 + (lane & 15), a.np - 1) * a.ldp;   // (rows beyond the last repeat it: their results are not kept)
+    const T *Q[FQ];
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) Q[j] = a.Q + min((int64_t)(j * 16 + (lane & 15)), a.nq - 1) * a.ldq;
+    float4v acc[FQ] = {};
+    const int64_t whole = a.nc / BC;   // fragments that the contraction fills
+    int64_t f = wave;
+    for (; f + (AHEAD - 1) * waves < whole; f += AHEAD * waves) {
+        Vec<T> fp[AHEAD], fq[AHEAD][FQ];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int64_t c = (f + u * waves) * BC + (lane >> 4) * V;
+            fp[u] = load_vec<Vec<T>>(P + c);
+#pragma unroll
+            for (int j = 0; j < FQ; ++j) fq[u][j] = load_vec<Vec<T>>(Q[j] + c);
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+            for (int j = 0; j < FQ; ++j) acc[j] = mma(fp[u], fq[u][j], acc[j]);
+    }
+    for (; f * BC < a.nc; f += waves) {
+        const int64_t c = f * BC + (lane >> 4) * V;
+        const int n = (int)max((int64_t)0, min((int64_t)V, a.nc - c));
+        const Vec<T> fp = load_part(P + c, n, (T)0.f);
+#pragma unroll
+        for (int j = 0; j < FQ; ++j) acc[j] = mma(fp, load_part(Q[j] + c, n, (T)0.f), acc[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) sums[wave][j][lane] = acc[j];
+    __syncthreads();
+    for (int j = wave; j < FQ; j += waves) {
+        float v[4] = {};
+        for (int w = 0; w < waves; ++w) {
+            const float4v u = sums[w][j][lane];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] += u[i];
+        }
+        const int64_t q = j * 16 + (lane & 15), p = p0 + (lane >> 4) * 4;
+        if (q < a.nq && p < a.np) finish(e, q, p, (int)min((int64_t)4, a.np - p), v);
+    }
+}
+
+// ---------------------------------------------------------------- large products
+
+// Where element chunks live in a tile in LDS.  An operand that is contiguous along c keeps rows of 128 bytes (eight 16-byte chunks
+// at chunk ^ (row % 8)); one that is contiguous along its rows keeps the lines of c as they come, in pieces that the matrix
+// instruction's lanes gather with transposing reads (2-byte types) or element by element (float32); the pieces of
+// a line are permuted by c so that the lines that one read touches lie in different banks.
+template <class T> __device__ __forceinline__ int line_place(int c, int line_bytes, int byte)
+{
+    if constexpr (sizeof(T) == 2) return c * line_bytes + (byte ^ (((c & 3) | (c >> 1 & 4)) << 5));
+    else return c * line_bytes + (byte ^ ((c >> 2 & 3) << 6));
+}
+
+typedef short short4v __attribute__((ext_vector_type(4)));
+
+// The fragment of rows r0 .. r0 + 15 and 64 bytes (half h) of the contraction.
+template <class T, bool ALONG_C, int ROWS> __device__ __forceinline__ Vec<T> fragment(const unsigned char *tile, int r0, int h, int lane)
+{
+    if constexpr (ALONG_C) {
+        const int r = r0 + (lane & 15), ch = h * 4 + (lane >> 4);
+        return *(const Vec<T> *)(tile + r * kRowBytes + ((ch ^ (r & 7)) << 4));
+    } else if constexpr (sizeof(T) == 2) {
+        // a transposing read hands lane i of sixteen the column i of the four lines whose pieces lanes 4 c .. 4 c + 3 address
+        const int c = h * 32 + (lane >> 4) * 8 + (lane >> 2 & 3);
+        const unsigned char *at = tile + line_place<T>(c, ROWS * 2, (r0 + (lane & 3) * 4) * 2);
+        using P = __attribute__((address_space(3))) short4v *;
+        const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)at);
+        const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(at + 4 * ROWS * 2));
+        Vec<T> f;
+        __builtin_memcpy(&f, &lo, 8);
+        __builtin_memcpy((char *)&f + 8, &hi, 8);
+        return f;
+    } else {
+        const int c = h * 16 + (lane >> 4) * 4;
+        const unsigned char *at = tile + line_place<T>(c, ROWS * 4, (r0 + (lane & 15)) * 4);
+        Vec<T> f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = *(const T *)(at + i * ROWS * 4);
+        return f;
+    }
+}
+
+// One thread's share of an operand's tile on its way from memory to LDS.
+template <class T, bool ALONG_C, int ROWS, int THREADS> struct Stage {
+    static constexpr int V = kVec<T>, BC = kRowBytes / (int)sizeof(T), N = ROWS * 8 / THREADS;
+    static constexpr int kLine = ROWS / V;   // vectors of a line of c
+    Vec<T> v[N];
+    const T *at;        // whole tiles: this thread's first vector in the next step
+    int64_t ld, r0, rows;
+    const T *src;
+
+    __device__ __forceinline__ void begin(const T *src_, int64_t ld_, int64_t r0_, int64_t rows_, int64_t c0)
+    {
+        src = src_; ld = ld_; r0 = r0_; rows = rows_;
+        const int t = threadIdx.x;
+        if constexpr (ALONG_C) at = src + r0 * ld + c0 + t % 8 * V;
+        else at = src + (c0 + t / kLine) * ld + r0 + t % kLine * V;
+    }
+    __device__ __forceinline__ void whole(int)
+    {
+        const int t = threadIdx.x;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if constexpr (ALONG_C) {   // rows beyond the last repeat it: their results are not kept
+                const int64_t r = min((int64_t)(t / 8 + i * (THREADS / 8)), rows - 1 - r0);
+                v[i] = load_vec<Vec<T>>(at + r * ld);
+            } else {
+                v[i] = load_vec<Vec<T>>(at + (int64_t)(i * (THREADS / kLine)) * ld);
+            }
+        }
+        at += ALONG_C ? BC : BC * ld;
+    }
+    // a step that leaves the operand: zeros beyond its rows and beyond c_end
+    __device__ __forceinline__ void part(int64_t c0, int64_t c_end)
+    {
+        const int t = threadIdx.x;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int id = t + i * THREADS;
+            if constexpr (ALONG_C) {
+                const int64_t r = r0 + id / 8, c = c0 + id % 8 * V;
+                v[i] = load_part(src + r * ld + c, r < rows ? (int)min((int64_t)V, max((int64_t)0, c_end - c)) : 0, (T)0.f);
+            } else {
+                const int64_t c = c0 + id / kLine, r = r0 + id % kLine * V;
+                v[i] = load_part(src + c * ld + r, c < c_end ? (int)min((int64_t)V, max((int64_t)0, rows - r)) : 0, (T)0.f);
+            }
+        }
+        at += ALONG_C ? BC : BC * ld;
+    }
+    __device__ __forceinline__ void keep(unsigned char *tile) const
+    {
+        const int t = threadIdx.x;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int id = t + i * THREADS;
+            if constexpr (ALONG_C) {
+                const int r = id / 8, ch = id % 8;
+                *(Vec<T> *)(tile + r * kRowBytes + ((ch ^ (r & 7)) << 4)) = v[i];
+            } else {
+                *(Vec<T> *)(tile + line_place<T>(id / kLine, ROWS * (int)sizeof(T), id % kLine * 16)) = v[i];
+            }
+        }
+    }
+};
+
+// The end of a workgroup: each wave turns sixteen rows of its accumulators at a time through LDS, so that its stores are whole stretches
+// of a row (half the time of the eight-byte pieces that a lane holds).
+template <class T, int FP, int FQ, int WAVE_P, int WAVE_Q>
+__device__ __forceinline__ void store_tile(const Product<T> &a, const Epilogue<T> &e, const float4v (&acc)[FP][FQ], unsigned char *lds, int wave,
+                                           int lane, int64_t p_first, int64_t q_first)
+{
+    constexpr int kRow = WAVE_P * 4 + 16, kLanes = WAVE_P / 8;   // 16 bytes more: rows start in other banks
+    unsigned char *turn = lds + wave * (16 * kRow);
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) {
+#pragma unroll
+        for (int i = 0; i < FP; ++i) *(float4v *)(turn + (lane & 15) * kRow + (i * 16 + (lane >> 4) * 4) * 4) = acc[i][j];
+        wave_sync<true>();
+#pragma unroll 1
+        for (int r = lane / kLanes; r < 16; r += 64 / kLanes) {
+            const int64_t q = q_first + j * 16 + r, p = p_first + lane % kLanes * 8;
+            float v[8];
+            *(float4v *)v = *(const float4v *)(turn + r * kRow + lane % kLanes * 32);
+            *(float4v *)(v + 4) = *(const float4v *)(turn + r * kRow + lane % kLanes * 32 + 16);
+            if (q >= a.nq || p >= a.np) continue;
+            const int m = (int)min((int64_t)8, a.np - p);
+            if (a.splits > 1) {
+                float *to = a.part + ((int64_t)blockIdx.y * a.nq + q) * a.np + p;
+                if (m == 8) {
+                    store_vec(to, *(float4v *)v);
+                    store_vec(to + 4, *(float4v *)(v + 4));
+                } else {
+#pragma unroll
+                    for (int u = 0; u < 8; ++u)
+                        if (u < m) to[u] = v[u];
+                }
+            } else {
+                finish(e, q, p, m, v);
+            }
+        }
+        wave_sync<true>();
+    }
+}
+
+// BP x BQ outputs per workgroup of WP x WQ waves; two tiles of each operand in LDS, one being read while the other is filled.
+template <class T, bool PC, bool QC, int BP, int BQ, int WP, int WQ>
+__global__ __launch_bounds__(WP *WQ * 64) void tile_kernel(Product<T> a, Epilogue<T> e)
+{
+    constexpr int THREADS = WP * WQ * 64, BC = kRowBytes / (int)sizeof(T), FP = BP / WP / 16, FQ = BQ / WQ / 16;
+    extern __shared__ __align__(16) unsigned char tiles[];   // [2][(BP + BQ) * kRowBytes]
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t tiles_p = (a.np + BP - 1) / BP;
+    // neighbouring workgroups go to the eight XCDs in turn: each XCD takes a run of neighbouring tiles, whose operands its L2 holds
+    const int64_t n = gridDim.x, xcd = blockIdx.x & 7, run = n / 8, left = n % 8;
+    const int64_t tile = xcd * run + min(xcd, left) + (blockIdx.x >> 3);
+    const int64_t p0 = tile % tiles_p * BP, q0 = tile / tiles_p * BQ;
+    const int64_t c_first = (int64_t)blockIdx.y * a.chunk, c_end = min(a.nc, c_first + a.chunk);
+    const bool p_whole = PC || p0 + BP <= a.np, q_whole = QC || q0 + BQ <= a.nq;
+
+    Stage<T, PC, BP, THREADS> sp;
+    Stage<T, QC, BQ, THREADS> sq;
+    sp.begin(a.P, a.ldp, p0, a.np, c_first);
+    sq.begin(a.Q, a.ldq, q0, a.nq, c_first);
+    auto fetch = [&](int64_t c0) {
+        const bool c_whole = c0 + BC <= c_end;
+        if (c_whole && p_whole) sp.whole(0); else sp.part(c0, c_end);
+        if (c_whole && q_whole) sq.whole(0); else sq.part(c0, c_end);
+    };
+    const int wp = wave % WP * (BP / WP), wq = wave / WP * (BQ / WQ);
+    float4v acc[FP][FQ] = {};
+    unsigned char *now = tiles, *next = tiles + (BP + BQ) * kRowBytes;
+    if (c_first < c_end) {
+        fetch(c_first);
+        sp.keep(now);
+        sq.keep(now + BP * kRowBytes);
+    }
+    for (int64_t c0 = c_first; c0 < c_end; c0 += BC) {
+        __syncthreads();
+        const bool more = c0 + BC < c_end;
+        if (more) fetch(c0 + BC);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            Vec<T> fp[FP], fq[FQ];
+#pragma unroll
+            for (int i = 0; i < FP; ++i) fp[i] = fragment<T, PC, BP>(now, wp + i * 16, h, lane);
+#pragma unroll
+            for (int j = 0; j < FQ; ++j) fq[j] = fragment<T, QC, BQ>(now + BP * kRowBytes, wq + j * 16, h, lane);
+#pragma unroll
+            for (int j = 0; j < FQ; ++j)
+#pragma unroll
+                for (int i = 0; i < FP; ++i) acc[i][j] = mma(fp[i], fq[j], acc[i][j]);
+        }
+        if (more) {
+            sp.keep(next);
+            sq.keep(next + BP * kRowBytes);
+        }
+        unsigned char *t = now;
+        now = next;
+        next = t;
+    }
+    store_tile<T, FP, FQ, BP / WP, BQ / WQ>(a, e, acc, tiles, wave, lane, p0 + wp, q0 + wq);
+}
+
+// The same for whole, aligned operands of 2-byte types: memory goes to LDS directly (no registers on the way), STEPS steps of 64 bytes of
+// the contraction deep.  While step t's fragments are multiplied, those of step t + 1 are read and step t + STEPS is requested into
+// the buffer that step t has left, so that a step waits only for loads STEPS - 1 steps old.
+//
+// The compiler does not see these loads (they have no result); what they need is stated by hand: before a barrier each wave waits for its
+// own loads of step t + 1 (loads return in order: all but those of the steps after it) and for its own reads of step t, so
+// that beyond the barrier every wave's part of t + 1 is there and nobody reads step t's buffer any more.
+// Rows of 64 bytes, four to a line of the banks: their chunks are permuted so that the sixteen lanes that LDS serves together (0-3,
+// 12-15, 20-27 and so on) touch sixteen different ones.
+__device__ __forceinline__ int direct_chunk(int r, int ch) { return ch ^ ((r >> 1 & 2) ^ (r >> 3 & 1) * 3); }
+
+// Offsets from the tile's first element, in bytes, of what a lane requests with the i-th load of an operand's step.
+template <class T, bool ALONG_C, int ROWS> __device__ __forceinline__ uint32_t direct_offset(int piece, int lane, int64_t ld, int64_t rows_left)
+{
+    // a piece is 1024 bytes of the tile in LDS
+    if constexpr (ALONG_C) {
+        const int r = piece * 16 + (lane >> 2);
+        return (uint32_t)(min((int64_t)r, rows_left - 1) * ld * (int64_t)sizeof(T)) + (direct_chunk(r, lane & 3) << 4);
+    } else {
+        constexpr int kLine = ROWS / 8;   // 16-byte chunks of a line
+        const int c = (piece * 64 + lane) / kLine;
+        const int byte = line_place<T>(c, 0, lane % kLine * 16);
+        return (uint32_t)(c * ld * (int64_t)sizeof(T)) + (uint32_t)min((int64_t)byte, rows_left * (int64_t)sizeof(T) - 16);
+    }
+}
+
+// Sixteen bytes a lane from base + offset to LDS at `to` + 16 lane.
+__device__ __forceinline__ void request(const void *base, uint32_t offset, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory", "m0");
+}
+
+template <class T, bool ALONG_C, int ROWS> __device__ __forceinline__ Vec<T> direct_fragment(const unsigned char *tile, int r0, int lane)
+{
+    if constexpr (ALONG_C) {
+        const int r = r0 + (lane & 15);
+        return *(const Vec<T> *)(tile + r * 64 + (direct_chunk(r, lane >> 4) << 4));
+    } else {
+        return fragment<T, false, ROWS>(tile, r0, 0, lane);
+    }
+}
+
+// BP x BQ outputs per workgroup of WP x WQ waves.
+template <class T, bool PC, bool QC, int BP, int BQ, int WP, int WQ, int STEPS>
+__global__ __launch_bounds__(WP *WQ * 64, 2) void direct_kernel(Product<T> a, Epilogue<T> e)
+{
+    constexpr int BC = 32, WAVES = WP * WQ, FP = BP / WP / 16, FQ = BQ / WQ / 16;
+    constexpr int LP = BP / 16 / WAVES, LQ = BQ / 16 / WAVES, LOADS = LP + LQ;   // loads of a wave, per step
+    constexpr int kStep = (BP + BQ) * 64;
+    static_assert(LP * 16 * WAVES == BP && LQ * 16 * WAVES == BQ, "every wave requests as much");
+    extern __shared__ __align__(16) unsigned char tiles[];   // [STEPS][P, Q][rows of 64 bytes, or 32 lines]
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t tiles_p = (a.np + BP - 1) / BP;
+    const int64_t n = gridDim.x, xcd = blockIdx.x & 7, run = n / 8, left = n % 8;
+    const int64_t tile = xcd * run + min(xcd, left) + (blockIdx.x >> 3);
+    const int64_t p0 = tile % tiles_p * BP, q0 = tile / tiles_p * BQ;
+    const int64_t c_first = (int64_t)blockIdx.y * a.chunk, c_end = min(a.nc, c_first + a.chunk);
+    const int steps = (int)max((int64_t)0, (c_end - c_first) / BC);
+
+    const T *P = PC ? a.P + p0 * a.ldp + c_first : a.P + c_first * a.ldp + p0;
+    const T *Q = QC ? a.Q + q0 * a.ldq + c_first : a.Q + c_first * a.ldq + q0;
+    uint32_t off_p[LP], off_q[LQ];
+#pragma unroll
+    for (int i = 0; i < LP; ++i) off_p[i] = direct_offset<T, PC, BP>(wave * LP + i, lane, a.ldp, a.np - p0);
+#pragma unroll
+    for (int i = 0; i < LQ; ++i) off_q[i] = direct_offset<T, QC, BQ>(wave * LQ + i, lane, a.ldq, a.nq - q0);
+    const int64_t step_p = PC ? BC : BC * a.ldp, step_q = QC ? BC : BC * a.ldq;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)tiles;
+    const uint32_t lds_p = lds0 + wave * (LP * 1024), lds_q = lds0 + BP * 64 + wave * (LQ * 1024);
+    auto buffer_of = [](int t) { return (STEPS & (STEPS - 1)) == 0 ? t & (STEPS - 1) : t % STEPS; };
+    auto request_step = [&](int t) {
+        const uint32_t at = buffer_of(t) * kStep;
+        const T *p = P + t * step_p, *q = Q + t * step_q;
+#pragma unroll
+        for (int i = 0; i < LP; ++i) request(p, off_p[i], lds_p + at + i * 1024);
+#pragma unroll
+        for (int i = 0; i < LQ; ++i) request(q, off_q[i], lds_q + at + i * 1024);
+    };
+    const int wp = wave % WP * (FP * 16), wq = wave / WP * (FQ * 16);
+    float4v acc[FP][FQ] = {};
+    Vec<T> fp[2][FP], fq[2][FQ];
+    auto read_step = [&](int t, Vec<T> (&p)[FP], Vec<T> (&q)[FQ]) {
+        const unsigned char *at = tiles + buffer_of(t) * kStep;
+#pragma unroll
+        for (int j = 0; j < FQ; ++j) q[j] = direct_fragment<T, QC, BQ>(at + BP * 64, wq + j * 16, lane);
+#pragma unroll
+        for (int i = 0; i < FP; ++i) p[i] = direct_fragment<T, PC, BP>(at, wp + i * 16, lane);
+    };
+    auto multiply = [&](const Vec<T> (&p)[FP], const Vec<T> (&q)[FQ]) {
+#pragma unroll
+        for (int i = 0; i < FP; ++i)
+#pragma unroll
+            for (int j = 0; j < FQ; ++j) acc[i][j] = mma(p[i], q[j], acc[i][j]);
+    };
+    if (steps > 0) {
+        for (int t = 0; t < min(steps, STEPS); ++t) request_step(t);
+        if (steps >= STEPS) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STEPS - 1) * LOADS) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        asm volatile("s_barrier" ::: "memory");
+        read_step(0, fp[0], fq[0]);
+    }
+    // MORE: step t + STEPS exists
+    auto one_step = [&](auto more, int t, int set) {
+        __builtin_amdgcn_sched_barrier(0);
+        if (more.value || t + STEPS - 1 < steps) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((STEPS - 2) * LOADS) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        if (more.value || t + STEPS < steps) request_step(t + STEPS);
+        read_step(t + 1, fp[set ^ 1], fq[set ^ 1]);   // (beyond the last step: a buffer's old contents, not used)
+        multiply(fp[set], fq[set]);
+        constexpr int kReads = FP * (PC ? 1 : 2) + FQ * (QC ? 1 : 2);
+#pragma unroll
+        for (int i = 0; i < kReads; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);   // one LDS read
+            __builtin_amdgcn_sched_group_barrier(0x008, FP * FQ / kReads, 0);   // ... between the matrix instructions
+        }
+    };
+    int t = 0;
+    for (; t + 1 + STEPS < steps; t += 2) {
+        one_step(std::true_type(), t, 0);
+        one_step(std::true_type(), t + 1, 1);
+    }
+    for (; t + 1 < steps; t += 2) {
+        one_step(std::false_type(), t, 0);
+        one_step(std::false_type(), t + 1, 1);
+    }
+    if (t < steps) multiply(fp[0], fq[0]);
+    if (c_first + (int64_t)steps * BC < c_end) {   // what is left of the contraction, through registers, with zeros beyond it
+        const int64_t c0 = c_first + (int64_t)steps * BC;
+        __syncthreads();
+        auto keep_part = [&](auto along_c, auto rows_of, const T *src, int64_t ld, int64_t r0, int64_t rows, unsigned char *to) {
+            constexpr int ROWS = rows_of.value, kLine = ROWS / 8;
+            for (int id = threadIdx.x; id < ROWS * 4; id += WAVES * 64) {
+                if constexpr (along_c.value) {
+                    const int r = id >> 2, ch = id & 3;
+                    const int64_t c = c0 + ch * 8;
+                    *(Vec<T> *)(to + r * 64 + (direct_chunk(r, ch) << 4)) =
+                        load_part(src + (r0 + r) * ld + c, r0 + r < rows ? (int)min((int64_t)8, max((int64_t)0, c_end - c)) : 0, (T)0.f);
+                } else {
+                    const int64_t c = c0 + id / kLine, r = r0 + id % kLine * 8;
+                    *(Vec<T> *)(to + line_place<T>(id / kLine, ROWS * 2, id % kLine * 16)) =
+                        load_part(src + c * ld + r, c < c_end ? (int)min((int64_t)8, max((int64_t)0, rows - r)) : 0, (T)0.f);
+                }
+            }
+        };
+        keep_part(std::integral_constant<bool, PC>(), std::integral_constant<int, BP>(), a.P, a.ldp, p0, a.np, tiles);
+        keep_part(std::integral_constant<bool, QC>(), std::integral_constant<int, BQ>(), a.Q, a.ldq, q0, a.nq, tiles + BP * 64);
+        __syncthreads();
+        read_step(0, fp[0], fq[0]);
+        multiply(fp[0], fq[0]);
+    }
+    store_tile<T, FP, FQ, FP * 16, FQ * 16>(a, e, acc, tiles, wave, lane, p0 + wp, q0 + wq);
 }
 
 // The splits' sums, in order, and the epilogue.
@@ -181,21 +616,21 @@ __global__ __launch_bounds__(256) void product_join_kernel(int64_t np, int64_t n
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < quads * nq; i += (int64_t)gridDim.x * 256) {
         const int64_t q = i / quads, p = (i - q * quads) * 4;
         const int n = (int)min((int64_t)4, np - p);
-        float4v a = {0.f, 0.f, 0.f, 0.f};
+        float a[4] = {}, u[4];
         for (int s = 0; s < splits; ++s) {
-            const float *from = part + ((int64_t)s * nq + q) * np + p;
-            if (n == 4) a += load_vec<float4v>(from);
-            else for (int u = 0; u < n; ++u) a[u] += from[u];
+            load_row(part + ((int64_t)s * nq + q) * np + p, n, u);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) a[j] += u[j];
         }
-        finish4(e, q, p, n, a);
+        finish(e, q, p, n, a);
     }
 }
 
 // dz = dy act'(z), and column sums of it: blockIdx.x has 64 vectors of columns, blockIdx.y every gridDim.y-th group of four rows;
 // one partial row each.
-template <class T>
+template <class T, int ACT>
 __global__ __launch_bounds__(256) void slope_kernel(int64_t m, int64_t n, const T *__restrict__ dy, int64_t lddy, const T *__restrict__ z,
-                                                    int64_t ldz, int act, T *__restrict__ dz, float *__restrict__ part)
+                                                    int64_t ldz, T *__restrict__ dz, float *__restrict__ part)
 {
     constexpr int V = kVec<T>;
     __shared__ float comb[3][V][64];
@@ -207,10 +642,10 @@ __global__ __launch_bounds__(256) void slope_kernel(int64_t m, int64_t n, const 
         for (int64_t row = (int64_t)blockIdx.y * 4 + sub; row < m; row += (int64_t)gridDim.y * 4) {
             const Vec<T> g = load_part(dy + row * lddy + c, cols, (T)0.f);
             Vec<T> u, o;
-            if (act != VF_ACT_NONE) u = load_part(z + row * ldz + c, cols, (T)0.f);
+            if (ACT != VF_ACT_NONE) u = load_part(z + row * ldz + c, cols, (T)0.f);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const float d = act == VF_ACT_NONE ? (float)g[j] : (float)g[j] * act_slope((float)u[j], act);
+                const float d = ACT == VF_ACT_NONE ? (float)g[j] : (float)g[j] * act_slope<ACT>((float)u[j]);
                 sum[j] += d;
                 o[j] = (T)d;
             }
@@ -232,36 +667,136 @@ __global__ __launch_bounds__(256) void slope_kernel(int64_t m, int64_t n, const 
 
 // ---------------------------------------------------------------- host side
 
-struct ProductPlan {
-    int splits = 1;
-    int64_t chunk = 0;
-    size_t bytes = 0;
+// The kernels of a product, by the tile that a workgroup computes.
+enum Tiling {
+    kFewRows,       // 16 rows of P, all rows of Q (at most 64); both operands along c
+    kSmall,         // 64 x 64, any operands
+    kMedium,        // 128 x 128, any operands
+    kDirect128,     // 128 x 128, aligned operands of 2 bytes, straight to LDS
+    kDirectWide,    // 128 x 256, the same, two workgroups per compute unit; both operands along c
+    kDirect256,     // 256 x 256, the same
 };
 
-// The contraction is split where there are too few tiles for the chip and it is long enough for that.
-static ProductPlan plan_product(int32_t dtype, int64_t np, int64_t nq, int64_t nc)
+// What a tiling costs, in microseconds, as measured on 10,000 x 4,096 x 1,024 in its three products and on parts of it: `step` per 128
+// bytes of the contraction with a compute unit full of `together` workgroups, at least `alone` however few there are; `fixed` per workgroup
+// for its first loads and its stores.
+struct TilingCost {
+    int bp, bq, together;
+    double step, alone, fixed;
+};
+static TilingCost cost_of(Tiling t, bool f32)
 {
-    ProductPlan p;
+    switch (t) {
+    case kSmall: return f32 ? TilingCost{64, 64, 6, 6.0, 1.0, 4} : TilingCost{64, 64, 6, 2.0, 0.55, 4};
+    case kMedium: return f32 ? TilingCost{128, 128, 2, 7.0, 3.6, 5} : TilingCost{128, 128, 2, 1.4, 0.8, 5};
+    case kDirect128: return TilingCost{128, 128, 3, 1.45, 0.6, 5};
+    case kDirectWide: return TilingCost{128, 256, 2, 1.4, 0.9, 5};
+    default: return TilingCost{256, 256, 1, 1.45, 1.45, 8};
+    }
+}
+
+struct ProductPlan {
+    Tiling tiling = kSmall;
+    int splits = 1;
+    int64_t chunk = 0;    // elements of the contraction per split
+    size_t bytes = 0;     // of workspace
+};
+
+// What the choice of a kernel depends on beside the sizes.
+struct Operands {
+    bool p_along, q_along;   // contiguous along the contraction
+    bool direct;             // 2-byte types; rows start on 16 bytes, and an operand contiguous along its rows has whole vectors of them
+};
+
+// The tiling and the number of splits of the contraction that should take least time.  A split costs its partial sums' way
+// through memory and one more launch; it pays where there are too few tiles for the chip's 256 compute units.
+static ProductPlan plan_product(int32_t dtype, int64_t np, int64_t nq, int64_t nc, const Operands &o)
+{
+    ProductPlan best;
+    const bool f32 = dtype == VF_F32;
     const int64_t step = kRowBytes / (int64_t)type_size(dtype);
-    const int64_t tiles = ceil_div(np, kTile) * ceil_div(nq, kTile);
-    const int64_t most = std::max<int64_t>(1, nc / (4 * step));
-    const int64_t splits = tiles >= 256 ? 1 : std::min<int64_t>({ceil_div(512, std::max<int64_t>(1, tiles)), most, 64});
-    p.chunk = std::max<int64_t>(step, ceil_div(ceil_div(nc, splits), step) * step);
-    p.splits = (int)std::max<int64_t>(1, ceil_div(nc, p.chunk));
-    p.bytes = p.splits > 1 ? (size_t)p.splits * nq * np * 4 : 0;
-    return p;
+    if (o.p_along && o.q_along && nq <= 64) {
+        best.tiling = kFewRows;
+        best.chunk = nc;
+        return best;
+    }
+    double least = 0;
+    for (Tiling t : {kSmall, kMedium, kDirect128, kDirectWide, kDirect256}) {
+        if (t >= kDirect128 && !o.direct) continue;
+        if (t == kDirectWide && !(o.p_along && o.q_along)) continue;
+        const TilingCost c = cost_of(t, f32);
+        const int64_t tiles = ceil_div(np, c.bp) * ceil_div(nq, c.bq);
+        for (int64_t splits = 1; splits <= 64; splits = splits < 4 ? splits + 1 : splits * 2) {
+            const int64_t chunk = std::max<int64_t>(step, ceil_div(ceil_div(nc, splits), step) * step);
+            const int64_t used = std::max<int64_t>(1, ceil_div(nc, chunk));
+            if (splits > 1 && (used != splits || chunk < 4 * step || tiles * splits > 1024)) break;
+            const int64_t per_cu = ceil_div(tiles * used, 256), rounds = ceil_div(per_cu, c.together);
+            const double steps = (double)ceil_div(chunk, step);
+            const double last = (double)(per_cu - (rounds - 1) * c.together) / c.together;   // how full the last round is
+            double us = (double)(rounds - 1) * (steps * c.step + c.fixed) + steps * std::max(c.alone, c.step * last) + c.fixed;
+            if (used > 1) us += 4 + (double)used * np * nq * 8 / 4e6;
+            if (least == 0 || us < least) {
+                least = us;
+                best.tiling = t;
+                best.splits = (int)used;
+                best.chunk = chunk;
+                best.bytes = used > 1 ? (size_t)used * nq * np * 4 : 0;
+            }
+        }
+    }
+    return best;
+}
+
+template <class K> static int allow_lds(K kernel, size_t bytes)
+{
+    if (bytes > 64 * 1024) VF_HIP(hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    return VF_OK;
+}
+
+template <class T, bool PC, bool QC, int BP, int BQ, int WP, int WQ, int STEPS>
+static int launch_direct(const Product<T> &a, const Epilogue<T> &e, dim3 grid, hipStream_t s)
+{
+    constexpr size_t lds = (size_t)STEPS * (BP + BQ) * 64;
+    if (int rc = allow_lds(direct_kernel<T, PC, QC, BP, BQ, WP, WQ, STEPS>, lds); rc != VF_OK) return rc;
+    direct_kernel<T, PC, QC, BP, BQ, WP, WQ, STEPS><<<grid, dim3(WP * WQ * 64), lds, s>>>(a, e);
+    return VF_OK;
 }
 
 template <class T, bool PC, bool QC>
 static int run_product(int32_t dtype, const T *P, int64_t ldp, int64_t np, const T *Q, int64_t ldq, int64_t nq, int64_t nc,
-                       const Epilogue<T> &e, float *part, hipStream_t s)
+                       const Epilogue<T> &e, const ProductPlan &plan, float *part, hipStream_t s)
 {
     if (np == 0 || nq == 0) return VF_OK;
-    const ProductPlan plan = plan_product(dtype, np, nq, nc);
-    const int64_t tiles = ceil_div(np, kTile) * ceil_div(nq, kTile);
-    VF_REQUIRE(tiles < (1 << 24), "linear: too many output tiles in one call");
     const Product<T> a{P, Q, ldp, ldq, np, nq, nc, plan.chunk, plan.splits, part};
-    product_kernel<T, PC, QC><<<dim3((unsigned)tiles, (unsigned)plan.splits), dim3(256), 0, s>>>(a, e);
+    if (plan.tiling == kFewRows) {
+        if constexpr (PC && QC) {
+            // four fragments of the contraction and more for each wave
+            const int waves = (int)std::max<int64_t>(1, std::min<int64_t>(16, nc / (4 * 4 * kVec<T>)));
+            const dim3 grid((unsigned)ceil_div(np, 16)), block(waves * 64);
+            if (nq <= 16) few_rows_kernel<T, 1><<<grid, block, 0, s>>>(a, e);
+            else if (nq <= 32) few_rows_kernel<T, 2><<<grid, block, 0, s>>>(a, e);
+            else few_rows_kernel<T, 4><<<grid, block, 0, s>>>(a, e);
+        }
+        VF_HIP(hipGetLastError());
+        return VF_OK;
+    }
+    const TilingCost c = cost_of(plan.tiling, dtype == VF_F32);
+    const int64_t tiles = ceil_div(np, c.bp) * ceil_div(nq, c.bq);
+    VF_REQUIRE(tiles < (1 << 22), "linear: too many output tiles in one call");   // (a launch holds fewer than 2^32 threads)
+    const dim3 grid((unsigned)tiles, (unsigned)plan.splits);
+    int rc = VF_OK;
+    if (plan.tiling == kSmall) {
+        product_kernel<T, PC, QC><<<grid, dim3(256), 0, s>>>(a, e);
+    } else if (plan.tiling == kMedium) {
+        constexpr size_t lds = (size_t)2 * 256 * kRowBytes;
+        if ((rc = allow_lds(tile_kernel<T, PC, QC, 128, 128, 2, 4>, lds)) != VF_OK) return rc;
+        tile_kernel<T, PC, QC, 128, 128, 2, 4><<<grid, dim3(512), lds, s>>>(a, e);
+    } else if constexpr (sizeof(T) == 2) {
+        if (plan.tiling == kDirect256) rc = launch_direct<T, PC, QC, 256, 256, 2, 4, 4>(a, e, grid, s);
+        else if (plan.tiling == kDirect128) rc = launch_direct<T, PC, QC, 128, 128, 2, 2, 3>(a, e, grid, s);
+        else if constexpr (PC && QC) rc = launch_direct<T, PC, QC, 128, 256, 2, 2, 3>(a, e, grid, s);
+    }
+    if (rc != VF_OK) return rc;
     if (plan.splits > 1)
         product_join_kernel<T><<<dim3((unsigned)std::min<int64_t>(ceil_div(ceil_div(np, 4) * nq, 256), 4096)), dim3(256), 0, s>>>(
             np, nq, plan.splits, part, e);
@@ -270,6 +805,19 @@ static int run_product(int32_t dtype, const T *P, int64_t ldp, int64_t np, const
 }
 
 static size_t rounded(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
+
+// Whether rows of an operand that lie `ld` elements apart can go to LDS directly: the kernel's offsets within a tile have 32 bits.
+static bool direct_rows(int32_t dtype, const void *p, int64_t ld)
+{
+    return dtype != VF_F32 && ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && ld < (1 << 22);
+}
+
+// Workspace of a product whose operands' alignment is not known yet.
+static size_t most_bytes(int32_t dtype, int64_t np, int64_t nq, int64_t nc, bool p_along, bool q_along)
+{
+    return std::max(plan_product(dtype, np, nq, nc, {p_along, q_along, false}).bytes,
+                    dtype == VF_F32 ? 0 : plan_product(dtype, np, nq, nc, {p_along, q_along, true}).bytes);
+}
 
 // What the backward pass takes of its workspace: dz, the partial column sums, the splits of a product (one at a time).
 struct BackwardPlan {
@@ -284,7 +832,7 @@ static BackwardPlan plan_backward(int32_t dtype, int64_t m, int64_t n, int64_t k
     b.row_parts = std::max<int64_t>(1, std::min<int64_t>(ceil_div(m, 4), 1024 / std::max<int64_t>(1, std::min<int64_t>(across, 1024))));
     b.dz = act == VF_ACT_NONE ? 0 : (size_t)m * n * type_size(dtype);
     b.parts = (size_t)b.row_parts * n * 4;
-    b.product = std::max(plan_product(dtype, k, m, n).bytes, plan_product(dtype, k, n, m).bytes);
+    b.product = std::max(most_bytes(dtype, k, m, n, false, true), most_bytes(dtype, k, n, m, false, false));
     return b;
 }
 
@@ -300,26 +848,26 @@ int linear_workspace_impl(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_
 {
     VF_REQUIRE(bytes != nullptr, "linear: bytes is NULL");
     if (int rc = check_sizes(dtype, m, n, k, act); rc != VF_OK) return rc;
-    *bytes = backward ? plan_backward(dtype, m, n, k, act).total() : plan_product(dtype, n, m, k).bytes;
+    *bytes = backward ? plan_backward(dtype, m, n, k, act).total() : most_bytes(dtype, n, m, k, true, true);
     return VF_OK;
 }
 
 int linear_impl(const LinearArgs &a)
 {
-    size_t need = 0;
-    if (int rc = linear_workspace_impl(a.dtype, a.m, a.n, a.k, a.act, 0, &need); rc != VF_OK) return rc;
+    if (int rc = check_sizes(a.dtype, a.m, a.n, a.k, a.act); rc != VF_OK) return rc;
     if (a.m == 0 || a.n == 0) return VF_OK;
     VF_REQUIRE((a.x && a.w) || a.k == 0, "linear: x or w is NULL");
     VF_REQUIRE(a.y != nullptr, "linear: y is NULL");
     VF_REQUIRE(a.ldx >= a.k && a.ldw >= a.k, "linear: ldx or ldw is less than k");
     VF_REQUIRE(a.ldy >= a.n && (!a.z || a.ldz >= a.n) && (!a.residual || a.ldr >= a.n), "linear: ldy, ldz or ldr is less than n");
-    VF_REQUIRE(need == 0 || (a.workspace != nullptr && a.workspace_bytes >= need),
-               "linear: the workspace must hold " + std::to_string(need) + " bytes");
+    const ProductPlan plan = plan_product(a.dtype, a.n, a.m, a.k, {true, true, direct_rows(a.dtype, a.x, a.ldx) && direct_rows(a.dtype, a.w, a.ldw)});
+    VF_REQUIRE(plan.bytes == 0 || (a.workspace != nullptr && a.workspace_bytes >= plan.bytes),
+               "linear: the workspace must hold " + std::to_string(plan.bytes) + " bytes");
     int rc = VF_OK;
     by_type(a.dtype, [&](auto *t) {
         using T = std::remove_pointer_t<decltype(t)>;
         const Epilogue<T> e{(const T *)a.bias, a.act, (const T *)a.residual, a.ldr, (T *)a.y, a.ldy, (T *)a.z, a.ldz};
-        rc = run_product<T, true, true>(a.dtype, (const T *)a.w, a.ldw, a.n, (const T *)a.x, a.ldx, a.m, a.k, e, (float *)a.workspace,
+        rc = run_product<T, true, true>(a.dtype, (const T *)a.w, a.ldw, a.n, (const T *)a.x, a.ldx, a.m, a.k, e, plan, (float *)a.workspace,
                                         a.stream);
     });
     return rc;
@@ -348,19 +896,25 @@ int linear_backward_impl(const LinearArgs &a)
         const bool products = (a.dx || a.dw) && a.k > 0;
         if (rows && (a.dbias || (a.act != VF_ACT_NONE && products))) {
             const int64_t across = ceil_div(a.n, 64 * kVec<T>);
-            slope_kernel<T><<<dim3((unsigned)across, (unsigned)b.row_parts), dim3(256), 0, a.stream>>>(
-                a.m, a.n, (const T *)a.dy, a.lddy, (const T *)a.z, a.ldz, a.act, a.act != VF_ACT_NONE && products ? made : nullptr,
-                a.dbias ? parts : nullptr);
+            by_act(a.act, [&](auto act) {
+                slope_kernel<T, act.value><<<dim3((unsigned)across, (unsigned)b.row_parts), dim3(256), 0, a.stream>>>(
+                    a.m, a.n, (const T *)a.dy, a.lddy, (const T *)a.z, a.ldz, a.act != VF_ACT_NONE && products ? made : nullptr,
+                    a.dbias ? parts : nullptr);
+            });
         }
         if (a.dbias && a.n > 0)
             launch_join_parts<T>(rows ? (int)b.row_parts : 0, a.n, 1, parts, (T *)a.dbias, nullptr, a.stream);
         if (a.dx) {
             const Epilogue<T> e{nullptr, VF_ACT_NONE, nullptr, 0, (T *)a.dx, a.lddx, nullptr, 0};
-            rc = run_product<T, false, true>(a.dtype, (const T *)a.w, a.ldw, a.k, dz, lddz, a.m, a.n, e, splits, a.stream);
+            const bool direct = a.k % 8 == 0 && direct_rows(a.dtype, a.w, a.ldw) && direct_rows(a.dtype, dz, lddz);
+            rc = run_product<T, false, true>(a.dtype, (const T *)a.w, a.ldw, a.k, dz, lddz, a.m, a.n, e,
+                                             plan_product(a.dtype, a.k, a.m, a.n, {false, true, direct}), splits, a.stream);
         }
         if (a.dw && rc == VF_OK) {
             const Epilogue<T> e{nullptr, VF_ACT_NONE, nullptr, 0, (T *)a.dw, a.lddw, nullptr, 0};
-            rc = run_product<T, false, false>(a.dtype, (const T *)a.x, a.ldx, a.k, dz, lddz, a.n, a.m, e, splits, a.stream);
+            const bool direct = a.k % 8 == 0 && a.n % 8 == 0 && direct_rows(a.dtype, a.x, a.ldx) && direct_rows(a.dtype, dz, lddz);
+            rc = run_product<T, false, false>(a.dtype, (const T *)a.x, a.ldx, a.k, dz, lddz, a.n, a.m, e,
+                                              plan_product(a.dtype, a.k, a.n, a.m, {false, false, direct}), splits, a.stream);
         }
     });
     if (rc == VF_OK) VF_HIP(hipGetLastError());
