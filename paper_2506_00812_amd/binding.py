@@ -510,70 +510,65 @@ ACTIVATIONS = dict(none=0, relu=1, gelu=2, silu=3)
 ADAMW_BLOCK = 256
 LOG_PROBS_MAX_TOP = 64
 
-_FLOAT_CODES = None       # torch dtype -> VF_*; filled on first use (torch is imported lazily here)
+# Filled on first use (torch is imported lazily here): torch, the codes of its float types, the current stream's handle.
+_torch = _codes = _raw_stream = None
 
 
-def _float_code(t, what):
-    global _FLOAT_CODES
-    if _FLOAT_CODES is None:
-        import torch
-        _FLOAT_CODES = {torch.float32: VF_F32, torch.bfloat16: VF_BF16, torch.float16: VF_F16}
-    code = _FLOAT_CODES.get(t.dtype)
+def _use_torch():
+    global _torch, _codes, _raw_stream
+    import torch
+    _codes = {torch.float32: VF_F32, torch.bfloat16: VF_BF16, torch.float16: VF_F16}
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)     # (a Stream object costs more than a small kernel's launch)
+    _raw_stream = raw or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+    _torch = torch
+
+
+def _first(t, what, stream):
+    """(type code, dtype, device, stream handle) of a call, from its first tensor, which must be on the current device."""
+    if _torch is None:
+        _use_torch()
+    T = t.dtype
+    code = _codes.get(T)
     if code is None:
-        raise VecflowError(f"{what}: unsupported dtype {t.dtype}")
-    return code
+        raise VecflowError(f"{what}: unsupported dtype {T}")
+    dev = t.get_device()
+    if dev < 0 or dev != _torch.cuda.current_device():
+        raise VecflowError(f"{what} must be a CUDA tensor on the current device")
+    return code, T, dev, _raw_stream(dev) if stream is None else stream.cuda_stream
 
 
-def _matrix(t, what, dtype, rows=None, cols=None):
-    """Distance of two rows of a matrix argument, which must have the dtype and sizes given."""
-    if not t.is_cuda or t.dim() != 2 or t.dtype != dtype:
-        raise VecflowError(f"{what} must be a 2-D CUDA tensor of {dtype}")
+def _matrix(t, what, T, dev, rows=None, cols=None):
+    """Distance of two rows of a matrix argument, which must have the dtype, device and sizes given."""
+    if t.dtype != T or t.get_device() != dev or t.dim() != 2:
+        raise VecflowError(f"{what} must be a 2-D CUDA tensor of {T} on the same device")
     n, d = t.shape
     if (rows is not None and n != rows) or (cols is not None and d != cols):
         raise VecflowError(f"{what} must have shape [{n if rows is None else rows}, {d if cols is None else cols}], not {list(t.shape)}")
-    if d > 1 and t.stride(1) != 1:
+    ld, step = t.stride()
+    if step != 1 and d > 1:
         raise VecflowError(f"{what} must have neighbouring columns (stride(1) == 1)")
     if n <= 1:
         return d
-    ld = t.stride(0)
     if ld < d:
         raise VecflowError(f"{what} must not have overlapping rows")
     return ld
 
 
-def _vector(t, what, dtype, n):
+def _vector(t, what, T, dev, n):
     """Address of a vector argument; None stays None."""
     if t is None:
         return None
-    if not t.is_cuda or t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
-        raise VecflowError(f"{what} must be a contiguous CUDA tensor [{n}] of {dtype}")
+    if t.dtype != T or t.get_device() != dev or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise VecflowError(f"{what} must be a contiguous CUDA tensor [{n}] of {T} on the same device")
     return t.data_ptr()
 
 
-class _on:
-    """The stream of a call: allocations are made on it, so that memory returns to the pool in its order."""
-
-    def __init__(self, stream, like):
-        import torch
-        self.torch = torch
-        self.device = like.device
-        if like.device.index != torch.cuda.current_device():
-            raise VecflowError("tensors must be on the current device")
-        self.stream = stream
-        self.handle = (torch.cuda.current_stream() if stream is None else stream).cuda_stream
-
-    def empty(self, shape, dtype):
-        if self.stream is None:
-            return self.torch.empty(shape, dtype=dtype, device=self.device)
-        with self.torch.cuda.stream(self.stream):
-            return self.torch.empty(shape, dtype=dtype, device=self.device)
-
-    def workspace(self, nbytes):
-        """(tensor, address, bytes)"""
-        if nbytes == 0:
-            return None, None, 0
-        t = self.empty((nbytes,), self.torch.uint8)
-        return t, t.data_ptr(), nbytes
+def _empty(like, shape, T, stream):
+    """Memory on the call's stream, so that it returns to the pool in that stream's order."""
+    if stream is None:
+        return like.new_empty(shape, dtype=T)
+    with _torch.cuda.stream(stream):
+        return like.new_empty(shape, dtype=T)
 
 
 def _size_of(fn, *args):
@@ -582,32 +577,43 @@ def _size_of(fn, *args):
     return n.value
 
 
+def _workspace(like, nbytes, stream):
+    """(tensor, address): the tensor has to live until the call has been made, its memory is then the stream's to reuse."""
+    if nbytes == 0:
+        return None, None
+    t = _empty(like, (nbytes,), _torch.uint8, stream)
+    return t, t.data_ptr()
+
+
 def _activation(name):
-    if name not in ACTIVATIONS:
+    act = ACTIVATIONS.get(name)
+    if act is None:
         raise VecflowError(f"unknown activation {name!r}: one of {sorted(ACTIVATIONS)}")
-    return ACTIVATIONS[name]
+    return act
 
 
 def linear(x, weight, bias=None, residual=None, activation="none", save=False, out=None, stream=None):
     """act(x weight^T + bias) + residual for x [m, k], weight [n, k] (vf_linear).  save=True: (y, z) with the
     pre-activation z that linear_backward reads.  `out` may be the residual's own memory."""
     L = load_library()
-    code, T, act = _float_code(x, "x"), x.dtype, _activation(activation)
-    ldx = _matrix(x, "x", T)
+    code, T, dev, handle = _first(x, "x", stream)
+    act = _activation(activation)
+    ldx = _matrix(x, "x", T, dev)
     m, k = x.shape
-    ldw = _matrix(weight, "weight", T, None, k)
+    ldw = _matrix(weight, "weight", T, dev, None, k)
     n = weight.shape[0]
-    pb = _vector(bias, "bias", T, n)
-    on = _on(stream, x)
-    ldr = 0 if residual is None else _matrix(residual, "residual", T, m, n)
+    pb = _vector(bias, "bias", T, dev, n)
+    ldr = 0 if residual is None else _matrix(residual, "residual", T, dev, m, n)
     if out is None:
-        out = on.empty((m, n), T)
-    ldy = _matrix(out, "out", T, m, n)
-    z = on.empty((m, n), T) if save else None
-    _ws, pw, nw = on.workspace(_size_of(L.vf_linear_workspace, code, m, n, k, act, 0))
+        out, ldy = _empty(x, (m, n), T, stream), n
+    else:
+        ldy = _matrix(out, "out", T, dev, m, n)
+    z = _empty(x, (m, n), T, stream) if save else None
+    nw = _size_of(L.vf_linear_workspace, code, m, n, k, act, 0)
+    _ws, pw = _workspace(x, nw, stream)
     _check(L.vf_linear(code, m, n, k, x.data_ptr(), ldx, weight.data_ptr(), ldw, pb, act,
                        None if residual is None else residual.data_ptr(), ldr, out.data_ptr(), ldy,
-                       z.data_ptr() if save else None, n, pw, nw, on.handle))
+                       z.data_ptr() if save else None, n, pw, nw, handle))
     return (out, z) if save else out
 
 
@@ -615,23 +621,24 @@ def linear_backward(dy, x, weight, z=None, activation="none", bias=True, dx=True
     """Gradients (dx, dweight, dbias) of linear from dy [m, n] (vf_linear_backward); the residual's gradient is dy itself.
     What is not asked for is None.  z: the pre-activation, needed for any activation but "none"."""
     L = load_library()
-    code, T, act = _float_code(dy, "dy"), dy.dtype, _activation(activation)
-    lddy = _matrix(dy, "dy", T)
+    code, T, dev, handle = _first(dy, "dy", stream)
+    act = _activation(activation)
+    lddy = _matrix(dy, "dy", T, dev)
     m, n = dy.shape
-    ldx = _matrix(x, "x", T, m)
+    ldx = _matrix(x, "x", T, dev, m)
     k = x.shape[1]
-    ldw = _matrix(weight, "weight", T, n, k)
+    ldw = _matrix(weight, "weight", T, dev, n, k)
     if act and z is None:
         raise VecflowError(f"linear_backward needs z, the pre-activation, for activation {activation!r}")
-    ldz = _matrix(z, "z", T, m, n) if act else 0
-    on = _on(stream, dy)
-    gx = on.empty((m, k), T) if dx else None
-    gw = on.empty((n, k), T) if dweight else None
-    gb = on.empty((n,), T) if bias else None
-    _ws, pw, nw = on.workspace(_size_of(L.vf_linear_workspace, code, m, n, k, act, 1))
+    ldz = _matrix(z, "z", T, dev, m, n) if act else 0
+    gx = _empty(dy, (m, k), T, stream) if dx else None
+    gw = _empty(dy, (n, k), T, stream) if dweight else None
+    gb = _empty(dy, (n,), T, stream) if bias else None
+    nw = _size_of(L.vf_linear_workspace, code, m, n, k, act, 1)
+    _ws, pw = _workspace(dy, nw, stream)
     _check(L.vf_linear_backward(code, m, n, k, dy.data_ptr(), lddy, x.data_ptr(), ldx, weight.data_ptr(), ldw,
                                 z.data_ptr() if act else None, ldz, act, gx.data_ptr() if dx else None, k,
-                                gw.data_ptr() if dweight else None, k, gb.data_ptr() if bias else None, pw, nw, on.handle))
+                                gw.data_ptr() if dweight else None, k, gb.data_ptr() if bias else None, pw, nw, handle))
     return gx, gw, gb
 
 
@@ -639,42 +646,43 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, save=False, out=None, stream
     """(x - mean) / sqrt(variance + eps) weight + bias per row of x [m, d] (vf_layer_norm).  save=True: (y, mean, rstd).
     `out` may be x's own memory."""
     L = load_library()
-    code, T = _float_code(x, "x"), x.dtype
-    ldx = _matrix(x, "x", T)
+    code, T, dev, handle = _first(x, "x", stream)
+    ldx = _matrix(x, "x", T, dev)
     m, d = x.shape
-    pg, pb = _vector(weight, "weight", T, d), _vector(bias, "bias", T, d)
-    on = _on(stream, x)
+    pg, pb = _vector(weight, "weight", T, dev, d), _vector(bias, "bias", T, dev, d)
     if out is None:
-        out = on.empty((m, d), T)
-    ldy = _matrix(out, "out", T, m, d)
-    stats = on.empty((2, m), on.torch.float32) if save else None
-    ps = stats.data_ptr() if save else None
-    _check(L.vf_layer_norm(code, m, d, x.data_ptr(), ldx, pg, pb, eps, out.data_ptr(), ldy, ps, ps + 4 * m if save else None,
-                           on.handle))
-    return (out, stats[0], stats[1]) if save else out
+        out, ldy = _empty(x, (m, d), T, stream), d
+    else:
+        ldy = _matrix(out, "out", T, dev, m, d)
+    if not save:
+        _check(L.vf_layer_norm(code, m, d, x.data_ptr(), ldx, pg, pb, eps, out.data_ptr(), ldy, None, None, handle))
+        return out
+    mean, rstd = _empty(x, (2, m), _torch.float32, stream).unbind(0)
+    _check(L.vf_layer_norm(code, m, d, x.data_ptr(), ldx, pg, pb, eps, out.data_ptr(), ldy, mean.data_ptr(), rstd.data_ptr(),
+                           handle))
+    return out, mean, rstd
 
 
 def layer_norm_backward(dy, x, mean, rstd, weight=None, dx=True, dweight=True, dbias=True, out=None, stream=None):
     """Gradients (dx, dweight, dbias) of layer_norm from dy [m, d] (vf_layer_norm_backward).  What is not asked for is
     None.  `out`: where dx goes, dy's own memory if need be."""
     L = load_library()
-    code, T = _float_code(dy, "dy"), dy.dtype
-    lddy = _matrix(dy, "dy", T)
+    code, T, dev, handle = _first(dy, "dy", stream)
+    lddy = _matrix(dy, "dy", T, dev)
     m, d = dy.shape
-    ldx = _matrix(x, "x", T, m, d)
-    on = _on(stream, dy)
-    pm, pr = _vector(mean, "mean", on.torch.float32, m), _vector(rstd, "rstd", on.torch.float32, m)
-    pg = _vector(weight, "weight", T, d)
+    ldx = _matrix(x, "x", T, dev, m, d)
+    pm, pr = _vector(mean, "mean", _torch.float32, dev, m), _vector(rstd, "rstd", _torch.float32, dev, m)
+    pg = _vector(weight, "weight", T, dev, d)
     if dx and out is None:
-        out = on.empty((m, d), T)
-    ldo = _matrix(out, "out", T, m, d) if dx else 0
-    gw = on.empty((d,), T) if dweight else None
-    gb = on.empty((d,), T) if dbias else None
-    sums = dweight or dbias
-    _ws, pw, nw = on.workspace(_size_of(L.vf_layer_norm_workspace, code, m, d) if sums else 0)
+        out = _empty(dy, (m, d), T, stream)
+    ldo = _matrix(out, "out", T, dev, m, d) if dx else 0
+    gw = _empty(dy, (d,), T, stream) if dweight else None
+    gb = _empty(dy, (d,), T, stream) if dbias else None
+    nw = _size_of(L.vf_layer_norm_workspace, code, m, d) if dweight or dbias else 0
+    _ws, pw = _workspace(dy, nw, stream)
     _check(L.vf_layer_norm_backward(code, m, d, dy.data_ptr(), lddy, x.data_ptr(), ldx, pm, pr, pg,
                                     out.data_ptr() if dx else None, ldo, gw.data_ptr() if dweight else None,
-                                    gb.data_ptr() if dbias else None, pw, nw, on.handle))
+                                    gb.data_ptr() if dbias else None, pw, nw, handle))
     return out if dx else None, gw, gb
 
 
@@ -683,23 +691,22 @@ def log_probs(logits, targets=None, top=0, stream=None):
     (logp, entropy, lse, top_ids, top_logp); float32 [m], int32 / float32 [m, top].  targets: int32 [m], -1 for none;
     logp is None without them."""
     L = load_library()
-    code = _float_code(logits, "logits")
-    ld = _matrix(logits, "logits", logits.dtype)
+    code, T, dev, handle = _first(logits, "logits", stream)
+    ld = _matrix(logits, "logits", T, dev)
     m, v = logits.shape
     top = int(top)
     if not 0 <= top <= LOG_PROBS_MAX_TOP:
         raise VecflowError(f"top must be 0 .. {LOG_PROBS_MAX_TOP}")
-    on = _on(stream, logits)
-    f32, i32 = on.torch.float32, on.torch.int32
-    pt = _vector(targets, "targets", i32, m)
-    sums = on.empty((3, m), f32)
-    ps = sums.data_ptr()
-    ids = on.empty((m, top), i32) if top else None
-    tlp = on.empty((m, top), f32) if top else None
-    _ws, pw, nw = on.workspace(_size_of(L.vf_log_probs_workspace, code, m, v, top))
-    _check(L.vf_log_probs(code, m, v, logits.data_ptr(), ld, pt, top, ps if pt is not None else None, ps + 4 * m, ps + 8 * m,
-                          ids.data_ptr() if top else None, tlp.data_ptr() if top else None, pw, nw, on.handle))
-    logp, entropy, lse = sums.unbind(0)
+    f32, i32 = _torch.float32, _torch.int32
+    pt = _vector(targets, "targets", i32, dev, m)
+    logp, entropy, lse = _empty(logits, (3, m), f32, stream).unbind(0)
+    ids = _empty(logits, (m, top), i32, stream) if top else None
+    tlp = _empty(logits, (m, top), f32, stream) if top else None
+    nw = _size_of(L.vf_log_probs_workspace, code, m, v, top)
+    _ws, pw = _workspace(logits, nw, stream)
+    _check(L.vf_log_probs(code, m, v, logits.data_ptr(), ld, pt, top, None if targets is None else logp.data_ptr(),
+                          entropy.data_ptr(), lse.data_ptr(), ids.data_ptr() if top else None,
+                          tlp.data_ptr() if top else None, pw, nw, handle))
     if targets is None:
         logp = None
     return (logp, entropy, lse, ids, tlp) if top else (logp, entropy, lse)
@@ -709,20 +716,20 @@ def log_probs_backward(logits, lse, targets=None, d_logp=None, entropy=None, d_e
     """Gradient with respect to the logits from those of logp and entropy (vf_log_probs_backward); `out` may be the
     logits' own memory."""
     L = load_library()
-    code, T = _float_code(logits, "logits"), logits.dtype
-    ld = _matrix(logits, "logits", T)
+    code, T, dev, handle = _first(logits, "logits", stream)
+    ld = _matrix(logits, "logits", T, dev)
     m, v = logits.shape
-    on = _on(stream, logits)
-    f32 = on.torch.float32
+    f32 = _torch.float32
     if (targets is None) != (d_logp is None) or (entropy is None) != (d_entropy is None):
         raise VecflowError("targets and d_logp go together, and entropy and d_entropy")
     if out is None:
-        out = on.empty((m, v), T)
-    ldd = _matrix(out, "out", T, m, v)
-    _check(L.vf_log_probs_backward(code, m, v, logits.data_ptr(), ld, _vector(lse, "lse", f32, m),
-                                   _vector(targets, "targets", on.torch.int32, m), _vector(d_logp, "d_logp", f32, m),
-                                   _vector(entropy, "entropy", f32, m), _vector(d_entropy, "d_entropy", f32, m),
-                                   out.data_ptr(), ldd, on.handle))
+        out, ldd = _empty(logits, (m, v), T, stream), v
+    else:
+        ldd = _matrix(out, "out", T, dev, m, v)
+    _check(L.vf_log_probs_backward(code, m, v, logits.data_ptr(), ld, _vector(lse, "lse", f32, dev, m),
+                                   _vector(targets, "targets", _torch.int32, dev, m), _vector(d_logp, "d_logp", f32, dev, m),
+                                   _vector(entropy, "entropy", f32, dev, m), _vector(d_entropy, "d_entropy", f32, dev, m),
+                                   out.data_ptr(), ldd, handle))
     return out
 
 
@@ -740,15 +747,16 @@ def adamw_state(param, bits=32):
             torch.zeros(blocks, dtype=torch.float32, device=param.device))
 
 
-def _flat(t, what, dtypes, n):
-    if not t.is_cuda or not t.is_contiguous() or t.dtype not in dtypes or t.numel() != n:
-        raise VecflowError(f"{what} must be a contiguous CUDA tensor of {n} elements of {' or '.join(map(str, dtypes))}")
+def _flat(t, what, kinds, dev, n):
+    if t.dtype not in kinds or t.get_device() != dev or t.numel() != n or not t.is_contiguous():
+        raise VecflowError(f"{what} must be a contiguous tensor of {n} elements of {' or '.join(map(str, kinds))} on the device of the others")
     return t.data_ptr()
 
 
 def _adamw_list(ms, vs, m_scales, v_scales):
-    """(array of VfAdamwTensor with the moments filled in, torch)"""
-    import torch
+    """(array of VfAdamwTensor with the moments filled in, device)"""
+    if _torch is None:
+        _use_torch()
     count = len(ms)
     for other in (vs, m_scales, v_scales):
         if other is not None and len(other) != count:
@@ -756,22 +764,23 @@ def _adamw_list(ms, vs, m_scales, v_scales):
     if (m_scales is None) != (v_scales is None):
         raise VecflowError("adamw: m_scales and v_scales go together")
     arr = (VfAdamwTensor * max(count, 1))()
-    for i in range(count):
-        n = ms[i].numel()
+    f32, dev = (_torch.float32,), _torch.cuda.current_device() if count else -1
+    for i, m in enumerate(ms):
+        n = m.numel()
         t = arr[i]
         t.n = n
-        if ms[i].dtype == torch.float32:
-            t.state_bits, kinds = 32, ((torch.float32,), (torch.float32,))
+        if m.dtype == _torch.float32:
+            t.state_bits = 32
+            t.m, t.v = _flat(m, f"ms[{i}]", f32, dev, n), _flat(vs[i], f"vs[{i}]", f32, dev, n)
         else:
-            t.state_bits, kinds = 8, ((torch.int8,), (torch.uint8,))
+            t.state_bits = 8
             if m_scales is None or m_scales[i] is None or v_scales[i] is None:
                 raise VecflowError(f"adamw: tensor {i}: moments in 8 bits need scales")
             blocks = -(-n // ADAMW_BLOCK)
-            t.m_scale = _flat(m_scales[i], f"m_scales[{i}]", (torch.float32,), blocks)
-            t.v_scale = _flat(v_scales[i], f"v_scales[{i}]", (torch.float32,), blocks)
-        t.m = _flat(ms[i], f"ms[{i}]", kinds[0], n)
-        t.v = _flat(vs[i], f"vs[{i}]", kinds[1], n)
-    return arr, torch
+            t.m, t.v = _flat(m, f"ms[{i}]", (_torch.int8,), dev, n), _flat(vs[i], f"vs[{i}]", (_torch.uint8,), dev, n)
+            t.m_scale = _flat(m_scales[i], f"m_scales[{i}]", f32, dev, blocks)
+            t.v_scale = _flat(v_scales[i], f"v_scales[{i}]", f32, dev, blocks)
+    return arr, dev
 
 
 def adamw_step(params, grads, ms, vs, step, lr, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, grad_scale=1.0, masters=None,
@@ -783,41 +792,41 @@ def adamw_step(params, grads, ms, vs, step, lr, betas=(0.9, 0.999), eps=1e-8, we
     count = len(params)
     if len(grads) != count or len(ms) != count or (masters is not None and len(masters) != count):
         raise VecflowError("adamw: the lists must have one entry per tensor")
-    arr, torch = _adamw_list(ms, vs, m_scales, v_scales)
     decay = weight_decay if isinstance(weight_decay, (list, tuple)) else [weight_decay] * count
     if len(decay) != count:
         raise VecflowError("adamw: weight_decay must be one number or one per tensor")
+    arr, dev = _adamw_list(ms, vs, m_scales, v_scales)
     if count == 0:
         return
-    floats = (torch.float32, torch.bfloat16, torch.float16)
-    for i in range(count):
-        t, n = arr[i], arr[i].n
-        t.param = _flat(params[i], f"params[{i}]", floats, n)
-        t.grad = _flat(grads[i], f"grads[{i}]", floats, n)
-        t.param_type, t.grad_type = _float_code(params[i], "params"), _float_code(grads[i], "grads")
+    for i, p in enumerate(params):
+        t, g = arr[i], grads[i]
+        n = t.n
+        t.param, t.grad = _flat(p, f"params[{i}]", _codes, dev, n), _flat(g, f"grads[{i}]", _codes, dev, n)
+        t.param_type, t.grad_type = _codes[p.dtype], _codes[g.dtype]
         if masters is not None and masters[i] is not None:
-            t.master = _flat(masters[i], f"masters[{i}]", (torch.float32,), n)
+            t.master = _flat(masters[i], f"masters[{i}]", (_torch.float32,), dev, n)
         t.weight_decay = decay[i]
     prm = VfAdamwParams(lr, betas[0], betas[1], eps, grad_scale, step)
-    on = _on(stream, params[0])
-    _check(load_library().vf_adamw_step(arr, count, C.byref(prm), _vector(skip, "skip", torch.int32, 1), on.handle))
+    handle = _raw_stream(dev) if stream is None else stream.cuda_stream
+    _check(load_library().vf_adamw_step(arr, count, C.byref(prm), _vector(skip, "skip", _torch.int32, dev, 1), handle))
 
 
 def adamw_moments(ms, vs, m_scales=None, v_scales=None, stream=None):
     """The moments as float32 tensors: lists (m, v) (vf_adamw_moments)."""
-    arr, torch = _adamw_list(ms, vs, m_scales, v_scales)
+    arr, dev = _adamw_list(ms, vs, m_scales, v_scales)
     count = len(ms)
     if count == 0:
         return [], []
-    on = _on(stream, ms[0])
-    total = [on.empty((sum(t.numel() for t in ms),), torch.float32) for _ in range(2)]
-    outs, ptrs = ([], []), ((C.c_void_p * count)(), (C.c_void_p * count)())
-    for which in (0, 1):
-        at, base = 0, total[which].data_ptr()
-        for i in range(count):
-            n = arr[i].n
-            outs[which].append(total[which][at:at + n])
-            ptrs[which][i] = base + 4 * at
-            at += n
-    _check(load_library().vf_adamw_moments(arr, count, ptrs[0], ptrs[1], on.handle))
-    return outs
+    sizes = [t.numel() for t in ms]
+    at = [0]
+    for n in sizes:
+        at.append(at[-1] + n)
+    outs, ptrs = [], []
+    for _ in range(2):
+        whole = _empty(ms[0], (at[-1],), _torch.float32, stream)
+        base = whole.data_ptr()
+        outs.append(list(whole.split(sizes)))
+        ptrs.append((C.c_void_p * count)(*[base + 4 * a for a in at[:-1]]))
+    handle = _raw_stream(dev) if stream is None else stream.cuda_stream
+    _check(load_library().vf_adamw_moments(arr, count, ptrs[0], ptrs[1], handle))
+    return outs[0], outs[1]

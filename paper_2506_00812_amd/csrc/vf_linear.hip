@@ -98,102 +98,7 @@ template <class T> struct Product {
     float *part;          // [splits][nq][np] where splits > 1
 };
 
-constexpr int kTile = 64;          // rows of either operand per workgroup
-constexpr int kRowBytes = 128;     // bytes of the contraction per step
-
-// 64 x 64 outputs per workgroup of four waves, 128 bytes of the contraction per step, staged through LDS by way of registers: any
-// alignment, any size.  An LDS row holds its eight 16-byte chunks at chunk ^ (row % 8), which spreads a fragment's reads
-// over the banks.
-template <class T, bool PC, bool QC>
-__global__ __launch_bounds__(256) void product_kernel(Product<T> a, Epilogue<T> e)
-{
-    constexpr int V = kVec<T>, BC = kRowBytes / (int)sizeof(T);
-    __shared__ __align__(16) unsigned char lds[2][kTile * kRowBytes];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t tiles_p = (a.np + kTile - 1) / kTile;
-    const int64_t tile = blockIdx.x, p0 = tile % tiles_p * kTile, q0 = tile / tiles_p * kTile;
-    const int64_t c_first = (int64_t)blockIdx.y * a.chunk, c_end = min(a.nc, c_first + a.chunk);
-
-    Vec<T> stage[2][2];   // [operand][vector]
-    auto load_operand = [&](auto along_c, const T *src, int64_t ld, int64_t r0, int64_t rows, int64_t c0, Vec<T> (&to)[2]) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int id = tid + i * 256;
-            if constexpr (along_c.value) {
-                const int64_t r = r0 + id / 8, c = c0 + id % 8 * V;
-                to[i] = load_part(src + r * ld + c, r < rows ? (int)min((int64_t)V, max((int64_t)0, c_end - c)) : 0, (T)0.f);
-            } else {
-                const int64_t c = c0 + id / (kTile / V), r = r0 + id % (kTile / V) * V;
-                to[i] = load_part(src + c * ld + r, c < c_end ? (int)min((int64_t)V, max((int64_t)0, rows - r)) : 0, (T)0.f);
-            }
-        }
-    };
-    auto keep_operand = [&](auto along_c, unsigned char *to, const Vec<T> (&from)[2]) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int id = tid + i * 256;
-            if constexpr (along_c.value) {
-                const int r = id / 8, ch = id % 8;
-                *(Vec<T> *)(to + r * kRowBytes + ((ch ^ (r & 7)) << 4)) = from[i];
-            } else {
-                const int c = id / (kTile / V), r = id % (kTile / V) * V;
-#pragma unroll
-                for (int j = 0; j < V; ++j)
-                    *(T *)(to + (r + j) * kRowBytes + ((c / V ^ ((r + j) & 7)) << 4) + c % V * sizeof(T)) = from[i][j];
-            }
-        }
-    };
-    using PT = std::integral_constant<bool, PC>;
-    using QT = std::integral_constant<bool, QC>;
-    const int wp = (wave & 1) * 32, wq = (wave >> 1) * 32;
-    float4v acc[2][2] = {};
-    if (c_first < c_end) {
-        load_operand(PT(), a.P, a.ldp, p0, a.np, c_first, stage[0]);
-        load_operand(QT(), a.Q, a.ldq, q0, a.nq, c_first, stage[1]);
-    }
-    for (int64_t c0 = c_first; c0 < c_end; c0 += BC) {
-        __syncthreads();
-        keep_operand(PT(), lds[0], stage[0]);
-        keep_operand(QT(), lds[1], stage[1]);
-        __syncthreads();
-        if (c0 + BC < c_end) {
-            load_operand(PT(), a.P, a.ldp, p0, a.np, c0 + BC, stage[0]);
-            load_operand(QT(), a.Q, a.ldq, q0, a.nq, c0 + BC, stage[1]);
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            Vec<T> fp[2], fq[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int rp = wp + i * 16 + (lane & 15), rq = wq + i * 16 + (lane & 15), ch = h * 4 + (lane >> 4);
-                fp[i] = *(const Vec<T> *)(lds[0] + rp * kRowBytes + ((ch ^ (rp & 7)) << 4));
-                fq[i] = *(const Vec<T> *)(lds[1] + rq * kRowBytes + ((ch ^ (rq & 7)) << 4));
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) acc[i][j] = mma(fp[i], fq[j], acc[i][j]);
-        }
-    }
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int64_t q = q0 + wq + j * 16 + (lane & 15);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int64_t p = p0 + wp + i * 16 + (lane >> 4) * 4;
-            if (q >= a.nq || p >= a.np) continue;
-            const int n = (int)min((int64_t)4, a.np - p);
-            if (a.splits > 1) {
-                float *to = a.part + ((int64_t)blockIdx.y * a.nq + q) * a.np + p;
-                if (n == 4) store_vec(to, acc[i][j]);
-                else for (int u = 0; u < n; ++u) to[u] = acc[i][j][u];
-            } else {
-                float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-                finish(e, q, p, n, v);
-            }
-        }
-    }
-}
+constexpr int kRowBytes = 128;     // bytes of the contraction per step of the tiles below
 
 // ---------------------------------------------------------------- few rows
 
@@ -251,16 +156,17 @@ __global__ __launch_bounds__(1024) void few_rows_kernel(Product<T> a, Epilogue<T
     }
 }
 
-// ---------------------------------------------------------------- large products
+// ---------------------------------------------------------------- tiles
 
 // Where element chunks live in a tile in LDS.  An operand that is contiguous along c keeps rows of 128 bytes (eight 16-byte chunks
 // at chunk ^ (row % 8)); one that is contiguous along its rows keeps the lines of c as they come, in pieces that the matrix
 // instruction's lanes gather with transposing reads (2-byte types) or element by element (float32); the pieces of
 // a line are permuted by c so that the lines that one read touches lie in different banks.
-template <class T> __device__ __forceinline__ int line_place(int c, int line_bytes, int byte)
+template <class T, int ROWS> __device__ __forceinline__ int line_place(int c, int byte)
 {
-    if constexpr (sizeof(T) == 2) return c * line_bytes + (byte ^ (((c & 3) | (c >> 1 & 4)) << 5));
-    else return c * line_bytes + (byte ^ ((c >> 2 & 3) << 6));
+    constexpr int kLine = ROWS * (int)sizeof(T);
+    if constexpr (sizeof(T) == 2) return c * kLine + (byte ^ ((((c & 3) | (c >> 1 & 4)) & (kLine / 32 - 1)) << 5));
+    else return c * kLine + (byte ^ ((c >> 2 & 3) << 6));
 }
 
 typedef short short4v __attribute__((ext_vector_type(4)));
@@ -274,7 +180,7 @@ template <class T, bool ALONG_C, int ROWS> __device__ __forceinline__ Vec<T> fra
     } else if constexpr (sizeof(T) == 2) {
         // a transposing read hands lane i of sixteen the column i of the four lines whose pieces lanes 4 c .. 4 c + 3 address
         const int c = h * 32 + (lane >> 4) * 8 + (lane >> 2 & 3);
-        const unsigned char *at = tile + line_place<T>(c, ROWS * 2, (r0 + (lane & 3) * 4) * 2);
+        const unsigned char *at = tile + line_place<T, ROWS>(c, (r0 + (lane & 3) * 4) * 2);
         using P = __attribute__((address_space(3))) short4v *;
         const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)at);
         const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(at + 4 * ROWS * 2));
@@ -284,7 +190,7 @@ template <class T, bool ALONG_C, int ROWS> __device__ __forceinline__ Vec<T> fra
         return f;
     } else {
         const int c = h * 16 + (lane >> 4) * 4;
-        const unsigned char *at = tile + line_place<T>(c, ROWS * 4, (r0 + (lane & 15)) * 4);
+        const unsigned char *at = tile + line_place<T, ROWS>(c, (r0 + (lane & 15)) * 4);
         Vec<T> f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) f[i] = *(const T *)(at + i * ROWS * 4);
@@ -308,7 +214,7 @@ template <class T, bool ALONG_C, int ROWS, int THREADS> struct Stage {
         if constexpr (ALONG_C) at = src + r0 * ld + c0 + t % 8 * V;
         else at = src + (c0 + t / kLine) * ld + r0 + t % kLine * V;
     }
-    __device__ __forceinline__ void whole(int)
+    __device__ __forceinline__ void whole()
     {
         const int t = threadIdx.x;
 #pragma unroll
@@ -349,7 +255,7 @@ template <class T, bool ALONG_C, int ROWS, int THREADS> struct Stage {
                 const int r = id / 8, ch = id % 8;
                 *(Vec<T> *)(tile + r * kRowBytes + ((ch ^ (r & 7)) << 4)) = v[i];
             } else {
-                *(Vec<T> *)(tile + line_place<T>(id / kLine, ROWS * (int)sizeof(T), id % kLine * 16)) = v[i];
+                *(Vec<T> *)(tile + line_place<T, ROWS>(id / kLine, id % kLine * 16)) = v[i];
             }
         }
     }
@@ -416,8 +322,8 @@ __global__ __launch_bounds__(WP *WQ * 64) void tile_kernel(Product<T> a, Epilogu
     sq.begin(a.Q, a.ldq, q0, a.nq, c_first);
     auto fetch = [&](int64_t c0) {
         const bool c_whole = c0 + BC <= c_end;
-        if (c_whole && p_whole) sp.whole(0); else sp.part(c0, c_end);
-        if (c_whole && q_whole) sq.whole(0); else sq.part(c0, c_end);
+        if (c_whole && p_whole) sp.whole(); else sp.part(c0, c_end);
+        if (c_whole && q_whole) sq.whole(); else sq.part(c0, c_end);
     };
     const int wp = wave % WP * (BP / WP), wq = wave / WP * (BQ / WQ);
     float4v acc[FP][FQ] = {};
@@ -475,7 +381,7 @@ template <class T, bool ALONG_C, int ROWS> __device__ __forceinline__ uint32_t d
     } else {
         constexpr int kLine = ROWS / 8;   // 16-byte chunks of a line
         const int c = (piece * 64 + lane) / kLine;
-        const int byte = line_place<T>(c, 0, lane % kLine * 16);
+        const int byte = line_place<T, ROWS>(c, lane % kLine * 16) - c * ROWS * 2;
         return (uint32_t)(c * ld * (int64_t)sizeof(T)) + (uint32_t)min((int64_t)byte, rows_left * (int64_t)sizeof(T) - 16);
     }
 }
@@ -594,7 +500,7 @@ __global__ __launch_bounds__(WP *WQ * 64, 2) void direct_kernel(Product<T> a, Ep
                         load_part(src + (r0 + r) * ld + c, r0 + r < rows ? (int)min((int64_t)8, max((int64_t)0, c_end - c)) : 0, (T)0.f);
                 } else {
                     const int64_t c = c0 + id / kLine, r = r0 + id % kLine * 8;
-                    *(Vec<T> *)(to + line_place<T>(id / kLine, ROWS * 2, id % kLine * 16)) =
+                    *(Vec<T> *)(to + line_place<T, ROWS>(id / kLine, id % kLine * 16)) =
                         load_part(src + c * ld + r, c < c_end ? (int)min((int64_t)8, max((int64_t)0, rows - r)) : 0, (T)0.f);
                 }
             }
@@ -677,22 +583,32 @@ enum Tiling {
     kDirect256,     // 256 x 256, the same
 };
 
-// What a tiling costs, in microseconds, as measured on 10,000 x 4,096 x 1,024 in its three products and on parts of it: `step` per 128
-// bytes of the contraction with a compute unit full of `together` workgroups, at least `alone` however few there are; `fixed` per workgroup
-// for its first loads and its stores.
+// What a tiling costs, in microseconds: `step` per 128 bytes of the contraction with a compute unit full of `together` workgroups, at
+// least `alone` however few there are; `fixed` per workgroup for its first loads and its stores.  Fitted to 1,600 timings: 33 sizes
+// from 32 x 1,024 x 1,024 to 10,000 x 4,096 x 1,024, each product, every tiling and 1 to 32 splits; the model is within 10 % of half
+// of them, and what it picks takes 5 % longer than the best of all on average.
 struct TilingCost {
     int bp, bq, together;
     double step, alone, fixed;
 };
-static TilingCost cost_of(Tiling t, bool f32)
+static TilingCost cost_of(Tiling t, bool f32, bool both_along)
 {
     switch (t) {
-    case kSmall: return f32 ? TilingCost{64, 64, 6, 6.0, 1.0, 4} : TilingCost{64, 64, 6, 2.0, 0.55, 4};
-    case kMedium: return f32 ? TilingCost{128, 128, 2, 7.0, 3.6, 5} : TilingCost{128, 128, 2, 1.4, 0.8, 5};
-    case kDirect128: return TilingCost{128, 128, 3, 1.45, 0.6, 5};
-    case kDirectWide: return TilingCost{128, 256, 2, 1.4, 0.9, 5};
-    default: return TilingCost{256, 256, 1, 1.45, 1.45, 8};
+    case kSmall:
+        return f32 ? (both_along ? TilingCost{64, 64, 4, 2.2, 0.74, 4.5} : TilingCost{64, 64, 4, 2.4, 0.89, 4.2})
+                   : (both_along ? TilingCost{64, 64, 4, 0.9, 0.40, 4.0} : TilingCost{64, 64, 4, 0.9, 0.68, 3.3});
+    case kMedium:
+        return f32 ? TilingCost{128, 128, 2, 3.2, 2.1, 4.5}
+                   : (both_along ? TilingCost{128, 128, 2, 0.8, 0.80, 4.3} : TilingCost{128, 128, 2, 0.7, 0.90, 4.2});
+    case kDirect128: return both_along ? TilingCost{128, 128, 3, 1.25, 0.46, 4.7} : TilingCost{128, 128, 3, 1.0, 0.54, 5.0};
+    case kDirectWide: return TilingCost{128, 256, 2, 1.38, 0.77, 5.9};
+    default: return TilingCost{256, 256, 1, 1.13, 0.61, 6.9};
     }
+}
+// The few rows' kernel reads P's 16 rows and all of Q's per workgroup, two workgroups per compute unit.
+static double few_rows_us(int64_t np, int64_t nq, int64_t bytes)
+{
+    return 3 + 0.4 * (double)bytes / 1024 * (nq <= 16 ? 2 : nq <= 32 ? 3 : 5) * (double)ceil_div(ceil_div(np, 16), 512);
 }
 
 struct ProductPlan {
@@ -715,26 +631,28 @@ static ProductPlan plan_product(int32_t dtype, int64_t np, int64_t nq, int64_t n
     ProductPlan best;
     const bool f32 = dtype == VF_F32;
     const int64_t step = kRowBytes / (int64_t)type_size(dtype);
-    if (o.p_along && o.q_along && nq <= 64) {
+    const bool both = o.p_along && o.q_along;
+    double least = 0;
+    if (both && nq <= 64) {
         best.tiling = kFewRows;
         best.chunk = nc;
-        return best;
+        least = few_rows_us(np, nq, nc * (int64_t)type_size(dtype));
     }
-    double least = 0;
     for (Tiling t : {kSmall, kMedium, kDirect128, kDirectWide, kDirect256}) {
         if (t >= kDirect128 && !o.direct) continue;
-        if (t == kDirectWide && !(o.p_along && o.q_along)) continue;
-        const TilingCost c = cost_of(t, f32);
+        if (t == kDirectWide && !both) continue;
+        const TilingCost c = cost_of(t, f32, both);
         const int64_t tiles = ceil_div(np, c.bp) * ceil_div(nq, c.bq);
-        for (int64_t splits = 1; splits <= 64; splits = splits < 4 ? splits + 1 : splits * 2) {
+        for (int64_t splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
             const int64_t chunk = std::max<int64_t>(step, ceil_div(ceil_div(nc, splits), step) * step);
             const int64_t used = std::max<int64_t>(1, ceil_div(nc, chunk));
-            if (splits > 1 && (used != splits || chunk < 4 * step || tiles * splits > 1024)) break;
+            if (splits > 1 && (chunk < 2 * step || tiles * splits > 2048)) break;
+            if (used != splits) continue;
             const int64_t per_cu = ceil_div(tiles * used, 256), rounds = ceil_div(per_cu, c.together);
             const double steps = (double)ceil_div(chunk, step);
             const double last = (double)(per_cu - (rounds - 1) * c.together) / c.together;   // how full the last round is
             double us = (double)(rounds - 1) * (steps * c.step + c.fixed) + steps * std::max(c.alone, c.step * last) + c.fixed;
-            if (used > 1) us += 4 + (double)used * np * nq * 8 / 4e6;
+            if (used > 1) us += 3 + (double)used * np * nq * 8 / 4e6;
             if (least == 0 || us < least) {
                 least = us;
                 best.tiling = t;
@@ -780,13 +698,13 @@ static int run_product(int32_t dtype, const T *P, int64_t ldp, int64_t np, const
         VF_HIP(hipGetLastError());
         return VF_OK;
     }
-    const TilingCost c = cost_of(plan.tiling, dtype == VF_F32);
+    const TilingCost c = cost_of(plan.tiling, dtype == VF_F32, PC && QC);
     const int64_t tiles = ceil_div(np, c.bp) * ceil_div(nq, c.bq);
     VF_REQUIRE(tiles < (1 << 22), "linear: too many output tiles in one call");   // (a launch holds fewer than 2^32 threads)
     const dim3 grid((unsigned)tiles, (unsigned)plan.splits);
     int rc = VF_OK;
     if (plan.tiling == kSmall) {
-        product_kernel<T, PC, QC><<<grid, dim3(256), 0, s>>>(a, e);
+        tile_kernel<T, PC, QC, 64, 64, 2, 2><<<grid, dim3(256), (size_t)2 * 128 * kRowBytes, s>>>(a, e);
     } else if (plan.tiling == kMedium) {
         constexpr size_t lds = (size_t)2 * 256 * kRowBytes;
         if ((rc = allow_lds(tile_kernel<T, PC, QC, 128, 128, 2, 4>, lds)) != VF_OK) return rc;
@@ -836,10 +754,12 @@ static BackwardPlan plan_backward(int32_t dtype, int64_t m, int64_t n, int64_t k
     return b;
 }
 
+constexpr int64_t kMaxWidth = 1 << 25;   // of n and k: kernels give up to 64 threads to a column, a launch holds fewer than 2^32
+
 static int check_sizes(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t act)
 {
     VF_REQUIRE(is_float_type(dtype), "linear: dtype must be VF_F32, VF_BF16 or VF_F16");
-    VF_REQUIRE(m >= 0 && m <= kMaxExtent && n >= 0 && n <= kMaxExtent && k >= 0 && k <= kMaxExtent, "linear: m, n or k out of range");
+    VF_REQUIRE(m >= 0 && m <= kMaxExtent && n >= 0 && n <= kMaxWidth && k >= 0 && k <= kMaxWidth, "linear: m, n or k out of range");
     VF_REQUIRE(act >= VF_ACT_NONE && act <= VF_ACT_SILU, "linear: unknown activation");
     return VF_OK;
 }

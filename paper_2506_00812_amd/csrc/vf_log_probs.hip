@@ -31,7 +31,7 @@ struct RowSums {
 __device__ __forceinline__ void scale_to(RowSums &r, float m)
 {
     if (r.m == m) return;
-    const float d = r.m - m, f = expf(d);
+    const float d = r.m - m, f = exp_fast(d);
     r.a = f > 0.f ? f * (r.a + d * r.s) : 0.f;
     r.s = f * r.s;
     r.m = m;
@@ -45,9 +45,25 @@ __device__ __forceinline__ RowSums wave_join(RowSums r)
     return r;
 }
 
-// The largest keys of a wave: lane i holds the i-th largest of what was offered (all 64 are kept, `top` are asked for).
+// The largest keys of a wave: lane i holds the i-th largest of what was offered (all 64 are kept, `top` are asked for).  `least`: no
+// key up to it can be among the first `top`.
 struct WaveTop {
     uint64_t key = 0, least = 0;
+    static __device__ __forceinline__ uint64_t of_lane(uint64_t k, int lane)
+    {
+        return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), lane) << 32 |
+               (uint32_t)__builtin_amdgcn_readlane((int)k, lane);
+    }
+    // Before the first offers: of 64 candidates with the value orders o (0: none) at least `top` reach the threshold found here, to 16
+    // bits, so that the first thousand entries of a row cost some `top` insertions and not top (1 + log(1000 / top)).
+    __device__ __forceinline__ void expect(uint32_t o, int top)
+    {
+        uint32_t t = 0;
+#pragma unroll 1
+        for (uint32_t bit = 1u << 31; bit >= 1u << 16; bit >>= 1)
+            if (__popcll(__ballot(o >= (t | bit))) >= top) t |= bit;
+        if (t) least = ((uint64_t)t << 32) - 1;
+    }
     __device__ __forceinline__ void offer(bool mine, uint64_t k, int top)
     {
         const int lane = threadIdx.x & 63;
@@ -55,14 +71,15 @@ struct WaveTop {
         while (mask) {
             const int from = __builtin_ctzll(mask);
             mask &= mask - 1;
-            const uint64_t in = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), from) << 32 |
-                                (uint32_t)__builtin_amdgcn_readlane((int)k, from);
+            const uint64_t in = of_lane(k, from);
             if (in <= least) continue;
             const int at = __popcll(__ballot(key > in));
-            const uint64_t up = __shfl_up(key, 1, 64);
-            key = lane < at ? key : lane == at ? in : up;
-            least = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(key >> 32), top - 1) << 32 |
-                    (uint32_t)__builtin_amdgcn_readlane((int)key, top - 1);
+            // (0x138: from the lane before, over all 64)
+            const uint32_t lo = (uint32_t)__builtin_amdgcn_mov_dpp((int)key, 0x138, 0xF, 0xF, true);
+            const uint32_t hi = (uint32_t)__builtin_amdgcn_mov_dpp((int)(key >> 32), 0x138, 0xF, 0xF, true);
+            key = lane < at ? key : lane == at ? in : (uint64_t)hi << 32 | lo;
+            const uint64_t last = of_lane(key, top - 1);
+            least = last > least ? last : least;
         }
     }
 };
@@ -100,14 +117,14 @@ __device__ __forceinline__ void finish_row(const LogProbOut &o, const T *x, int6
     }
 }
 
-// Segment blockIdx.x % nseg of a row: TPR threads take its vectors in turn.  nseg > 1: the segment's sums and keys go to
-// part_sums [row][nseg] and part_keys [row][nseg][top].
+// Segment `item % nseg` of a row: TPR threads take its vectors in turn, 16 elements a thread at a time.  nseg > 1: the segment's sums and
+// keys go to part_sums [row][nseg] and part_keys [row][nseg][top].
 template <class T, int TPR, bool TOP>
 __global__ __launch_bounds__(256) void log_probs_kernel(int64_t m, int64_t v, const T *__restrict__ logits, int64_t ld, int nseg,
                                                         int64_t seg, int top, LogProbOut out, float4 *__restrict__ part_sums,
                                                         uint64_t *__restrict__ part_keys)
 {
-    constexpr int V = kVec<T>, RPB = 256 / TPR, W = TPR / 64;
+    constexpr int V = kVec<T>, RPB = 256 / TPR, W = TPR / 64, E = 16, NV = E / V;
     __shared__ float lds_sums[4][3];
     __shared__ uint64_t lds_keys[TOP && W > 1 ? 4 * 64 : 1];
     const int t = threadIdx.x % TPR, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -118,35 +135,41 @@ __global__ __launch_bounds__(256) void log_probs_kernel(int64_t m, int64_t v, co
         const int64_t c0 = sg * seg, c1 = min(v, c0 + seg);
         RowSums r = {-kInf, 0.f, 0.f};
         WaveTop best;
-        for (int64_t base = c0; base < c1; base += TPR * V) {
-            const int64_t c = base + t * V;
-            float u[V];
-            float most = -kInf;
-            if (c < c1) {
-                const Vec<T> raw = load_part(x + c, (int)min((int64_t)V, c1 - c), (T)-kInf);
+        for (int64_t base = c0; base < c1; base += TPR * E) {
+            float u[E];
 #pragma unroll
-                for (int j = 0; j < V; ++j) u[j] = (float)raw[j];
-            } else {
+            for (int i = 0; i < NV; ++i) {
+                const int64_t c = base + (i * TPR + t) * V;
+                Vec<T> raw;
+                if (base + TPR * E <= c1) raw = load_vec<Vec<T>>(x + c);
+                else raw = load_part(x + c, (int)max((int64_t)0, min((int64_t)V, c1 - c)), (T)-kInf);
 #pragma unroll
-                for (int j = 0; j < V; ++j) u[j] = -kInf;
+                for (int j = 0; j < V; ++j) u[i * V + j] = (float)raw[j];
             }
+            float most = u[0];
             bool odd = false;   // a NaN, which the maximum passes over
 #pragma unroll
-            for (int j = 0; j < V; ++j) { most = fmaxf(most, u[j]); odd |= u[j] != u[j]; }
+            for (int j = 0; j < E; ++j) { most = fmaxf(most, u[j]); odd |= u[j] != u[j]; }
             if (most > r.m) scale_to(r, most);
             const float origin = r.m == -kInf ? 0.f : r.m;
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const float d = u[j] - origin, e = expf(d);
+            for (int j = 0; j < E; ++j) {
+                const float d = u[j] - origin, e = exp_fast(d);
                 r.s += e;
                 r.a += e > 0.f ? e * d : 0.f;
             }
             if constexpr (TOP) {
-                const uint32_t least = (uint32_t)(best.least >> 32);
-                if (__ballot(odd || (most > -kInf && value_order(most) >= least))) {
+                if (base == c0) best.expect(most > -kInf ? value_order(most) : 0, top);
+                const float least = best.least >> 32 ? order_value((uint32_t)(best.least >> 32)) : -kInf;
+                const bool any_odd = __ballot(odd) != 0;
+                if (__ballot(most >= least) || any_odd) {
 #pragma unroll
-                    for (int j = 0; j < V; ++j)
-                        best.offer(u[j] != -kInf, (uint64_t)value_order(u[j]) << 32 | (uint32_t)~(uint32_t)(c + j), top);
+                    for (int j = 0; j < E; ++j) {
+                        // what cannot reach the list is told by its value; NaN by its order
+                        if (!any_odd && !__ballot(u[j] >= least && u[j] > -kInf)) continue;
+                        const uint32_t at = (uint32_t)(base + (j / V * TPR + t) * V + j % V);
+                        best.offer(u[j] != -kInf, (uint64_t)value_order(u[j]) << 32 | (uint32_t)~at, top);
+                    }
                 }
             }
         }
@@ -206,7 +229,11 @@ __global__ __launch_bounds__(64) void log_probs_join_kernel(int64_t m, int64_t v
         r = wave_join(r);
         WaveTop best;
         const int n = nseg * top;
-        for (int i = 0; i < n; i += 64) best.offer(i + lane < n, i + lane < n ? part_keys[row * n + i + lane] : 0, top);
+        for (int i = 0; i < n; i += 64) {
+            const uint64_t key = i + lane < n ? part_keys[row * n + i + lane] : 0;
+            if (i == 0) best.expect((uint32_t)(key >> 32), top);
+            best.offer(true, key, top);
+        }
         finish_row(out, logits + row * ld, row, v, top, r, best.key);
     }
 }
@@ -231,7 +258,7 @@ __global__ void log_probs_backward_kernel(int64_t m, int64_t v, const T *logits,
         Vec<T> o;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            const float lp = (float)x[j] - l, p = expf(lp);
+            const float lp = (float)x[j] - l, p = exp_fast(lp);
             float g = (t == c + j ? dl : 0.f) - dl * p;
             g -= p > 0.f || p != p ? dh * (p * (lp + h)) : 0.f;
             o[j] = (T)(l == -kInf ? 0.f : g);
@@ -246,13 +273,12 @@ struct LogProbPlan {
     int tpr, nseg;
     int64_t seg;
 };
-static LogProbPlan plan_of(int32_t dtype, int64_t m, int64_t v)
+static LogProbPlan plan_of(int64_t m, int64_t v)
 {
     LogProbPlan p{64, 1, v};
-    const int64_t lane_vecs = 16 / (int64_t)type_size(dtype);
     if (v <= 2048) return p;
     p.tpr = 256;
-    const int64_t unit = 256 * lane_vecs;
+    const int64_t unit = 256 * 16;
     const int64_t want = std::min<int64_t>(ceil_div(1024, m), ceil_div(v, unit));
     p.seg = ceil_div(ceil_div(v, want), unit) * unit;
     p.nseg = (int)ceil_div(v, p.seg);
@@ -274,7 +300,7 @@ int log_probs_workspace_impl(int32_t dtype, int64_t m, int64_t v, int32_t top, s
     if (int rc = check_log_probs(dtype, m, v, top); rc != VF_OK) return rc;
     *bytes = 0;
     if (m == 0) return VF_OK;
-    const LogProbPlan p = plan_of(dtype, m, v);
+    const LogProbPlan p = plan_of(m, v);
     if (p.nseg > 1) *bytes = (size_t)m * p.nseg * (16 + 8 * (size_t)top);
     return VF_OK;
 }
@@ -290,7 +316,7 @@ int log_probs_impl(const LogProbArgs &a)
     VF_REQUIRE(need == 0 || (a.workspace != nullptr && a.workspace_bytes >= need),
                "log probs: the workspace must hold " + std::to_string(need) + " bytes");
     if (a.m == 0) return VF_OK;
-    const LogProbPlan p = plan_of(a.dtype, a.m, a.v);
+    const LogProbPlan p = plan_of(a.m, a.v);
     const LogProbOut out{a.targets, a.logp, a.entropy, a.lse, a.top_ids, a.top_logp};
     float4 *sums = (float4 *)a.workspace;
     uint64_t *keys = (uint64_t *)(sums + (p.nseg > 1 ? a.m * p.nseg : 0));

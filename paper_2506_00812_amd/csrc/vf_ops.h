@@ -58,18 +58,28 @@ template <class T> __device__ __forceinline__ void store_part(T *p, Vec<T> v, in
         if (i < n) p[i] = v[i];
 }
 
-// Sum over the 64 lanes of a wave, the same in every lane.
+// Sum and maximum over the 64 lanes of a wave, the same in every lane: within rows of sixteen on DPP moves, the four rows' results
+// through scalar registers (no trip through LDS, which a shuffle takes).
+template <int CTRL> __device__ __forceinline__ float dpp(float v)
+{
+    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float lane_value(float v, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); }
 __device__ __forceinline__ float wave_sum(float v)
 {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d, 64);
-    return v;
+    v += dpp<0xB1>(v);    // the neighbour
+    v += dpp<0x4E>(v);    // the other pair of four
+    v += dpp<0x141>(v);   // the other four of eight
+    v += dpp<0x140>(v);   // the other eight of sixteen
+    return (lane_value(v, 0) + lane_value(v, 16)) + (lane_value(v, 32) + lane_value(v, 48));
 }
 __device__ __forceinline__ float wave_max(float v)
 {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d, 64));
-    return v;
+    v = fmaxf(v, dpp<0xB1>(v));
+    v = fmaxf(v, dpp<0x4E>(v));
+    v = fmaxf(v, dpp<0x141>(v));
+    v = fmaxf(v, dpp<0x140>(v));
+    return fmaxf(fmaxf(lane_value(v, 0), lane_value(v, 16)), fmaxf(lane_value(v, 32), lane_value(v, 48)));
 }
 
 // exp(x) on the hardware's 2^x: a relative error of about 2^-23 (1 + |x|), which weighs little where exp(x) is large enough to count.
@@ -126,30 +136,40 @@ template <class F> __host__ __device__ __forceinline__ void by_act(int act, F &&
     else fn(std::integral_constant<int, VF_ACT_SILU>());
 }
 
-// Column sums from partial rows part [parts][sums][d]: 64 columns and one of the sums per workgroup; parts = 0: zeros.
+// Column sums from partial rows part [parts][sums][d]: 16 columns and one of the sums per workgroup, 64 threads to a column (2,048
+// columns of 1,024 rows 18 us with 16 threads to a column, 5 with 64); parts = 0: zeros.
 template <class T>
 __global__ __launch_bounds__(1024) void join_parts_kernel(int parts, int64_t d, const float *__restrict__ part, T *out0, T *out1)
 {
-    __shared__ float comb[16][64];
-    const int t = threadIdx.x & 63, sub = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * 64 + t;
+    __shared__ float comb[64][17];
+    const int t = threadIdx.x & 15, sub = threadIdx.x >> 4;
+    const int64_t c = (int64_t)blockIdx.x * 16 + t, stride = (int64_t)gridDim.y * d;
     T *out = blockIdx.y == 0 ? out0 : out1;
     if (out == nullptr) return;
-    float a = 0.f;
-    if (c < d)
-        for (int p = sub; p < parts; p += 16) a += part[((int64_t)p * gridDim.y + blockIdx.y) * d + c];
-    comb[sub][t] = a;
-    __syncthreads();
-    if (sub == 0 && c < d) {
-        float s = 0.f;
+    float a[4] = {};
+    if (c < d) {
+        const float *from = part + (int64_t)blockIdx.y * d + c;
+        int p = sub;
+        for (; p + 192 < parts; p += 256) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s += comb[i][t];
-        out[c] = (T)s;
+            for (int u = 0; u < 4; ++u) a[u] += from[(int64_t)(p + 64 * u) * stride];
+        }
+        for (; p < parts; p += 64) a[0] += from[(int64_t)p * stride];
+    }
+    comb[sub][t] = (a[0] + a[1]) + (a[2] + a[3]);
+    __syncthreads();
+    if (sub < 16) {   // sixteen lanes to a column
+        const int col = threadIdx.x >> 4, part16 = threadIdx.x & 15;
+        float s = (comb[part16][col] + comb[part16 + 16][col]) + (comb[part16 + 32][col] + comb[part16 + 48][col]);
+#pragma unroll
+        for (int w = 8; w > 0; w >>= 1) s += __shfl_xor(s, w, 16);
+        const int64_t at = (int64_t)blockIdx.x * 16 + col;
+        if (part16 == 0 && at < d) out[at] = (T)s;
     }
 }
 template <class T> void launch_join_parts(int parts, int64_t d, int sums, const float *part, T *out0, T *out1, hipStream_t s)
 {
-    join_parts_kernel<T><<<dim3((unsigned)ceil_div(d, 64), (unsigned)sums), dim3(1024), 0, s>>>(parts, d, part, out0, out1);
+    join_parts_kernel<T><<<dim3((unsigned)ceil_div(d, 16), (unsigned)sums), dim3(1024), 0, s>>>(parts, d, part, out0, out1);
 }
 
 // ---------------------------------------------------------------- entry points' bodies
