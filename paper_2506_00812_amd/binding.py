@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -749,12 +750,16 @@ def adamw_state(param, bits=32):
 
 def _flat(t, what, kinds, dev, n):
     if t.dtype not in kinds or t.get_device() != dev or t.numel() != n or not t.is_contiguous():
-        raise VecflowError(f"{what} must be a contiguous tensor of {n} elements of {' or '.join(map(str, kinds))} on the device of the others")
+        raise VecflowError(f"adamw: {what} must be a contiguous tensor of {n} elements of {' or '.join(map(str, kinds))} "
+                           "on the current device")
     return t.data_ptr()
 
 
-def _adamw_list(ms, vs, m_scales, v_scales):
-    """(array of VfAdamwTensor with the moments filled in, device)"""
+_ADAMW_ITEM = struct.Struct("@7Pqd4i")     # VfAdamwTensor, field by field: one pack per tensor costs a tenth of its assignments
+
+
+def _adamw_moments_of(ms, vs, m_scales, v_scales):
+    """Per tensor (elements, state bits, addresses of m, v, m_scale, v_scale), and the device."""
     if _torch is None:
         _use_torch()
     count = len(ms)
@@ -763,24 +768,20 @@ def _adamw_list(ms, vs, m_scales, v_scales):
             raise VecflowError("adamw: the lists must have one entry per tensor")
     if (m_scales is None) != (v_scales is None):
         raise VecflowError("adamw: m_scales and v_scales go together")
-    arr = (VfAdamwTensor * max(count, 1))()
-    f32, dev = (_torch.float32,), _torch.cuda.current_device() if count else -1
+    F, I8, U8 = (_torch.float32,), (_torch.int8,), (_torch.uint8,)
+    dev = _torch.cuda.current_device() if count else -1
+    out = []
     for i, m in enumerate(ms):
         n = m.numel()
-        t = arr[i]
-        t.n = n
-        if m.dtype == _torch.float32:
-            t.state_bits = 32
-            t.m, t.v = _flat(m, f"ms[{i}]", f32, dev, n), _flat(vs[i], f"vs[{i}]", f32, dev, n)
-        else:
-            t.state_bits = 8
-            if m_scales is None or m_scales[i] is None or v_scales[i] is None:
-                raise VecflowError(f"adamw: tensor {i}: moments in 8 bits need scales")
-            blocks = -(-n // ADAMW_BLOCK)
-            t.m, t.v = _flat(m, f"ms[{i}]", (_torch.int8,), dev, n), _flat(vs[i], f"vs[{i}]", (_torch.uint8,), dev, n)
-            t.m_scale = _flat(m_scales[i], f"m_scales[{i}]", f32, dev, blocks)
-            t.v_scale = _flat(v_scales[i], f"v_scales[{i}]", f32, dev, blocks)
-    return arr, dev
+        if m.dtype == F[0]:
+            out.append((n, 32, _flat(m, "a first moment", F, dev, n), _flat(vs[i], "a second moment", F, dev, n), 0, 0))
+            continue
+        if m_scales is None or m_scales[i] is None or v_scales[i] is None:
+            raise VecflowError(f"adamw: tensor {i}: moments in 8 bits need scales")
+        blocks = -(-n // ADAMW_BLOCK)
+        out.append((n, 8, _flat(m, "a first moment", I8, dev, n), _flat(vs[i], "a second moment", U8, dev, n),
+                    _flat(m_scales[i], "a scale", F, dev, blocks), _flat(v_scales[i], "a scale", F, dev, blocks)))
+    return out, dev
 
 
 def adamw_step(params, grads, ms, vs, step, lr, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, grad_scale=1.0, masters=None,
@@ -795,29 +796,29 @@ def adamw_step(params, grads, ms, vs, step, lr, betas=(0.9, 0.999), eps=1e-8, we
     decay = weight_decay if isinstance(weight_decay, (list, tuple)) else [weight_decay] * count
     if len(decay) != count:
         raise VecflowError("adamw: weight_decay must be one number or one per tensor")
-    arr, dev = _adamw_list(ms, vs, m_scales, v_scales)
+    moments, dev = _adamw_moments_of(ms, vs, m_scales, v_scales)
     if count == 0:
         return
+    items, F, pack = [], (_torch.float32,), _ADAMW_ITEM.pack
     for i, p in enumerate(params):
-        t, g = arr[i], grads[i]
-        n = t.n
-        t.param, t.grad = _flat(p, f"params[{i}]", _codes, dev, n), _flat(g, f"grads[{i}]", _codes, dev, n)
-        t.param_type, t.grad_type = _codes[p.dtype], _codes[g.dtype]
-        if masters is not None and masters[i] is not None:
-            t.master = _flat(masters[i], f"masters[{i}]", (_torch.float32,), dev, n)
-        t.weight_decay = decay[i]
+        n, bits, pm, pv, pms, pvs = moments[i]
+        g, w = grads[i], None if masters is None else masters[i]
+        items.append(pack(_flat(p, "a parameter", _codes, dev, n), _flat(g, "a gradient", _codes, dev, n),
+                          0 if w is None else _flat(w, "a master", F, dev, n), pm, pv, pms, pvs, n, decay[i],
+                          _codes[p.dtype], _codes[g.dtype], bits, 0))
     prm = VfAdamwParams(lr, betas[0], betas[1], eps, grad_scale, step)
     handle = _raw_stream(dev) if stream is None else stream.cuda_stream
-    _check(load_library().vf_adamw_step(arr, count, C.byref(prm), _vector(skip, "skip", _torch.int32, dev, 1), handle))
+    _check(load_library().vf_adamw_step(b"".join(items), count, C.byref(prm), _vector(skip, "skip", _torch.int32, dev, 1), handle))
 
 
 def adamw_moments(ms, vs, m_scales=None, v_scales=None, stream=None):
     """The moments as float32 tensors: lists (m, v) (vf_adamw_moments)."""
-    arr, dev = _adamw_list(ms, vs, m_scales, v_scales)
+    moments, dev = _adamw_moments_of(ms, vs, m_scales, v_scales)
     count = len(ms)
     if count == 0:
         return [], []
-    sizes = [t.numel() for t in ms]
+    items = b"".join([_ADAMW_ITEM.pack(0, 0, 0, pm, pv, pms, pvs, n, 0.0, 0, 0, bits, 0) for n, bits, pm, pv, pms, pvs in moments])
+    sizes = [t[0] for t in moments]
     at = [0]
     for n in sizes:
         at.append(at[-1] + n)
@@ -828,5 +829,5 @@ def adamw_moments(ms, vs, m_scales=None, v_scales=None, stream=None):
         outs.append(list(whole.split(sizes)))
         ptrs.append((C.c_void_p * count)(*[base + 4 * a for a in at[:-1]]))
     handle = _raw_stream(dev) if stream is None else stream.cuda_stream
-    _check(load_library().vf_adamw_moments(arr, count, ptrs[0], ptrs[1], handle))
+    _check(load_library().vf_adamw_moments(items, count, ptrs[0], ptrs[1], handle))
     return outs[0], outs[1]

@@ -1,6 +1,7 @@
 // One AdamW step over a list of tensors in few launches: the list travels as a kernel argument (48 tensors a launch), a
-// wave takes blocks of 256 elements, four neighbours a lane.  With moments in 8 bits a block shares a scale, so the wave that
-// holds it takes the largest moment without leaving its registers.  Bound by memory: every operand is read and written once.
+// wave takes four blocks of 256 elements at a time, four neighbours a lane and block, all of whose loads are on their way before the
+// first result.  With moments in 8 bits a block shares a scale, so the wave that holds it takes the largest moment without leaving
+// its registers.  Bound by memory: every operand is read and written once.
 //
 // The operations are single float32 ones in the order that the header states (no fused multiply-add), divisions and square
 // roots rounded correctly: a plain evaluation gives the same bits, codes included.
@@ -9,6 +10,7 @@
 namespace vf {
 
 constexpr int kBlock = VF_ADAMW_BLOCK;
+constexpr int kUnit = 4;             // blocks that a wave takes at a time
 constexpr int kLaunchTensors = 48;   // 76 bytes each: the argument block of a kernel holds 4096
 
 struct AdamwItem {
@@ -23,7 +25,7 @@ struct AdamwItem {
 };
 struct AdamwList {
     AdamwItem item[kLaunchTensors];
-    uint32_t first[kLaunchTensors + 1];   // tensor i has the blocks first[i] .. first[i + 1]
+    uint32_t first[kLaunchTensors + 1];   // tensor i has the units (of kUnit blocks) first[i] .. first[i + 1]
     int32_t n;
 };
 static_assert(sizeof(AdamwList) <= 3900, "the list must fit a kernel's argument block");
@@ -89,52 +91,69 @@ __device__ __forceinline__ void store4_codes(void *p, int64_t at, int n, const u
     else for (int j = 0; j < 4; ++j) if (j < n) q[j] = c[j];
 }
 
-// Code of x >= 0 under the block's scale, inv = 1 / scale.
-__device__ __forceinline__ float code_of(float x, float inv, float steps)
+// Code of x >= 0 under the block's scale, inv = 1 / scale: steps sqrt(x inv), rounded to even.  EXACT: with the square root rounded
+// correctly.  Otherwise with the hardware's, which is off by at most one unit in the last place: `near` tells that the product may be
+// that close to the middle between two codes (a few in 10,000), so that the code has to be taken again.
+template <bool EXACT> __device__ __forceinline__ float code_of(float x, float inv, float steps, bool &near)
 {
-    return x > 0.f ? fminf(rintf(sqrtf(x * inv) * steps), steps) : 0.f;
+    const float y = x * inv;
+    const float c = (EXACT ? sqrtf(y) : __builtin_amdgcn_sqrtf(y)) * steps;
+    if constexpr (!EXACT) near |= fabsf(__builtin_amdgcn_fractf(c) - 0.5f) < 1e-4f;   // 254 x 2^-22 is 0.6e-4
+    return x > 0.f ? fminf(rintf(c), steps) : 0.f;
 }
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) <= kFltMax; }
 
-__device__ __forceinline__ int find_tensor(const AdamwList &l, uint32_t block)
+__device__ __forceinline__ int find_tensor(const AdamwList &l, uint32_t unit)
 {
     int lo = 0, hi = l.n - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (l.first[mid] <= block) lo = mid; else hi = mid - 1;
+        if (l.first[mid] <= unit) lo = mid; else hi = mid - 1;
     }
     return lo;
 }
 
-template <int BITS>
-__global__ __launch_bounds__(256) void adamw_kernel(const AdamwList l, const AdamwScalars c, const int32_t *skip)
-{
-    if (skip && *skip != 0) return;
-    const int lane = threadIdx.x & 63;
-    const uint32_t blocks = l.first[l.n];
-    for (uint32_t block = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)); block < blocks; block += gridDim.x * 4) {
-        const int i = find_tensor(l, block);
-        const AdamwItem &t = l.item[i];
-        const uint32_t b = block - l.first[i];
+// Four elements a lane of one block, before and after the step.
+template <int BITS> struct AdamwBlock {
+    float p[4], g[4], m[4], v[4], ms, vs;
+    uint8_t cm[4], cv[4];
+
+    __device__ __forceinline__ void load(const AdamwItem &t, uint32_t b, int lane)
+    {
         const int64_t at = (int64_t)b * kBlock + lane * 4;
         const int n = (int)max((int64_t)0, min((int64_t)4, t.n - at));
-        const int ptype = t.types & 0xFF, gtype = t.types >> 8;
-        float p[4], g[4], m[4], v[4], root[4];
-        if (t.master) load4(t.master, VF_F32, at, n, p); else load4(t.param, ptype, at, n, p);
-        load4(t.grad, gtype, at, n, g);
+        if (t.master) load4(t.master, VF_F32, at, n, p); else load4(t.param, t.types & 0xFF, at, n, p);
+        load4(t.grad, t.types >> 8, at, n, g);
         if constexpr (BITS == 32) {
             load4(t.m, VF_F32, at, n, m);
             load4(t.v, VF_F32, at, n, v);
         } else {
-            uint8_t cm[4], cv[4];
             load4_codes(t.m, at, n, cm);
             load4_codes(t.v, at, n, cv);
-            const float ms = t.m_scale[b], vs = t.v_scale[b];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) { m[j] = m_of((int8_t)cm[j], ms); v[j] = v_of(cv[j], vs); }
+            ms = t.m_scale[b];
+            vs = t.v_scale[b];
         }
+    }
+    template <bool EXACT> __device__ __forceinline__ bool encode(const float (&root)[4], float mi, float vi)
+    {
+        bool near = false;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
+            const int a = (int)code_of<EXACT>(fabsf(m[j]), mi, 127.f, near);
+            const int r = (int)fmaxf(code_of<EXACT>(root[j], vi, 254.f, near), root[j] > 0.f ? 1.f : 0.f);
+            cm[j] = finite(m[j]) ? (uint8_t)(m[j] < 0.f ? -a : a) : (uint8_t)0x80;
+            cv[j] = finite(root[j]) ? (uint8_t)r : (uint8_t)255;
+        }
+        return near;
+    }
+    __device__ __forceinline__ void step(const AdamwItem &t, uint32_t b, int lane, const AdamwScalars &c)
+    {
+        const int64_t at = (int64_t)b * kBlock + lane * 4;
+        const int n = (int)max((int64_t)0, min((int64_t)4, t.n - at));
+        float root[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (BITS == 8) { m[j] = m_of((int8_t)cm[j], ms); v[j] = v_of(cv[j], vs); }
             const float gj = g[j] * c.grad_scale;
             m[j] = m[j] * c.beta1 + gj * c.one_beta1;
             v[j] = v[j] * c.beta2 + (gj * gj) * c.one_beta2;
@@ -142,12 +161,12 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamwList l, const Ada
             p[j] = p[j] * t.decay - (m[j] * c.c1) / (root[j] * c.c2 + c.eps) * c.lr;
         }
         if (t.master) store4(t.master, VF_F32, at, n, p);
-        store4(t.param, ptype, at, n, p);
+        store4(t.param, t.types & 0xFF, at, n, p);
         if constexpr (BITS == 32) {
             store4(t.m, VF_F32, at, n, m);
             store4(t.v, VF_F32, at, n, v);
         } else {
-            float ms = 0.f, vs = 0.f;
+            ms = vs = 0.f;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 if (finite(m[j])) ms = fmaxf(ms, fabsf(m[j]));
@@ -156,17 +175,37 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamwList l, const Ada
             ms = wave_max(ms);
             vs = wave_max(vs);
             const float mi = ms > 0.f ? 1.f / ms : 0.f, vi = vs > 0.f ? 1.f / vs : 0.f;
-            uint8_t cm[4], cv[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float a = code_of(fabsf(m[j]), mi, 127.f);
-                const float r = fmaxf(code_of(root[j], vi, 254.f), root[j] > 0.f ? 1.f : 0.f);
-                cm[j] = finite(m[j]) ? (uint8_t)(int8_t)(m[j] < 0.f ? -(int)a : (int)a) : (uint8_t)0x80;
-                cv[j] = finite(root[j]) ? (uint8_t)(int)r : (uint8_t)255;
-            }
+            if (__ballot(encode<false>(root, mi, vi))) encode<true>(root, mi, vi);
             store4_codes(t.m, at, n, cm);
             store4_codes(t.v, at, n, cv);
             if (lane == 0) { t.m_scale[b] = ms; t.v_scale[b] = vs; }
+        }
+    }
+};
+
+template <int BITS>
+__global__ __launch_bounds__(256) void adamw_kernel(const AdamwList l, const AdamwScalars c, const int32_t *skip)
+{
+    if (skip && *skip != 0) return;
+    const int lane = threadIdx.x & 63;
+    const uint32_t units = l.first[l.n];
+    for (uint32_t unit = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)); unit < units; unit += gridDim.x * 4) {
+        const int i = find_tensor(l, unit);
+        const AdamwItem &t = l.item[i];
+        const uint32_t b = (unit - l.first[i]) * kUnit;
+        const int64_t left = t.n - (int64_t)b * kBlock;
+        AdamwBlock<BITS> k[kUnit];
+        if (left >= kUnit * kBlock) {
+#pragma unroll
+            for (int u = 0; u < kUnit; ++u) k[u].load(t, b + u, lane);
+#pragma unroll
+            for (int u = 0; u < kUnit; ++u) k[u].step(t, b + u, lane, c);
+        } else {
+#pragma unroll 1
+            for (int u = 0; u < kUnit && (int64_t)u * kBlock < left; ++u) {
+                k[0].load(t, b + u, lane);
+                k[0].step(t, b + u, lane, c);
+            }
         }
     }
 }
@@ -175,34 +214,39 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamwList l, const Ada
 template <int BITS> __global__ __launch_bounds__(256) void adamw_moments_kernel(const AdamwList l)
 {
     const int lane = threadIdx.x & 63;
-    const uint32_t blocks = l.first[l.n];
-    for (uint32_t block = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)); block < blocks; block += gridDim.x * 4) {
-        const int i = find_tensor(l, block);
+    const uint32_t units = l.first[l.n];
+    for (uint32_t unit = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)); unit < units; unit += gridDim.x * 4) {
+        const int i = find_tensor(l, unit);
         const AdamwItem &t = l.item[i];
-        const uint32_t b = block - l.first[i];
-        const int64_t at = (int64_t)b * kBlock + lane * 4;
-        const int n = (int)max((int64_t)0, min((int64_t)4, t.n - at));
-        float m[4], v[4];
-        if constexpr (BITS == 32) {
-            if (t.master) load4(t.m, VF_F32, at, n, m);
-            if (t.param) load4(t.v, VF_F32, at, n, v);
-        } else {
-            uint8_t cm[4], cv[4];
-            if (t.master) {
-                load4_codes(t.m, at, n, cm);
-                const float ms = t.m_scale[b];
+        const uint32_t first = (unit - l.first[i]) * kUnit;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) m[j] = m_of((int8_t)cm[j], ms);
-            }
-            if (t.param) {
-                load4_codes(t.v, at, n, cv);
-                const float vs = t.v_scale[b];
+        for (int u = 0; u < kUnit; ++u) {
+            const uint32_t b = first + u;
+            if ((int64_t)b * kBlock >= t.n) break;
+            const int64_t at = (int64_t)b * kBlock + lane * 4;
+            const int n = (int)max((int64_t)0, min((int64_t)4, t.n - at));
+            float m[4], v[4];
+            if constexpr (BITS == 32) {
+                if (t.master) load4(t.m, VF_F32, at, n, m);
+                if (t.param) load4(t.v, VF_F32, at, n, v);
+            } else {
+                uint8_t cm[4], cv[4];
+                if (t.master) {
+                    load4_codes(t.m, at, n, cm);
+                    const float ms = t.m_scale[b];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] = v_of(cv[j], vs);
+                    for (int j = 0; j < 4; ++j) m[j] = m_of((int8_t)cm[j], ms);
+                }
+                if (t.param) {
+                    load4_codes(t.v, at, n, cv);
+                    const float vs = t.v_scale[b];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[j] = v_of(cv[j], vs);
+                }
             }
+            if (t.master) store4(t.master, VF_F32, at, n, m);
+            if (t.param) store4(t.param, VF_F32, at, n, v);
         }
-        if (t.master) store4(t.master, VF_F32, at, n, m);
-        if (t.param) store4(t.param, VF_F32, at, n, v);
     }
 }
 
@@ -222,7 +266,7 @@ static int each_launch(const vf_adamw_tensor *tensors, int32_t n_tensors, Fill &
                 l.n = 0;
             }
             fill(i, l.item[l.n]);
-            l.first[l.n + 1] = l.first[l.n] + (uint32_t)ceil_div(t.n, kBlock);
+            l.first[l.n + 1] = l.first[l.n] + (uint32_t)ceil_div(t.n, kBlock * kUnit);
             ++l.n;
         }
         if (l.n > 0) launch(l, bits);
