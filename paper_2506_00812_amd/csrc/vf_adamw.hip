@@ -1,6 +1,6 @@
 // One AdamW step over a list of tensors in few launches: the list travels as a kernel argument (48 tensors a launch), a
-// wave takes four blocks of 256 elements at a time, four neighbours a lane and block, all of whose loads are on their way before the
-// first result.  With moments in 8 bits a block shares a scale, so the wave that holds it takes the largest moment without leaving
+// wave takes one or four blocks of 256 elements at a time, four neighbours a lane and block, all of whose loads are on their way before
+// the first result.  With moments in 8 bits a block shares a scale, so the wave that holds it takes the largest moment without leaving
 // its registers.  Bound by memory: every operand is read and written once.
 //
 // The operations are single float32 ones in the order that the header states (no fused multiply-add), divisions and square
@@ -10,7 +10,9 @@
 namespace vf {
 
 constexpr int kBlock = VF_ADAMW_BLOCK;
-constexpr int kUnit = 4;             // blocks that a wave takes at a time
+// Blocks that a wave takes at a time.  Moments in 8 bits have much to compute per byte and gain from more loads on their way (18.8 M
+// elements: 78 us with four, 87 with one); in 32 bits the smaller pieces spread better (9.6 M elements: 54 us with one, 62 with four).
+template <int BITS> constexpr int kUnit = BITS == 8 ? 4 : 1;
 constexpr int kLaunchTensors = 48;   // 76 bytes each: the argument block of a kernel holds 4096
 
 struct AdamwItem {
@@ -25,7 +27,7 @@ struct AdamwItem {
 };
 struct AdamwList {
     AdamwItem item[kLaunchTensors];
-    uint32_t first[kLaunchTensors + 1];   // tensor i has the units (of kUnit blocks) first[i] .. first[i + 1]
+    uint32_t first[kLaunchTensors + 1];   // tensor i has the units (of kUnit<BITS> blocks) first[i] .. first[i + 1]
     int32_t n;
 };
 static_assert(sizeof(AdamwList) <= 3900, "the list must fit a kernel's argument block");
@@ -192,17 +194,17 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamwList l, const Ada
     for (uint32_t unit = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)); unit < units; unit += gridDim.x * 4) {
         const int i = find_tensor(l, unit);
         const AdamwItem &t = l.item[i];
-        const uint32_t b = (unit - l.first[i]) * kUnit;
+        const uint32_t b = (unit - l.first[i]) * kUnit<BITS>;
         const int64_t left = t.n - (int64_t)b * kBlock;
-        AdamwBlock<BITS> k[kUnit];
-        if (left >= kUnit * kBlock) {
+        AdamwBlock<BITS> k[kUnit<BITS>];
+        if (left >= kUnit<BITS> * kBlock) {
 #pragma unroll
-            for (int u = 0; u < kUnit; ++u) k[u].load(t, b + u, lane);
+            for (int u = 0; u < kUnit<BITS>; ++u) k[u].load(t, b + u, lane);
 #pragma unroll
-            for (int u = 0; u < kUnit; ++u) k[u].step(t, b + u, lane, c);
+            for (int u = 0; u < kUnit<BITS>; ++u) k[u].step(t, b + u, lane, c);
         } else {
 #pragma unroll 1
-            for (int u = 0; u < kUnit && (int64_t)u * kBlock < left; ++u) {
+            for (int u = 0; u < kUnit<BITS> && (int64_t)u * kBlock < left; ++u) {
                 k[0].load(t, b + u, lane);
                 k[0].step(t, b + u, lane, c);
             }
@@ -218,9 +220,9 @@ template <int BITS> __global__ __launch_bounds__(256) void adamw_moments_kernel(
     for (uint32_t unit = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)); unit < units; unit += gridDim.x * 4) {
         const int i = find_tensor(l, unit);
         const AdamwItem &t = l.item[i];
-        const uint32_t first = (unit - l.first[i]) * kUnit;
+        const uint32_t first = (unit - l.first[i]) * kUnit<BITS>;
 #pragma unroll
-        for (int u = 0; u < kUnit; ++u) {
+        for (int u = 0; u < kUnit<BITS>; ++u) {
             const uint32_t b = first + u;
             if ((int64_t)b * kBlock >= t.n) break;
             const int64_t at = (int64_t)b * kBlock + lane * 4;
@@ -266,7 +268,7 @@ static int each_launch(const vf_adamw_tensor *tensors, int32_t n_tensors, Fill &
                 l.n = 0;
             }
             fill(i, l.item[l.n]);
-            l.first[l.n + 1] = l.first[l.n] + (uint32_t)ceil_div(t.n, kBlock * kUnit);
+            l.first[l.n + 1] = l.first[l.n] + (uint32_t)ceil_div(t.n, kBlock * (bits == 8 ? kUnit<8> : kUnit<32>));
             ++l.n;
         }
         if (l.n > 0) launch(l, bits);
