@@ -69,16 +69,35 @@ __device__ __forceinline__ void store4(void *p, int type, int64_t at, int n, con
     }
 }
 
-// The moments that the codes of a block stand for.
+// The moments that codes stand for; the codes of what is not finite aside.
 __device__ __forceinline__ float m_of(int8_t c, float scale)
 {
     const float a = (float)c * (float)(1.0 / 127);
-    return c == -128 ? __uint_as_float(0x7FC00000u) : scale * (a * fabsf(a));
+    return scale * (a * fabsf(a));
 }
 __device__ __forceinline__ float v_of(uint8_t c, float scale)
 {
     const float b = (float)c * (float)(1.0 / 254), r = scale * (b * b);
-    return c == 255 ? __uint_as_float(0x7FC00000u) : r * r;
+    return r * r;
+}
+// The moments of four codes.  Codes of NaN are looked for in all lanes at once (a byte of x is zero where x - 1 borrows into its top bit).
+__device__ __forceinline__ void decode4(const uint8_t (&cm)[4], const uint8_t (&cv)[4], float ms, float vs, float (&m)[4], float (&v)[4])
+{
+    uint32_t wm, wv;
+    __builtin_memcpy(&wm, cm, 4);
+    __builtin_memcpy(&wv, cv, 4);
+    const uint32_t xm = wm ^ 0x80808080u, xv = ~wv;
+    const uint32_t odd = ((xm - 0x01010101u) & ~xm | (xv - 0x01010101u) & ~xv) & 0x80808080u;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) { m[j] = m_of((int8_t)cm[j], ms); v[j] = v_of(cv[j], vs); }
+    if (__ballot(odd != 0)) {
+        const float nan = __uint_as_float(0x7FC00000u);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            m[j] = cm[j] == 0x80 ? nan : m[j];
+            v[j] = cv[j] == 0xFF ? nan : v[j];
+        }
+    }
 }
 __device__ __forceinline__ void load4_codes(const void *p, int64_t at, int n, uint8_t (&c)[4])
 {
@@ -93,15 +112,19 @@ __device__ __forceinline__ void store4_codes(void *p, int64_t at, int n, const u
     else for (int j = 0; j < 4; ++j) if (j < n) q[j] = c[j];
 }
 
-// Code of x >= 0 under the block's scale, inv = 1 / scale: steps sqrt(x inv), rounded to even.  EXACT: with the square root rounded
-// correctly.  Otherwise with the hardware's, which is off by at most one unit in the last place: `near` tells that the product may be
-// that close to the middle between two codes (a few in 10,000), so that the code has to be taken again.
-template <bool EXACT> __device__ __forceinline__ float code_of(float x, float inv, float steps, bool &near)
+// Code of x >= 0 under the block's scale, inv = 1 / scale: steps sqrt(x inv), to the nearest whole number, ties to even.
+__device__ __forceinline__ float code_of(float x, float inv, float steps)
 {
-    const float y = x * inv;
-    const float c = (EXACT ? sqrtf(y) : __builtin_amdgcn_sqrtf(y)) * steps;
-    if constexpr (!EXACT) near |= fabsf(__builtin_amdgcn_fractf(c) - 0.5f) < 1e-4f;   // 254 x 2^-22 is 0.6e-4
-    return x > 0.f ? fminf(rintf(c), steps) : 0.f;
+    return x > 0.f ? fminf(rintf(sqrtf(x * inv) * steps), steps) : 0.f;
+}
+// The same for a finite x and an inverse that did not overflow, with the hardware's square root, which is off by at most one unit
+// in the last place: `near` tells that the product may be that close to the middle between two codes (two in 10,000), so that the
+// code has to be taken again.
+__device__ __forceinline__ float code_fast(float x, float inv, float steps, bool &near)
+{
+    const float c = __builtin_amdgcn_sqrtf(x * inv) * steps, r = rintf(c);
+    near |= fabsf(c - r) > 0.5f - 1e-4f;   // 254 x 2^-22 is 0.6e-4
+    return r;
 }
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) <= kFltMax; }
 
@@ -136,26 +159,44 @@ template <int BITS> struct AdamwBlock {
             vs = t.v_scale[b];
         }
     }
-    template <bool EXACT> __device__ __forceinline__ bool encode(const float (&root)[4], float mi, float vi)
+    __device__ __forceinline__ bool encode_fast(const float (&root)[4], float mi, float vi)
     {
         bool near = false;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int a = (int)code_of<EXACT>(fabsf(m[j]), mi, 127.f, near);
-            const int r = (int)fmaxf(code_of<EXACT>(root[j], vi, 254.f, near), root[j] > 0.f ? 1.f : 0.f);
+            cm[j] = (uint8_t)(int)copysignf(code_fast(fabsf(m[j]), mi, 127.f, near), m[j]);
+            cv[j] = (uint8_t)(int)fmaxf(code_fast(root[j], vi, 254.f, near), root[j] > 0.f ? 1.f : 0.f);
+        }
+        return near;
+    }
+    // Any values: what is not finite gets its own code and has no part in the scale.
+    __device__ __forceinline__ void encode(const float (&root)[4])
+    {
+        ms = vs = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (finite(m[j])) ms = fmaxf(ms, fabsf(m[j]));
+            if (finite(root[j])) vs = fmaxf(vs, root[j]);
+        }
+        ms = wave_max(ms);
+        vs = wave_max(vs);
+        const float mi = ms > 0.f ? 1.f / ms : 0.f, vi = vs > 0.f ? 1.f / vs : 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int a = (int)code_of(fabsf(m[j]), mi, 127.f);
+            const int r = (int)fmaxf(code_of(root[j], vi, 254.f), root[j] > 0.f ? 1.f : 0.f);
             cm[j] = finite(m[j]) ? (uint8_t)(m[j] < 0.f ? -a : a) : (uint8_t)0x80;
             cv[j] = finite(root[j]) ? (uint8_t)r : (uint8_t)255;
         }
-        return near;
     }
     __device__ __forceinline__ void step(const AdamwItem &t, uint32_t b, int lane, const AdamwScalars &c)
     {
         const int64_t at = (int64_t)b * kBlock + lane * 4;
         const int n = (int)max((int64_t)0, min((int64_t)4, t.n - at));
         float root[4];
+        if constexpr (BITS == 8) decode4(cm, cv, ms, vs, m, v);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            if constexpr (BITS == 8) { m[j] = m_of((int8_t)cm[j], ms); v[j] = v_of(cv[j], vs); }
             const float gj = g[j] * c.grad_scale;
             m[j] = m[j] * c.beta1 + gj * c.one_beta1;
             v[j] = v[j] * c.beta2 + (gj * gj) * c.one_beta2;
@@ -168,16 +209,24 @@ template <int BITS> struct AdamwBlock {
             store4(t.m, VF_F32, at, n, m);
             store4(t.v, VF_F32, at, n, v);
         } else {
-            ms = vs = 0.f;
+            // as whole numbers, so that a NaN counts as the largest: blocks with one, or with a scale below the normal range (whose inverse
+            // may overflow), take the long way
+            uint32_t mb = 0, vb = 0;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                if (finite(m[j])) ms = fmaxf(ms, fabsf(m[j]));
-                if (finite(root[j])) vs = fmaxf(vs, root[j]);
+                mb = max(mb, __float_as_uint(m[j]) & 0x7FFFFFFFu);
+                vb = max(vb, __float_as_uint(root[j]));
             }
-            ms = wave_max(ms);
-            vs = wave_max(vs);
-            const float mi = ms > 0.f ? 1.f / ms : 0.f, vi = vs > 0.f ? 1.f / vs : 0.f;
-            if (__ballot(encode<false>(root, mi, vi))) encode<true>(root, mi, vi);
+            mb = wave_max(mb);
+            vb = wave_max(vb);
+            const uint32_t normal = 0x00800000u, infinite = 0x7F800000u;
+            if (mb - normal < infinite - normal && vb - normal < infinite - normal) {
+                ms = __uint_as_float(mb);
+                vs = __uint_as_float(vb);
+                if (__ballot(encode_fast(root, 1.f / ms, 1.f / vs))) encode(root);
+            } else {
+                encode(root);
+            }
             store4_codes(t.m, at, n, cm);
             store4_codes(t.v, at, n, cv);
             if (lane == 0) { t.m_scale[b] = ms; t.v_scale[b] = vs; }
@@ -233,18 +282,9 @@ template <int BITS> __global__ __launch_bounds__(256) void adamw_moments_kernel(
                 if (t.param) load4(t.v, VF_F32, at, n, v);
             } else {
                 uint8_t cm[4], cv[4];
-                if (t.master) {
-                    load4_codes(t.m, at, n, cm);
-                    const float ms = t.m_scale[b];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) m[j] = m_of((int8_t)cm[j], ms);
-                }
-                if (t.param) {
-                    load4_codes(t.v, at, n, cv);
-                    const float vs = t.v_scale[b];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) v[j] = v_of(cv[j], vs);
-                }
+                load4_codes(t.m, at, n, cm);
+                load4_codes(t.v, at, n, cv);
+                decode4(cm, cv, t.m_scale[b], t.v_scale[b], m, v);
             }
             if (t.master) store4(t.master, VF_F32, at, n, m);
             if (t.param) store4(t.param, VF_F32, at, n, v);
