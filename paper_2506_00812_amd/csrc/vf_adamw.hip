@@ -296,6 +296,7 @@ template <int BITS> __global__ __launch_bounds__(256) void adamw_moments_kernel(
 template <class Fill, class Launch>
 static int each_launch(const vf_adamw_tensor *tensors, int32_t n_tensors, Fill &&fill, Launch &&launch)
 {
+    bool launched = false;
     for (int bits : {32, 8}) {
         AdamwList l;
         l.n = 0;
@@ -310,10 +311,11 @@ static int each_launch(const vf_adamw_tensor *tensors, int32_t n_tensors, Fill &
             fill(i, l.item[l.n]);
             l.first[l.n + 1] = l.first[l.n] + (uint32_t)ceil_div(t.n, kBlock * (bits == 8 ? kUnit<8> : kUnit<32>));
             ++l.n;
+            launched = true;
         }
         if (l.n > 0) launch(l, bits);
     }
-    VF_HIP(hipGetLastError());
+    if (launched) VF_HIP(hipGetLastError());
     return VF_OK;
 }
 
