@@ -386,10 +386,10 @@ template <class T, bool ALONG_C, int ROWS> __device__ __forceinline__ uint32_t d
     }
 }
 
-// Sixteen bytes a lane from base + offset to LDS at `to` + 16 lane.
+// Sixteen bytes a lane from base + offset to LDS at `to` + 16 lane.  (A load to LDS may read m0 one wait state after its write at the earliest.)
 __device__ __forceinline__ void request(const void *base, uint32_t offset, uint32_t to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory", "m0");
 }
 
 template <class T, bool ALONG_C, int ROWS> __device__ __forceinline__ Vec<T> direct_fragment(const unsigned char *tile, int r0, int lane)
@@ -430,13 +430,15 @@ __global__ __launch_bounds__(WP *WQ * 64, 2) void direct_kernel(Product<T> a, Ep
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)tiles;
     const uint32_t lds_p = lds0 + wave * (LP * 1024), lds_q = lds0 + BP * 64 + wave * (LQ * 1024);
     auto buffer_of = [](int t) { return (STEPS & (STEPS - 1)) == 0 ? t & (STEPS - 1) : t % STEPS; };
-    auto request_step = [&](int t) {
+    auto request_some = [&](int t, int first, int last) {   // loads first .. last - 1 of a step's
         const uint32_t at = buffer_of(t) * kStep;
         const T *p = P + t * step_p, *q = Q + t * step_q;
 #pragma unroll
-        for (int i = 0; i < LP; ++i) request(p, off_p[i], lds_p + at + i * 1024);
-#pragma unroll
-        for (int i = 0; i < LQ; ++i) request(q, off_q[i], lds_q + at + i * 1024);
+        for (int i = 0; i < LOADS; ++i) {
+            if (i < first || i >= last) continue;
+            if (i < LP) request(p, off_p[i], lds_p + at + i * 1024);
+            else request(q, off_q[i - LP], lds_q + at + (i - LP) * 1024);
+        }
     };
     const int wp = wave % WP * (FP * 16), wq = wave / WP * (FQ * 16);
     float4v acc[FP][FQ] = {};
@@ -455,26 +457,41 @@ __global__ __launch_bounds__(WP *WQ * 64, 2) void direct_kernel(Product<T> a, Ep
             for (int j = 0; j < FQ; ++j) acc[i][j] = mma(p[i], q[j], acc[i][j]);
     };
     if (steps > 0) {
-        for (int t = 0; t < min(steps, STEPS); ++t) request_step(t);
+        for (int t = 0; t < min(steps, STEPS); ++t) request_some(t, 0, LOADS);
         if (steps >= STEPS) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STEPS - 1) * LOADS) : "memory");
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         asm volatile("s_barrier" ::: "memory");
         read_step(0, fp[0], fq[0]);
     }
-    // MORE: step t + STEPS exists
+    // A step in four parts, each with a quarter of its matrix instructions and between them a quarter of the next step's reads and of the
+    // requests.  (Requests in one go at its start held the waves up until the last of them had been taken, 16 cycles each.)
+    // MORE: step t + STEPS exists.
     auto one_step = [&](auto more, int t, int set) {
+        constexpr int kParts = 4, kFragments = FP + FQ, kRows = FP / kParts;
         __builtin_amdgcn_sched_barrier(0);
         if (more.value || t + STEPS - 1 < steps) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((STEPS - 2) * LOADS) : "memory");
         else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        __builtin_amdgcn_sched_barrier(0);
-        if (more.value || t + STEPS < steps) request_step(t + STEPS);
-        read_step(t + 1, fp[set ^ 1], fq[set ^ 1]);   // (beyond the last step: a buffer's old contents, not used)
-        multiply(fp[set], fq[set]);
-        constexpr int kReads = FP * (PC ? 1 : 2) + FQ * (QC ? 1 : 2);
+        const bool request_more = more.value || t + STEPS < steps;
+        const unsigned char *at = tiles + buffer_of(t + 1) * kStep;   // (beyond the last step: a buffer's old contents, not used)
 #pragma unroll
-        for (int i = 0; i < kReads; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);   // one LDS read
-            __builtin_amdgcn_sched_group_barrier(0x008, FP * FQ / kReads, 0);   // ... between the matrix instructions
+        for (int g = 0; g < kParts; ++g) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (request_more) request_some(t + STEPS, g * LOADS / kParts, (g + 1) * LOADS / kParts);
+            constexpr int kReads = (kFragments * 2 + kParts - 1) / kParts;
+#pragma unroll
+            for (int f = g * kFragments / kParts; f < (g + 1) * kFragments / kParts; ++f) {
+                if (f < FQ) fq[set ^ 1][f] = direct_fragment<T, QC, BQ>(at + BP * 64, wq + f * 16, lane);
+                else fp[set ^ 1][f - FQ] = direct_fragment<T, PC, BP>(at, wp + (f - FQ) * 16, lane);
+            }
+#pragma unroll
+            for (int i = g * kRows; i < (g + 1) * kRows; ++i)
+#pragma unroll
+                for (int j = 0; j < FQ; ++j) acc[i][j] = mma(fp[set][i], fq[set][j], acc[i][j]);
+#pragma unroll
+            for (int u = 0; u < kReads; ++u) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);   // a matrix instruction,
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);   // an LDS read
+            }
         }
     };
     int t = 0;
@@ -584,8 +601,8 @@ enum Tiling {
 };
 
 // What a tiling costs, in microseconds: `step` per 128 bytes of the contraction with a compute unit full of `together` workgroups, at
-// least `alone` however few there are; `fixed` per workgroup for its first loads and its stores.  Fitted to 1,600 timings: 33 sizes
-// from 32 x 1,024 x 1,024 to 10,000 x 4,096 x 1,024, each product, every tiling and 1 to 32 splits; the model is within 10 % of half
+// least `alone` however few there are; `fixed` per workgroup for its first loads and its stores.  Fitted to 2,000 timings: 40 sizes
+// from 32 x 1,024 x 1,024 to 10,000 x 4,096 x 1,024, each product, every tiling and 1 to 32 splits; the model is within 15 % of half
 // of them, and what it picks takes 5 % longer than the best of all on average.
 struct TilingCost {
     int bp, bq, together;
@@ -595,14 +612,14 @@ static TilingCost cost_of(Tiling t, bool f32, bool both_along)
 {
     switch (t) {
     case kSmall:
-        return f32 ? (both_along ? TilingCost{64, 64, 4, 2.2, 0.74, 4.5} : TilingCost{64, 64, 4, 2.4, 0.89, 4.2})
-                   : (both_along ? TilingCost{64, 64, 4, 0.9, 0.40, 4.0} : TilingCost{64, 64, 4, 0.9, 0.68, 3.3});
+        return f32 ? (both_along ? TilingCost{64, 64, 4, 2.2, 0.77, 3.9} : TilingCost{64, 64, 4, 2.3, 0.90, 3.9})
+                   : (both_along ? TilingCost{64, 64, 4, 0.86, 0.46, 3.4} : TilingCost{64, 64, 4, 0.95, 0.67, 3.5});
     case kMedium:
-        return f32 ? TilingCost{128, 128, 2, 3.2, 2.1, 4.5}
-                   : (both_along ? TilingCost{128, 128, 2, 0.8, 0.80, 4.3} : TilingCost{128, 128, 2, 0.7, 0.90, 4.2});
-    case kDirect128: return both_along ? TilingCost{128, 128, 3, 1.25, 0.46, 4.7} : TilingCost{128, 128, 3, 1.0, 0.54, 5.0};
-    case kDirectWide: return TilingCost{128, 256, 2, 1.38, 0.77, 5.9};
-    default: return TilingCost{256, 256, 1, 1.13, 0.61, 6.9};
+        return f32 ? TilingCost{128, 128, 2, 3.2, 2.1, 4.6}
+                   : (both_along ? TilingCost{128, 128, 2, 1.0, 0.85, 3.6} : TilingCost{128, 128, 2, 1.3, 0.95, 4.0});
+    case kDirect128: return both_along ? TilingCost{128, 128, 3, 1.43, 0.46, 4.2} : TilingCost{128, 128, 3, 1.35, 0.68, 4.6};
+    case kDirectWide: return TilingCost{128, 256, 2, 1.4, 0.74, 5.6};
+    default: return both_along ? TilingCost{256, 256, 1, 1.13, 0.61, 6.0} : TilingCost{256, 256, 1, 1.2, 0.61, 6.4};
     }
 }
 // The few rows' kernel reads P's 16 rows and all of Q's per workgroup, two workgroups per compute unit.
@@ -652,7 +669,7 @@ static ProductPlan plan_product(int32_t dtype, int64_t np, int64_t nq, int64_t n
             const double steps = (double)ceil_div(chunk, step);
             const double last = (double)(per_cu - (rounds - 1) * c.together) / c.together;   // how full the last round is
             double us = (double)(rounds - 1) * (steps * c.step + c.fixed) + steps * std::max(c.alone, c.step * last) + c.fixed;
-            if (used > 1) us += 3 + (double)used * np * nq * 8 / 4e6;
+            if (used > 1) us += 4 + (double)used * np * nq * 8 / 4e6;
             if (least == 0 || us < least) {
                 least = us;
                 best.tiling = t;
