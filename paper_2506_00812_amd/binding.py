@@ -24,7 +24,7 @@ EXPORTED_SYMBOLS = ("vf_build_index", "vf_search", "vf_search_exact", "vf_index_
                     "vf_index_free", "vf_last_error", "vf_profile_enable", "vf_profile_read", "vf_search_multi",
                     "vf_build_index_opt", "vf_tune", "vf_debug_route", "vf_search_noalloc", "vf_serve_begin", "vf_serve_submit",
                     "vf_serve_poll", "vf_serve_end", "vf_serve_run", "vf_search_ex",
-                    "vf_linear", "vf_linear_backward", "vf_linear_workspace", "vf_layer_norm", "vf_layer_norm_backward",
+                    "vf_linear", "vf_linear_backward", "vf_linear_workspace", "vf_debug_linear", "vf_layer_norm", "vf_layer_norm_backward",
                     "vf_layer_norm_workspace", "vf_log_probs", "vf_log_probs_backward", "vf_log_probs_workspace",
                     "vf_adamw_step", "vf_adamw_moments")
 
@@ -134,6 +134,7 @@ def load_library():
                 vf_linear=[i32, i64, i64, i64, p, i64, p, i64, p, i32, p, i64, p, i64, p, i64, p, sz, p],
                 vf_linear_backward=[i32, i64, i64, i64, p, i64, p, i64, p, i64, p, i64, i32, p, i64, p, i64, p, p, sz, p],
                 vf_linear_workspace=[i32, i64, i64, i64, i32, i32, C.POINTER(sz)],
+                vf_debug_linear=[i32, i64, i64, i64, i32, i32, C.POINTER(i32), C.POINTER(i32)],
                 vf_layer_norm=[i32, i64, i64, p, i64, p, p, C.c_double, p, i64, p, p, p],
                 vf_layer_norm_backward=[i32, i64, i64, p, i64, p, i64, p, p, p, p, i64, p, p, p, sz, p],
                 vf_layer_norm_workspace=[i32, i64, i64, C.POINTER(sz)],
@@ -641,6 +642,13 @@ def linear_backward(dy, x, weight, z=None, activation="none", bias=True, dx=True
                                 z.data_ptr() if act else None, ldz, act, gx.data_ptr() if dx else None, k,
                                 gw.data_ptr() if dweight else None, k, gb.data_ptr() if bias else None, pw, nw, handle))
     return gx, gw, gb
+
+
+def debug_linear(dtype, m, n, k, product=0, direct=True):
+    """(tiling, splits) of a product of the linear layer (vf_debug_linear); dtype: VF_F32, VF_BF16 or VF_F16."""
+    tiling, splits = C.c_int32(), C.c_int32()
+    _check(load_library().vf_debug_linear(dtype, m, n, k, product, int(direct), C.byref(tiling), C.byref(splits)))
+    return tiling.value, splits.value
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5, save=False, out=None, stream=None):

@@ -262,6 +262,12 @@ extern "C" int vf_linear_workspace(int32_t dtype, int64_t m, int64_t n, int64_t 
     return guarded([&] { return linear_workspace_impl(dtype, m, n, k, activation, backward, bytes); });
 }
 
+extern "C" int vf_debug_linear(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t product, int32_t direct, int32_t *tiling,
+                               int32_t *splits)
+{
+    return guarded([&] { return debug_linear_impl(dtype, m, n, k, product, direct, tiling, splits); });
+}
+
 extern "C" int vf_layer_norm(int32_t dtype, int64_t m, int64_t d, const void *x, int64_t ldx, const void *weight,
                              const void *bias, double eps, void *y, int64_t ldy, float *mean, float *rstd, void *hip_stream)
 {

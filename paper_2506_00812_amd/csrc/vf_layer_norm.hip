@@ -369,8 +369,7 @@ int layer_norm_backward_impl(const NormArgs &a)
     const bool sums = a.dweight != nullptr || a.dbias != nullptr;
     const int64_t parts = parts_of(a.dtype, a.m, a.d);
     const size_t need = sums ? (size_t)parts * 2 * (size_t)a.d * 4 : 0;
-    VF_REQUIRE(need == 0 || (a.workspace != nullptr && a.workspace_bytes >= need),
-               "layer norm: the workspace must hold " + std::to_string(need) + " bytes");
+    if (int rc = check_workspace("layer norm", a.workspace, a.workspace_bytes, need); rc != VF_OK) return rc;
     float *part = (float *)a.workspace;
     by_type(a.dtype, [&](auto *p) {
         using T = std::remove_pointer_t<decltype(p)>;

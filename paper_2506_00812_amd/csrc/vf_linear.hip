@@ -6,6 +6,8 @@
 //     dx        P = w  (along rows),   Q = dz (along c),     c = n
 //     dw        P = x  (along rows),   Q = dz (along rows),  c = m
 // P takes the matrix instruction's first operand, so that a lane's four accumulators are neighbours in a row of the output.
+#include <atomic>
+
 #include "vf_device.h"
 #include "vf_ops.h"
 
@@ -603,7 +605,7 @@ enum Tiling {
 // What a tiling costs, in microseconds: `step` per 128 bytes of the contraction with a compute unit full of `together` workgroups, at
 // least `alone` however few there are; `fixed` per workgroup for its first loads and its stores.  Fitted to 2,000 timings: 40 sizes
 // from 32 x 1,024 x 1,024 to 10,000 x 4,096 x 1,024, each product, every tiling and 1 to 32 splits; the model is within 15 % of half
-// of them, and what it picks takes 5 % longer than the best of all on average.
+// of them, and what it picks takes 4 % longer than the best of all on average.
 struct TilingCost {
     int bp, bq, together;
     double step, alone, fixed;
@@ -682,9 +684,15 @@ static ProductPlan plan_product(int32_t dtype, int64_t np, int64_t nq, int64_t n
     return best;
 }
 
-template <class K> static int allow_lds(K kernel, size_t bytes)
+// More than 64 KiB of LDS has to be allowed once per kernel and device.  (`done`: the devices where it has been; asking again does no harm.)
+static int allow_lds(const void *kernel, size_t bytes, std::atomic<uint64_t> &done)
 {
-    if (bytes > 64 * 1024) VF_HIP(hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    int dev = 0;
+    VF_HIP(hipGetDevice(&dev));
+    const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+    if (bit && (done.load(std::memory_order_relaxed) & bit)) return VF_OK;
+    VF_HIP(hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    done.fetch_or(bit, std::memory_order_relaxed);
     return VF_OK;
 }
 
@@ -692,7 +700,9 @@ template <class T, bool PC, bool QC, int BP, int BQ, int WP, int WQ, int STEPS>
 static int launch_direct(const Product<T> &a, const Epilogue<T> &e, dim3 grid, hipStream_t s)
 {
     constexpr size_t lds = (size_t)STEPS * (BP + BQ) * 64;
-    if (int rc = allow_lds(direct_kernel<T, PC, QC, BP, BQ, WP, WQ, STEPS>, lds); rc != VF_OK) return rc;
+    static std::atomic<uint64_t> done{0};
+    if constexpr (lds > 64 * 1024)
+        if (int rc = allow_lds((const void *)direct_kernel<T, PC, QC, BP, BQ, WP, WQ, STEPS>, lds, done); rc != VF_OK) return rc;
     direct_kernel<T, PC, QC, BP, BQ, WP, WQ, STEPS><<<grid, dim3(WP * WQ * 64), lds, s>>>(a, e);
     return VF_OK;
 }
@@ -723,8 +733,8 @@ static int run_product(int32_t dtype, const T *P, int64_t ldp, int64_t np, const
     if (plan.tiling == kSmall) {
         tile_kernel<T, PC, QC, 64, 64, 2, 2><<<grid, dim3(256), (size_t)2 * 128 * kRowBytes, s>>>(a, e);
     } else if (plan.tiling == kMedium) {
-        constexpr size_t lds = (size_t)2 * 256 * kRowBytes;
-        if ((rc = allow_lds(tile_kernel<T, PC, QC, 128, 128, 2, 4>, lds)) != VF_OK) return rc;
+        constexpr size_t lds = (size_t)2 * 256 * kRowBytes;   // 64 KiB, which need not be asked for
+        static_assert(lds <= 64 * 1024, "");
         tile_kernel<T, PC, QC, 128, 128, 2, 4><<<grid, dim3(512), lds, s>>>(a, e);
     } else if constexpr (sizeof(T) == 2) {
         if (plan.tiling == kDirect256) rc = launch_direct<T, PC, QC, 256, 256, 2, 4, 4>(a, e, grid, s);
@@ -798,8 +808,7 @@ int linear_impl(const LinearArgs &a)
     VF_REQUIRE(a.ldx >= a.k && a.ldw >= a.k, "linear: ldx or ldw is less than k");
     VF_REQUIRE(a.ldy >= a.n && (!a.z || a.ldz >= a.n) && (!a.residual || a.ldr >= a.n), "linear: ldy, ldz or ldr is less than n");
     const ProductPlan plan = plan_product(a.dtype, a.n, a.m, a.k, {true, true, direct_rows(a.dtype, a.x, a.ldx) && direct_rows(a.dtype, a.w, a.ldw)});
-    VF_REQUIRE(plan.bytes == 0 || (a.workspace != nullptr && a.workspace_bytes >= plan.bytes),
-               "linear: the workspace must hold " + std::to_string(plan.bytes) + " bytes");
+    if (int rc = check_workspace("linear", a.workspace, a.workspace_bytes, plan.bytes); rc != VF_OK) return rc;
     int rc = VF_OK;
     by_type(a.dtype, [&](auto *t) {
         using T = std::remove_pointer_t<decltype(t)>;
@@ -820,8 +829,7 @@ int linear_backward_impl(const LinearArgs &a)
     VF_REQUIRE(!a.dx || ((a.w || !rows || a.k == 0) && a.ldw >= a.k && a.lddx >= a.k), "linear: dx needs w, and ldw and lddx of at least k");
     VF_REQUIRE(!a.dw || ((a.x || !rows || a.k == 0) && a.ldx >= a.k && a.lddw >= a.k), "linear: dw needs x, and ldx and lddw of at least k");
     const BackwardPlan b = plan_backward(a.dtype, a.m, a.n, a.k, a.act);
-    VF_REQUIRE(b.total() == 0 || (a.workspace != nullptr && a.workspace_bytes >= b.total()),
-               "linear: the workspace must hold " + std::to_string(b.total()) + " bytes");
+    if (int rc = check_workspace("linear", a.workspace, a.workspace_bytes, b.total()); rc != VF_OK) return rc;
     int rc = VF_OK;
     by_type(a.dtype, [&](auto *t) {
         using T = std::remove_pointer_t<decltype(t)>;
@@ -856,6 +864,17 @@ int linear_backward_impl(const LinearArgs &a)
     });
     if (rc == VF_OK) VF_HIP(hipGetLastError());
     return rc;
+}
+
+int debug_linear_impl(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t product, int32_t direct, int32_t *tiling, int32_t *splits)
+{
+    if (int rc = check_sizes(dtype, m, n, k, VF_ACT_NONE); rc != VF_OK) return rc;
+    VF_REQUIRE(product >= 0 && product <= 2 && tiling && splits, "linear: product must be 0 .. 2, tiling and splits not NULL");
+    const Operands o{product == 0, product <= 1, direct != 0 && dtype != VF_F32};
+    const ProductPlan p = product == 0 ? plan_product(dtype, n, m, k, o) : product == 1 ? plan_product(dtype, k, m, n, o) : plan_product(dtype, k, n, m, o);
+    *tiling = p.tiling;
+    *splits = p.splits;
+    return VF_OK;
 }
 
 }  // namespace vf

@@ -229,11 +229,11 @@ __global__ __launch_bounds__(64) void log_probs_join_kernel(int64_t m, int64_t v
         r = wave_join(r);
         WaveTop best;
         const int n = nseg * top;
-        for (int i = 0; i < n; i += 64) {
-            const uint64_t key = i + lane < n ? part_keys[row * n + i + lane] : 0;
-            if (i == 0) best.expect((uint32_t)(key >> 32), top);
-            best.offer(true, key, top);
-        }
+        const uint64_t *keys = part_keys + row * n;
+        uint32_t most = 0;
+        for (int i = lane; i < n; i += 64) most = max(most, (uint32_t)(keys[i] >> 32));
+        if (top) best.expect(most, top);
+        for (int i = 0; i < n; i += 64) best.offer(i + lane < n, i + lane < n ? keys[i + lane] : 0, top);
         finish_row(out, logits + row * ld, row, v, top, r, best.key);
     }
 }
@@ -313,8 +313,7 @@ int log_probs_impl(const LogProbArgs &a)
     VF_REQUIRE(a.m == 0 || a.logits != nullptr, "log probs: logits is NULL");
     VF_REQUIRE(a.targets == nullptr || a.logp != nullptr || a.m == 0, "log probs: targets without logp");
     VF_REQUIRE(a.top == 0 || a.m == 0 || (a.top_ids && a.top_logp), "log probs: top_ids or top_logp is NULL");
-    VF_REQUIRE(need == 0 || (a.workspace != nullptr && a.workspace_bytes >= need),
-               "log probs: the workspace must hold " + std::to_string(need) + " bytes");
+    if (int rc = check_workspace("log probs", a.workspace, a.workspace_bytes, need); rc != VF_OK) return rc;
     if (a.m == 0) return VF_OK;
     const LogProbPlan p = plan_of(a.m, a.v);
     const LogProbOut out{a.targets, a.logp, a.entropy, a.lse, a.top_ids, a.top_logp};

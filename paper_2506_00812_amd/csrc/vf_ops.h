@@ -31,6 +31,14 @@ inline size_t type_size(int32_t dtype) { return dtype == VF_F32 ? 4 : 2; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 constexpr int64_t kMaxExtent = INT32_MAX;
 
+inline int check_workspace(const char *op, const void *workspace, size_t have, size_t need)
+{
+    if (need == 0) return VF_OK;
+    VF_REQUIRE(workspace != nullptr && have >= need, std::string(op) + ": the workspace must hold " + std::to_string(need) + " bytes");
+    VF_REQUIRE(((uintptr_t)workspace & 15) == 0, std::string(op) + ": the workspace must be aligned to 16 bytes");
+    return VF_OK;
+}
+
 // A vector at an address that is aligned to an element only: one 16-byte load or store all the same (global memory
 // takes any alignment; rows cut out of a wider matrix start anywhere).
 template <class V, class T> __device__ __forceinline__ V load_vec(const T *p)
@@ -197,6 +205,7 @@ struct LinearArgs {
 };
 int linear_impl(const LinearArgs &a);
 int linear_backward_impl(const LinearArgs &a);
+int debug_linear_impl(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t product, int32_t direct, int32_t *tiling, int32_t *splits);
 int linear_workspace_impl(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t act, int32_t backward, size_t *bytes);
 
 struct NormArgs {
