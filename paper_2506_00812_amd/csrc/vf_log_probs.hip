@@ -91,9 +91,21 @@ struct LogProbOut {
     float *top_logp;
 };
 
+// The label that a row is asked about and its logit, loaded before the sums are known (two loads, one after the other).
+template <class T> struct Asked {
+    int32_t t = -1;
+    float x = 0.f;
+    __device__ __forceinline__ void load(const LogProbOut &o, const T *row_x, int64_t row, int64_t v)
+    {
+        if (!o.targets) return;
+        t = o.targets[row];
+        if (t >= 0 && t < v) x = (float)row_x[t];
+    }
+};
+
 // What a row's sums and keys say, written by one wave.
 template <class T>
-__device__ __forceinline__ void finish_row(const LogProbOut &o, const T *x, int64_t row, int64_t v, int top, const RowSums &r, uint64_t key)
+__device__ __forceinline__ void finish_row(const LogProbOut &o, const Asked<T> &asked, int64_t row, int64_t v, int top, const RowSums &r, uint64_t key)
 {
     const int lane = threadIdx.x & 63;
     const bool empty = r.m == -kInf && r.s == 0.f;
@@ -102,11 +114,10 @@ __device__ __forceinline__ void finish_row(const LogProbOut &o, const T *x, int6
         if (o.lse) o.lse[row] = empty ? -kInf : r.m + log_s;
         if (o.entropy) o.entropy[row] = empty ? 0.f : log_s - r.a / r.s;
         if (o.targets) {
-            const int32_t t = o.targets[row];
             float l = 0.f;
-            if (t != -1) {
-                if (t < 0 || t >= v) l = __uint_as_float(0x7FC00000u);
-                else l = empty ? -kInf : ((float)x[t] - r.m) - log_s;
+            if (asked.t != -1) {
+                if (asked.t < 0 || asked.t >= v) l = __uint_as_float(0x7FC00000u);
+                else l = empty ? -kInf : (asked.x - r.m) - log_s;
             }
             o.logp[row] = l;
         }
@@ -135,6 +146,8 @@ __global__ __launch_bounds__(256) void log_probs_kernel(int64_t m, int64_t v, co
         const int64_t c0 = sg * seg, c1 = min(v, c0 + seg);
         RowSums r = {-kInf, 0.f, 0.f};
         WaveTop best;
+        Asked<T> asked;
+        if (nseg == 1) asked.load(out, x, row, v);
         for (int64_t base = c0; base < c1; base += TPR * E) {
             float u[E];
 #pragma unroll
@@ -147,26 +160,26 @@ __global__ __launch_bounds__(256) void log_probs_kernel(int64_t m, int64_t v, co
                 for (int j = 0; j < V; ++j) u[i * V + j] = (float)raw[j];
             }
             float most = u[0];
-            bool odd = false;   // a NaN, which the maximum passes over
 #pragma unroll
-            for (int j = 0; j < E; ++j) { most = fmaxf(most, u[j]); odd |= u[j] != u[j]; }
+            for (int j = 1; j < E; ++j) most = fmaxf(most, u[j]);
             if (most > r.m) scale_to(r, most);
             const float origin = r.m == -kInf ? 0.f : r.m;
 #pragma unroll
             for (int j = 0; j < E; ++j) {
+                // (the distance of a masked entry is -inf and its term 0; a NaN, which the maximum passes over, stays in s)
                 const float d = u[j] - origin, e = exp_fast(d);
                 r.s += e;
-                r.a += e > 0.f ? e * d : 0.f;
+                r.a = __builtin_fmaf(e, fmaxf(d, -kFltMax), r.a);
             }
             if constexpr (TOP) {
                 if (base == c0) best.expect(most > -kInf ? value_order(most) : 0, top);
                 const float least = best.least >> 32 ? order_value((uint32_t)(best.least >> 32)) : -kInf;
-                const bool any_odd = __ballot(odd) != 0;
+                const bool any_odd = __ballot(r.s != r.s) != 0;   // NaN or +inf among the values
                 if (__ballot(most >= least) || any_odd) {
 #pragma unroll
                     for (int j = 0; j < E; ++j) {
                         // what cannot reach the list is told by its value; NaN by its order
-                        if (!any_odd && !__ballot(u[j] >= least && u[j] > -kInf)) continue;
+                        if (!any_odd && !__ballot(u[j] >= least)) continue;
                         const uint32_t at = (uint32_t)(base + (j / V * TPR + t) * V + j % V);
                         best.offer(u[j] != -kInf, (uint64_t)value_order(u[j]) << 32 | (uint32_t)~at, top);
                     }
@@ -199,7 +212,7 @@ __global__ __launch_bounds__(256) void log_probs_kernel(int64_t m, int64_t v, co
         }
         if (W == 1 || wave == 0) {
             if (nseg == 1) {
-                finish_row(out, x, row, v, TOP ? top : 0, r, best.key);
+                finish_row(out, asked, row, v, TOP ? top : 0, r, best.key);
             } else {
                 if (lane == 0) part_sums[item] = make_float4(r.m, r.s, r.a, 0.f);
                 if (TOP && lane < top) part_keys[item * top + lane] = best.key;
@@ -217,6 +230,12 @@ __global__ __launch_bounds__(64) void log_probs_join_kernel(int64_t m, int64_t v
     const int lane = threadIdx.x;
     for (int64_t row = blockIdx.x; row < m; row += gridDim.x) {
         RowSums r = {-kInf, 0.f, 0.f};
+        Asked<T> asked;
+        asked.load(out, logits + row * ld, row, v);
+        const int n = nseg * top;
+        const uint64_t *keys = part_keys + row * n;
+        uint32_t most_key = 0;
+        for (int i = lane; i < n; i += 64) most_key = max(most_key, (uint32_t)(keys[i] >> 32));
         for (int i = lane; i < nseg; i += 64) {
             const float4 p = part_sums[row * nseg + i];
             RowSums q = {p.x, p.y, p.z};
@@ -228,13 +247,9 @@ __global__ __launch_bounds__(64) void log_probs_join_kernel(int64_t m, int64_t v
         }
         r = wave_join(r);
         WaveTop best;
-        const int n = nseg * top;
-        const uint64_t *keys = part_keys + row * n;
-        uint32_t most = 0;
-        for (int i = lane; i < n; i += 64) most = max(most, (uint32_t)(keys[i] >> 32));
-        if (top) best.expect(most, top);
+        if (top) best.expect(most_key, top);
         for (int i = 0; i < n; i += 64) best.offer(i + lane < n, i + lane < n ? keys[i + lane] : 0, top);
-        finish_row(out, logits + row * ld, row, v, top, r, best.key);
+        finish_row(out, asked, row, v, top, r, best.key);
     }
 }
 
