@@ -3,6 +3,7 @@
 // of two terms that are not negative).  A changed maximum turns (S, A) into f S and f (A + (m - m') S) with f = exp(m - m').
 // Bound by memory where there are many rows.  A row is one wave's, one workgroup's, or (few rows) split into segments whose
 // (m, S, A, largest) a second kernel joins.
+#include "vf_device.h"
 #include "vf_ops.h"
 
 namespace vf {
@@ -137,8 +138,9 @@ __global__ __launch_bounds__(256) void log_probs_kernel(int64_t m, int64_t v, co
 {
     constexpr int V = kVec<T>, RPB = 256 / TPR, W = TPR / 64, E = 16, NV = E / V;
     __shared__ float lds_sums[4][3];
-    __shared__ uint64_t lds_keys[TOP && W > 1 ? 4 * 64 : 1];
+    __shared__ uint64_t lds_keys[TOP && W > 1 ? 4 * 64 : 1], lds_chosen[TOP ? 4 * 128 : 1];
     const int t = threadIdx.x % TPR, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint64_t *chosen = lds_chosen + (TOP ? wave * 128 : 0);
     const int64_t items = m * nseg;
     for (int64_t item = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR; item < items; item += (int64_t)gridDim.x * RPB) {
         const int64_t row = nseg == 1 ? item : item / nseg, sg = nseg == 1 ? 0 : item - row * nseg;
@@ -173,17 +175,31 @@ __global__ __launch_bounds__(256) void log_probs_kernel(int64_t m, int64_t v, co
             }
             if constexpr (TOP) {
                 if (base == c0) best.expect(most > -kInf ? value_order(most) : 0, top);
-                const float least = best.least >> 32 ? order_value((uint32_t)(best.least >> 32)) : -kInf;
-                const bool any_odd = __ballot(r.s != r.s) != 0;   // NaN or +inf among the values
-                if (__ballot(most >= least) || any_odd) {
+                // what may reach the list is told by its value (NaN is not less than anything), gathered in LDS and offered together
+                const uint32_t bound = (uint32_t)(best.least >> 32);
+                const float least = bound ? fmaxf(order_value(bound), -kFltMax) : -kFltMax;
+                int found = 0;
 #pragma unroll
-                    for (int j = 0; j < E; ++j) {
-                        // what cannot reach the list is told by its value; NaN by its order
-                        if (!any_odd && !__ballot(u[j] >= least)) continue;
-                        const uint32_t at = (uint32_t)(base + (j / V * TPR + t) * V + j % V);
-                        best.offer(u[j] != -kInf, (uint64_t)value_order(u[j]) << 32 | (uint32_t)~at, top);
+                for (int j = 0; j < E; ++j) {
+                    const bool in = !(u[j] < least);
+                    const uint64_t mask = __ballot(in);
+                    if (mask == 0) continue;
+                    const uint32_t at = (uint32_t)(base + (j / V * TPR + t) * V + j % V);
+                    if (in) chosen[found + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0))] =
+                        (uint64_t)value_order(u[j]) << 32 | (uint32_t)~at;
+                    found += __popcll(mask);
+                    if (found >= 64) {   // (the bound stays that of the batch's start; the list's own is exact)
+                        wave_sync<true>();
+                        best.offer(true, chosen[lane], top);
+                        found -= 64;
+                        const uint64_t rest = chosen[64 + lane];
+                        wave_sync<true>();
+                        chosen[lane] = rest;
                     }
                 }
+                wave_sync<true>();
+                best.offer(lane < found, chosen[lane], top);
+                wave_sync<true>();
             }
         }
         r = wave_join(r);
