@@ -10,14 +10,15 @@ namespace vf {
 
 constexpr float kInf = __builtin_inff();
 
-// Orders values as whole numbers: NaN > +inf > ... > -inf, -0 = +0; with the complement of the label below it, a key orders
-// alternatives (larger first, ties to the lower label).  0: none.
+// Orders values as whole numbers: NaN > +inf > ... > -inf, -0 = +0.  Its complement with the label below it is a key that orders
+// alternatives ascending (larger values first, ties to the lower label).
 __device__ __forceinline__ uint32_t value_order(float x)
 {
     if (x != x) return ~0u;
     const uint32_t u = __float_as_uint(x + 0.f);
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
+__device__ __forceinline__ uint64_t key_of(float x, uint32_t label) { return (uint64_t)~value_order(x) << 32 | label; }
 __device__ __forceinline__ float order_value(uint32_t o)
 {
     return __uint_as_float(o == ~0u ? 0x7FC00000u : o & 0x80000000u ? o & 0x7FFFFFFFu : ~o);
@@ -46,42 +47,48 @@ __device__ __forceinline__ RowSums wave_join(RowSums r)
     return r;
 }
 
-// The largest keys of a wave: lane i holds the i-th largest of what was offered (all 64 are kept, `top` are asked for).  `least`: no
-// key up to it can be among the first `top`.
+// The largest keys of a wave, kept as their complements in ascending order: lane i holds the i-th of what was offered (all 64 are kept,
+// `top` are asked for).  `bound`: no complement from it on can be among the first `top`.
 struct WaveTop {
-    uint64_t key = 0, least = 0;
+    uint64_t key = KEY_MAX, bound = KEY_MAX;
     static __device__ __forceinline__ uint64_t of_lane(uint64_t k, int lane)
     {
         return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), lane) << 32 |
                (uint32_t)__builtin_amdgcn_readlane((int)k, lane);
     }
     // Before the first offers: of 64 candidates with the value orders o (0: none) at least `top` reach the threshold found here, to 16
-    // bits, so that the first thousand entries of a row cost some `top` insertions and not top (1 + log(1000 / top)).
+    // bits, so that the first thousand entries of a row have some `top` that are looked at and not top (1 + log(1000 / top)).
     __device__ __forceinline__ void expect(uint32_t o, int top)
     {
         uint32_t t = 0;
 #pragma unroll 1
         for (uint32_t bit = 1u << 31; bit >= 1u << 16; bit >>= 1)
             if (__popcll(__ballot(o >= (t | bit))) >= top) t |= bit;
-        if (t) least = ((uint64_t)t << 32) - 1;
+        if (t) bound = (uint64_t)(~t + 1) << 32;
     }
-    __device__ __forceinline__ void offer(bool mine, uint64_t k, int top)
+    // The least value order that may still be among the first `top`; 0: any.
+    __device__ __forceinline__ uint32_t least_order() const { return ~(uint32_t)((bound - 1) >> 32); }
+    // One key a lane (KEY_MAX: none).  A few are inserted one by one, some 130 cycles each; more are sorted and merged with the list, some
+    // 1,000 cycles however many (10,000 rows of 1,000, 32 alternatives: 24 us, 33 with insertions alone).
+    __device__ __forceinline__ void offer(uint64_t k, int top)
     {
         const int lane = threadIdx.x & 63;
-        uint64_t mask = __ballot(mine && k > least);
-        while (mask) {
-            const int from = __builtin_ctzll(mask);
-            mask &= mask - 1;
-            const uint64_t in = of_lane(k, from);
-            if (in <= least) continue;
-            const int at = __popcll(__ballot(key > in));
-            // (0x138: from the lane before, over all 64)
-            const uint32_t lo = (uint32_t)__builtin_amdgcn_mov_dpp((int)key, 0x138, 0xF, 0xF, true);
-            const uint32_t hi = (uint32_t)__builtin_amdgcn_mov_dpp((int)(key >> 32), 0x138, 0xF, 0xF, true);
-            key = lane < at ? key : lane == at ? in : (uint64_t)hi << 32 | lo;
-            const uint64_t last = of_lane(key, top - 1);
-            least = last > least ? last : least;
+        uint64_t mask = __ballot(k < bound);
+        if (mask == 0) return;
+        if (__popcll(mask) > 8) {
+            const uint64_t descending = ~wave_sort64(~(k < bound ? k : KEY_MAX), lane);
+            key = wave_merge64(key < descending ? key : descending, lane);
+        } else {
+            do {
+                const uint64_t in = of_lane(k, __builtin_ctzll(mask));
+                mask &= mask - 1;
+                const int at = __popcll(__ballot(key < in));
+                const uint64_t up = wave_shr1_64(key);
+                key = lane < at ? key : lane == at ? in : up;
+            } while (mask);
         }
+        const uint64_t last = of_lane(key, top - 1);
+        bound = last < bound ? last : bound;
     }
 };
 
@@ -124,8 +131,8 @@ __device__ __forceinline__ void finish_row(const LogProbOut &o, const Asked<T> &
         }
     }
     if (lane < top) {
-        o.top_ids[row * top + lane] = key ? (int32_t)~(uint32_t)key : -1;
-        o.top_logp[row * top + lane] = key ? (order_value((uint32_t)(key >> 32)) - r.m) - log_s : -kInf;
+        o.top_ids[row * top + lane] = key != KEY_MAX ? (int32_t)(uint32_t)key : -1;
+        o.top_logp[row * top + lane] = key != KEY_MAX ? (order_value(~(uint32_t)(key >> 32)) - r.m) - log_s : -kInf;
     }
 }
 
@@ -138,9 +145,9 @@ __global__ __launch_bounds__(256) void log_probs_kernel(int64_t m, int64_t v, co
 {
     constexpr int V = kVec<T>, RPB = 256 / TPR, W = TPR / 64, E = 16, NV = E / V;
     __shared__ float lds_sums[4][3];
-    __shared__ uint64_t lds_keys[TOP && W > 1 ? 4 * 64 : 1], lds_chosen[TOP ? 4 * 128 : 1];
+    __shared__ uint64_t lds_keys[TOP && W > 1 ? 4 * 64 : 1], lds_chosen[TOP ? 4 * 64 * E / 2 : 1];
     const int t = threadIdx.x % TPR, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    uint64_t *chosen = lds_chosen + (TOP ? wave * 128 : 0);
+    uint64_t *chosen = lds_chosen + (TOP ? wave * (64 * E / 2) : 0);
     const int64_t items = m * nseg;
     for (int64_t item = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR; item < items; item += (int64_t)gridDim.x * RPB) {
         const int64_t row = nseg == 1 ? item : item / nseg, sg = nseg == 1 ? 0 : item - row * nseg;
@@ -176,30 +183,25 @@ __global__ __launch_bounds__(256) void log_probs_kernel(int64_t m, int64_t v, co
             if constexpr (TOP) {
                 if (base == c0) best.expect(most > -kInf ? value_order(most) : 0, top);
                 // what may reach the list is told by its value (NaN is not less than anything), gathered in LDS and offered together
-                const uint32_t bound = (uint32_t)(best.least >> 32);
-                const float least = bound ? fmaxf(order_value(bound), -kFltMax) : -kFltMax;
-                int found = 0;
 #pragma unroll
-                for (int j = 0; j < E; ++j) {
-                    const bool in = !(u[j] < least);
-                    const uint64_t mask = __ballot(in);
-                    if (mask == 0) continue;
-                    const uint32_t at = (uint32_t)(base + (j / V * TPR + t) * V + j % V);
-                    if (in) chosen[found + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0))] =
-                        (uint64_t)value_order(u[j]) << 32 | (uint32_t)~at;
-                    found += __popcll(mask);
-                    if (found >= 64) {   // (the bound stays that of the batch's start; the list's own is exact)
-                        wave_sync<true>();
-                        best.offer(true, chosen[lane], top);
-                        found -= 64;
-                        const uint64_t rest = chosen[64 + lane];
-                        wave_sync<true>();
-                        chosen[lane] = rest;
+                for (int half = 0; half < 2; ++half) {
+                    const uint32_t least_order = best.least_order();
+                    const float least = least_order ? fmaxf(order_value(least_order), -kFltMax) : -kFltMax;
+                    int found = 0;
+#pragma unroll
+                    for (int j = half * (E / 2); j < (half + 1) * (E / 2); ++j) {
+                        const bool in = !(u[j] < least);
+                        const uint64_t mask = __ballot(in);
+                        if (mask == 0) continue;
+                        const uint32_t at = (uint32_t)(base + (j / V * TPR + t) * V + j % V);
+                        if (in) chosen[found + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0))] = key_of(u[j], at);
+                        found += __popcll(mask);
                     }
+                    wave_sync<true>();
+#pragma unroll 1
+                    for (int i = 0; i < found; i += 64) best.offer(i + lane < found ? chosen[i + lane] : KEY_MAX, top);
+                    wave_sync<true>();
                 }
-                wave_sync<true>();
-                best.offer(lane < found, chosen[lane], top);
-                wave_sync<true>();
             }
         }
         r = wave_join(r);
@@ -222,7 +224,7 @@ __global__ __launch_bounds__(256) void log_probs_kernel(int64_t m, int64_t v, co
                 }
                 r = all;
                 if constexpr (TOP) {
-                    for (int w = 1; w < W; ++w) best.offer(lane < top, lane < top ? lds_keys[w * 64 + lane] : 0, top);
+                    for (int w = 1; w < W; ++w) best.offer(lane < top ? lds_keys[w * 64 + lane] : KEY_MAX, top);
                 }
             }
         }
@@ -251,7 +253,7 @@ __global__ __launch_bounds__(64) void log_probs_join_kernel(int64_t m, int64_t v
         const int n = nseg * top;
         const uint64_t *keys = part_keys + row * n;
         uint32_t most_key = 0;
-        for (int i = lane; i < n; i += 64) most_key = max(most_key, (uint32_t)(keys[i] >> 32));
+        for (int i = lane; i < n; i += 64) most_key = max(most_key, ~(uint32_t)(keys[i] >> 32));
         for (int i = lane; i < nseg; i += 64) {
             const float4 p = part_sums[row * nseg + i];
             RowSums q = {p.x, p.y, p.z};
@@ -264,7 +266,7 @@ __global__ __launch_bounds__(64) void log_probs_join_kernel(int64_t m, int64_t v
         r = wave_join(r);
         WaveTop best;
         if (top) best.expect(most_key, top);
-        for (int i = 0; i < n; i += 64) best.offer(i + lane < n, i + lane < n ? keys[i + lane] : 0, top);
+        for (int i = 0; i < n; i += 64) best.offer(i + lane < n ? keys[i + lane] : KEY_MAX, top);
         finish_row(out, asked, row, v, top, r, best.key);
     }
 }
