@@ -68,15 +68,23 @@ template <class T, int N> __device__ __forceinline__ void store_row(T *p, int n,
             if (i < n) p[i] = v[i];
     }
 }
-// The epilogue: outputs p .. p + n - 1 of row q.
-template <class T, int N> __device__ __forceinline__ void finish(const Epilogue<T> &e, int64_t q, int64_t p, int n, float (&v)[N])
+// The epilogue: outputs p .. p + n - 1 of row q.  bias: of these outputs, loaded by the caller (one that writes many rows loads it
+// once: loaded per row it took 15 us of 10,000 x 4,096 outputs' 45).
+template <class T, int N> __device__ __forceinline__ void load_bias(const Epilogue<T> &e, int64_t p, int n, float (&bias)[N])
+{
+    if (e.bias) {
+        load_row(e.bias + p, n, bias);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) bias[i] = 0.f;
+    }
+}
+template <class T, int N>
+__device__ __forceinline__ void finish(const Epilogue<T> &e, int64_t q, int64_t p, int n, float (&v)[N], const float (&bias)[N])
 {
     float u[N];
-    if (e.bias) {
-        load_row(e.bias + p, n, u);
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += u[i];
-    }
+    for (int i = 0; i < N; ++i) v[i] += bias[i];
     if (e.z) store_row(e.z + q * e.ldz + p, n, v);
     if (e.act != VF_ACT_NONE)
         by_act(e.act, [&](auto act) {
@@ -154,7 +162,12 @@ __global__ __launch_bounds__(1024) void few_rows_kernel(Product<T> a, Epilogue<T
             for (int i = 0; i < 4; ++i) v[i] += u[i];
         }
         const int64_t q = j * 16 + (lane & 15), p = p0 + (lane >> 4) * 4;
-        if (q < a.nq && p < a.np) finish(e, q, p, (int)min((int64_t)4, a.np - p), v);
+        if (q < a.nq && p < a.np) {
+            const int n = (int)min((int64_t)4, a.np - p);
+            float bias[4];
+            load_bias(e, p, n, bias);
+            finish(e, q, p, n, v, bias);
+        }
     }
 }
 
@@ -271,6 +284,10 @@ __device__ __forceinline__ void store_tile(const Product<T> &a, const Epilogue<T
 {
     constexpr int kRow = WAVE_P * 4 + 16, kLanes = WAVE_P / 8;   // 16 bytes more: rows start in other banks
     unsigned char *turn = lds + wave * (16 * kRow);
+    const int64_t p = p_first + lane % kLanes * 8;
+    const int m = (int)max((int64_t)0, min((int64_t)8, a.np - p));
+    float bias[8];
+    load_bias(e, p, m, bias);
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < FQ; ++j) {
@@ -279,12 +296,11 @@ __device__ __forceinline__ void store_tile(const Product<T> &a, const Epilogue<T
         wave_sync<true>();
 #pragma unroll 1
         for (int r = lane / kLanes; r < 16; r += 64 / kLanes) {
-            const int64_t q = q_first + j * 16 + r, p = p_first + lane % kLanes * 8;
+            const int64_t q = q_first + j * 16 + r;
             float v[8];
             *(float4v *)v = *(const float4v *)(turn + r * kRow + lane % kLanes * 32);
             *(float4v *)(v + 4) = *(const float4v *)(turn + r * kRow + lane % kLanes * 32 + 16);
-            if (q >= a.nq || p >= a.np) continue;
-            const int m = (int)min((int64_t)8, a.np - p);
+            if (q >= a.nq || m == 0) continue;
             if (a.splits > 1) {
                 float *to = a.part + ((int64_t)blockIdx.y * a.nq + q) * a.np + p;
                 if (m == 8) {
@@ -296,7 +312,7 @@ __device__ __forceinline__ void store_tile(const Product<T> &a, const Epilogue<T
                         if (u < m) to[u] = v[u];
                 }
             } else {
-                finish(e, q, p, m, v);
+                finish(e, q, p, m, v, bias);
             }
         }
         wave_sync<true>();
@@ -547,7 +563,9 @@ __global__ __launch_bounds__(256) void product_join_kernel(int64_t np, int64_t n
 #pragma unroll
             for (int j = 0; j < 4; ++j) a[j] += u[j];
         }
-        finish(e, q, p, n, a);
+        float bias[4];
+        load_bias(e, p, n, bias);
+        finish(e, q, p, n, a, bias);
     }
 }
 
@@ -640,6 +658,7 @@ struct ProductPlan {
 // What the choice of a kernel depends on beside the sizes.
 struct Operands {
     bool p_along, q_along;   // contiguous along the contraction
+    bool costly_act;         // an epilogue with GELU or SiLU
     bool direct;             // 2-byte types; rows start on 16 bytes, and an operand contiguous along its rows has whole vectors of them
 };
 
@@ -660,7 +679,10 @@ static ProductPlan plan_product(int32_t dtype, int64_t np, int64_t nq, int64_t n
     for (Tiling t : {kSmall, kMedium, kDirect128, kDirectWide, kDirect256}) {
         if (t >= kDirect128 && !o.direct) continue;
         if (t == kDirectWide && !both) continue;
-        const TilingCost c = cost_of(t, f32, both);
+        TilingCost c = cost_of(t, f32, both);
+        // 9 us of a compute unit's vector ALUs for 256 x 256 outputs, three quarters of that where other workgroups multiply meanwhile
+        // (10,000 x 4,096 x 1,024 with GELU: 114 us in tiles of 128 x 256, 124 in 256 x 256; without 93 and 98)
+        if (o.costly_act) c.fixed += 9.0 * c.together * c.bp * c.bq / 65536 * (c.together > 1 ? 0.75 : 1);
         const int64_t tiles = ceil_div(np, c.bp) * ceil_div(nq, c.bq);
         for (int64_t splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
             const int64_t chunk = std::max<int64_t>(step, ceil_div(ceil_div(nc, splits), step) * step);
@@ -751,6 +773,8 @@ static int run_product(int32_t dtype, const T *P, int64_t ldp, int64_t np, const
 
 static size_t rounded(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 
+static bool costly(int32_t act) { return act == VF_ACT_GELU || act == VF_ACT_SILU; }
+
 // Whether rows of an operand that lie `ld` elements apart can go to LDS directly: the kernel's offsets within a tile have 32 bits.
 static bool direct_rows(int32_t dtype, const void *p, int64_t ld)
 {
@@ -758,10 +782,10 @@ static bool direct_rows(int32_t dtype, const void *p, int64_t ld)
 }
 
 // Workspace of a product whose operands' alignment is not known yet.
-static size_t most_bytes(int32_t dtype, int64_t np, int64_t nq, int64_t nc, bool p_along, bool q_along)
+static size_t most_bytes(int32_t dtype, int64_t np, int64_t nq, int64_t nc, bool p_along, bool q_along, bool costly)
 {
-    return std::max(plan_product(dtype, np, nq, nc, {p_along, q_along, false}).bytes,
-                    dtype == VF_F32 ? 0 : plan_product(dtype, np, nq, nc, {p_along, q_along, true}).bytes);
+    return std::max(plan_product(dtype, np, nq, nc, {p_along, q_along, costly, false}).bytes,
+                    dtype == VF_F32 ? 0 : plan_product(dtype, np, nq, nc, {p_along, q_along, costly, true}).bytes);
 }
 
 // What the backward pass takes of its workspace: dz, the partial column sums, the splits of a product (one at a time).
@@ -777,7 +801,7 @@ static BackwardPlan plan_backward(int32_t dtype, int64_t m, int64_t n, int64_t k
     b.row_parts = std::max<int64_t>(1, std::min<int64_t>(ceil_div(m, 4), 1024 / std::max<int64_t>(1, std::min<int64_t>(across, 1024))));
     b.dz = act == VF_ACT_NONE ? 0 : (size_t)m * n * type_size(dtype);
     b.parts = (size_t)b.row_parts * n * 4;
-    b.product = std::max(most_bytes(dtype, k, m, n, false, true), most_bytes(dtype, k, n, m, false, false));
+    b.product = std::max(most_bytes(dtype, k, m, n, false, true, false), most_bytes(dtype, k, n, m, false, false, false));
     return b;
 }
 
@@ -795,7 +819,7 @@ int linear_workspace_impl(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_
 {
     VF_REQUIRE(bytes != nullptr, "linear: bytes is NULL");
     if (int rc = check_sizes(dtype, m, n, k, act); rc != VF_OK) return rc;
-    *bytes = backward ? plan_backward(dtype, m, n, k, act).total() : most_bytes(dtype, n, m, k, true, true);
+    *bytes = backward ? plan_backward(dtype, m, n, k, act).total() : most_bytes(dtype, n, m, k, true, true, costly(act));
     return VF_OK;
 }
 
@@ -807,7 +831,7 @@ int linear_impl(const LinearArgs &a)
     VF_REQUIRE(a.y != nullptr, "linear: y is NULL");
     VF_REQUIRE(a.ldx >= a.k && a.ldw >= a.k, "linear: ldx or ldw is less than k");
     VF_REQUIRE(a.ldy >= a.n && (!a.z || a.ldz >= a.n) && (!a.residual || a.ldr >= a.n), "linear: ldy, ldz or ldr is less than n");
-    const ProductPlan plan = plan_product(a.dtype, a.n, a.m, a.k, {true, true, direct_rows(a.dtype, a.x, a.ldx) && direct_rows(a.dtype, a.w, a.ldw)});
+    const ProductPlan plan = plan_product(a.dtype, a.n, a.m, a.k, {true, true, costly(a.act), direct_rows(a.dtype, a.x, a.ldx) && direct_rows(a.dtype, a.w, a.ldw)});
     if (int rc = check_workspace("linear", a.workspace, a.workspace_bytes, plan.bytes); rc != VF_OK) return rc;
     int rc = VF_OK;
     by_type(a.dtype, [&](auto *t) {
@@ -853,13 +877,13 @@ int linear_backward_impl(const LinearArgs &a)
             const Epilogue<T> e{nullptr, VF_ACT_NONE, nullptr, 0, (T *)a.dx, a.lddx, nullptr, 0};
             const bool direct = a.k % 8 == 0 && direct_rows(a.dtype, a.w, a.ldw) && direct_rows(a.dtype, dz, lddz);
             rc = run_product<T, false, true>(a.dtype, (const T *)a.w, a.ldw, a.k, dz, lddz, a.m, a.n, e,
-                                             plan_product(a.dtype, a.k, a.m, a.n, {false, true, direct}), splits, a.stream);
+                                             plan_product(a.dtype, a.k, a.m, a.n, {false, true, false, direct}), splits, a.stream);
         }
         if (a.dw && rc == VF_OK) {
             const Epilogue<T> e{nullptr, VF_ACT_NONE, nullptr, 0, (T *)a.dw, a.lddw, nullptr, 0};
             const bool direct = a.k % 8 == 0 && a.n % 8 == 0 && direct_rows(a.dtype, a.x, a.ldx) && direct_rows(a.dtype, dz, lddz);
             rc = run_product<T, false, false>(a.dtype, (const T *)a.x, a.ldx, a.k, dz, lddz, a.n, a.m, e,
-                                              plan_product(a.dtype, a.k, a.n, a.m, {false, false, direct}), splits, a.stream);
+                                              plan_product(a.dtype, a.k, a.n, a.m, {false, false, false, direct}), splits, a.stream);
         }
     });
     if (rc == VF_OK) VF_HIP(hipGetLastError());
@@ -870,7 +894,7 @@ int debug_linear_impl(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t pr
 {
     if (int rc = check_sizes(dtype, m, n, k, VF_ACT_NONE); rc != VF_OK) return rc;
     VF_REQUIRE(product >= 0 && product <= 2 && tiling && splits, "linear: product must be 0 .. 2, tiling and splits not NULL");
-    const Operands o{product == 0, product <= 1, direct != 0 && dtype != VF_F32};
+    const Operands o{product == 0, product <= 1, false, direct != 0 && dtype != VF_F32};
     const ProductPlan p = product == 0 ? plan_product(dtype, n, m, k, o) : product == 1 ? plan_product(dtype, k, m, n, o) : plan_product(dtype, k, n, m, o);
     *tiling = p.tiling;
     *splits = p.splits;
