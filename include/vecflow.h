@@ -381,8 +381,9 @@ int vf_linear_backward(int32_t dtype, int64_t m, int64_t n, int64_t k, const voi
 int vf_linear_workspace(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t activation, int32_t backward,
                         size_t *bytes);
 /*
- * Test support, host only: the tiling (0 few rows, 1 64 x 64, 2 128 x 128, 3 - 5 straight to LDS: 128 x 128, 128 x 256, 256 x 256) and the
- * number of splits of the contraction that the forward product (product = 0), dx (1) or dw (2) of these sizes takes.
+ * Test support, host only: the tiling (0 few rows, 1 64 x 64, 2 128 x 128, 3 - 6 straight to LDS: 128 x 128, 128 x 256, 256 x 192, 256 x 256)
+ * and the number of splits of the contraction that the forward product without activation (product = 0), dx (1) or dw (2) of these
+ * sizes takes.
  *   direct   1: both operands' rows start on 16 bytes and have whole 16-byte vectors
  */
 int vf_debug_linear(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t product, int32_t direct, int32_t *tiling,

@@ -398,8 +398,8 @@ template <class T, bool ALONG_C, int ROWS> __device__ __forceinline__ uint32_t d
         return (uint32_t)(min((int64_t)r, rows_left - 1) * ld * (int64_t)sizeof(T)) + (direct_chunk(r, lane & 3) << 4);
     } else {
         constexpr int kLine = ROWS / 8;   // 16-byte chunks of a line
-        const int c = (piece * 64 + lane) / kLine;
-        const int byte = line_place<T, ROWS>(c, lane % kLine * 16) - c * ROWS * 2;
+        const int id = piece * 64 + lane, c = id / kLine;
+        const int byte = line_place<T, ROWS>(c, id % kLine * 16) - c * ROWS * 2;
         return (uint32_t)(c * ld * (int64_t)sizeof(T)) + (uint32_t)min((int64_t)byte, rows_left * (int64_t)sizeof(T) - 16);
     }
 }
@@ -425,9 +425,9 @@ template <class T, bool PC, bool QC, int BP, int BQ, int WP, int WQ, int STEPS>
 __global__ __launch_bounds__(WP *WQ * 64, 2) void direct_kernel(Product<T> a, Epilogue<T> e)
 {
     constexpr int BC = 32, WAVES = WP * WQ, FP = BP / WP / 16, FQ = BQ / WQ / 16;
-    constexpr int LP = BP / 16 / WAVES, LQ = BQ / 16 / WAVES, LOADS = LP + LQ;   // loads of a wave, per step
+    constexpr int NP = BP / 16, NQ = BQ / 16;   // loads of a step; where they do not divide among the waves the last one is made twice
+    constexpr int LP = (NP + WAVES - 1) / WAVES, LQ = (NQ + WAVES - 1) / WAVES, LOADS = LP + LQ;
     constexpr int kStep = (BP + BQ) * 64;
-    static_assert(LP * 16 * WAVES == BP && LQ * 16 * WAVES == BQ, "every wave requests as much");
     extern __shared__ __align__(16) unsigned char tiles[];   // [STEPS][P, Q][rows of 64 bytes, or 32 lines]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t tiles_p = (a.np + BP - 1) / BP;
@@ -441,12 +441,11 @@ __global__ __launch_bounds__(WP *WQ * 64, 2) void direct_kernel(Product<T> a, Ep
     const T *Q = QC ? a.Q + q0 * a.ldq + c_first : a.Q + c_first * a.ldq + q0;
     uint32_t off_p[LP], off_q[LQ];
 #pragma unroll
-    for (int i = 0; i < LP; ++i) off_p[i] = direct_offset<T, PC, BP>(wave * LP + i, lane, a.ldp, a.np - p0);
+    for (int i = 0; i < LP; ++i) off_p[i] = direct_offset<T, PC, BP>(min(wave * LP + i, NP - 1), lane, a.ldp, a.np - p0);
 #pragma unroll
-    for (int i = 0; i < LQ; ++i) off_q[i] = direct_offset<T, QC, BQ>(wave * LQ + i, lane, a.ldq, a.nq - q0);
+    for (int i = 0; i < LQ; ++i) off_q[i] = direct_offset<T, QC, BQ>(min(wave * LQ + i, NQ - 1), lane, a.ldq, a.nq - q0);
     const int64_t step_p = PC ? BC : BC * a.ldp, step_q = QC ? BC : BC * a.ldq;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)tiles;
-    const uint32_t lds_p = lds0 + wave * (LP * 1024), lds_q = lds0 + BP * 64 + wave * (LQ * 1024);
     auto buffer_of = [](int t) { return (STEPS & (STEPS - 1)) == 0 ? t & (STEPS - 1) : t % STEPS; };
     auto request_some = [&](int t, int first, int last) {   // loads first .. last - 1 of a step's
         const uint32_t at = buffer_of(t) * kStep;
@@ -454,8 +453,8 @@ __global__ __launch_bounds__(WP *WQ * 64, 2) void direct_kernel(Product<T> a, Ep
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             if (i < first || i >= last) continue;
-            if (i < LP) request(p, off_p[i], lds_p + at + i * 1024);
-            else request(q, off_q[i - LP], lds_q + at + (i - LP) * 1024);
+            if (i < LP) request(p, off_p[i], lds0 + at + min(wave * LP + i, NP - 1) * 1024);
+            else request(q, off_q[i - LP], lds0 + BP * 64 + at + min(wave * LQ + i - LP, NQ - 1) * 1024);
         }
     };
     const int wp = wave % WP * (FP * 16), wq = wave / WP * (FQ * 16);
@@ -616,7 +615,8 @@ enum Tiling {
     kSmall,         // 64 x 64, any operands
     kMedium,        // 128 x 128, any operands
     kDirect128,     // 128 x 128, aligned operands of 2 bytes, straight to LDS
-    kDirectWide,    // 128 x 256, the same, two workgroups per compute unit; both operands along c
+    kDirectWide,    // 128 x 256, two workgroups per compute unit; both operands along c
+    kDirect192,     // 256 x 192, the same, any operands
     kDirect256,     // 256 x 256, the same
 };
 
@@ -633,12 +633,13 @@ static TilingCost cost_of(Tiling t, bool f32, bool both_along)
     switch (t) {
     case kSmall:
         return f32 ? (both_along ? TilingCost{64, 64, 4, 2.2, 0.77, 3.9} : TilingCost{64, 64, 4, 2.3, 0.90, 3.9})
-                   : (both_along ? TilingCost{64, 64, 4, 0.86, 0.46, 3.4} : TilingCost{64, 64, 4, 0.95, 0.67, 3.5});
+                   : (both_along ? TilingCost{64, 64, 4, 0.95, 0.50, 3.4} : TilingCost{64, 64, 4, 0.95, 0.67, 3.5});
     case kMedium:
         return f32 ? TilingCost{128, 128, 2, 3.2, 2.1, 4.6}
                    : (both_along ? TilingCost{128, 128, 2, 1.0, 0.85, 3.6} : TilingCost{128, 128, 2, 1.3, 0.95, 4.0});
     case kDirect128: return both_along ? TilingCost{128, 128, 3, 1.43, 0.46, 4.2} : TilingCost{128, 128, 3, 1.35, 0.68, 4.6};
     case kDirectWide: return TilingCost{128, 256, 2, 1.4, 0.74, 5.6};
+    case kDirect192: return both_along ? TilingCost{256, 192, 1, 0.97, 0.60, 4.8} : TilingCost{256, 192, 1, 0.95, 0.60, 5.5};
     default: return both_along ? TilingCost{256, 256, 1, 1.13, 0.61, 6.0} : TilingCost{256, 256, 1, 1.2, 0.61, 6.4};
     }
 }
@@ -676,7 +677,7 @@ static ProductPlan plan_product(int32_t dtype, int64_t np, int64_t nq, int64_t n
         best.chunk = nc;
         least = few_rows_us(np, nq, nc * (int64_t)type_size(dtype));
     }
-    for (Tiling t : {kSmall, kMedium, kDirect128, kDirectWide, kDirect256}) {
+    for (Tiling t : {kSmall, kMedium, kDirect128, kDirectWide, kDirect192, kDirect256}) {
         if (t >= kDirect128 && !o.direct) continue;
         if (t == kDirectWide && !both) continue;
         TilingCost c = cost_of(t, f32, both);
@@ -759,7 +760,8 @@ static int run_product(int32_t dtype, const T *P, int64_t ldp, int64_t np, const
         static_assert(lds <= 64 * 1024, "");
         tile_kernel<T, PC, QC, 128, 128, 2, 4><<<grid, dim3(512), lds, s>>>(a, e);
     } else if constexpr (sizeof(T) == 2) {
-        if (plan.tiling == kDirect256) rc = launch_direct<T, PC, QC, 256, 256, 2, 4, 4>(a, e, grid, s);
+        if (plan.tiling == kDirect192) rc = launch_direct<T, PC, QC, 256, 192, 4, 2, 4>(a, e, grid, s);
+        else if (plan.tiling == kDirect256) rc = launch_direct<T, PC, QC, 256, 256, 2, 4, 4>(a, e, grid, s);
         else if (plan.tiling == kDirect128) rc = launch_direct<T, PC, QC, 128, 128, 2, 2, 3>(a, e, grid, s);
         else if constexpr (PC && QC) rc = launch_direct<T, PC, QC, 128, 256, 2, 2, 3>(a, e, grid, s);
     }

@@ -16,7 +16,8 @@ CODE = {BF: vf.VF_BF16, FP: vf.VF_F32, HF: vf.VF_F16}
 CASES = [(40, 1000, 200, BF, 0), (64, 4099, 1025, HF, 0), (300, 1000, 520, BF, 0), (2049, 1096, 520, BF, 0), (2049, 1096, 520, HF, 8),
          (2500, 2056, 520, BF, 0), (5000, 4104, 264, BF, 0), (700, 4000, 4104, HF, 0), (9000, 4104, 1032, BF, 0), (9000, 4104, 1032, HF, 8),
          (2500, 2056, 520, BF, 3), (9000, 4104, 1032, BF, 5), (3001, 1030, 777, FP, 0), (9000, 1032, 520, FP, 3), (130, 90, 5000, BF, 0),
-         (64, 128, 4096, BF, 0), (10000, 96, 100, FP, 0), (257, 257, 8, BF, 0)]
+         (64, 128, 4096, BF, 0), (10000, 96, 100, FP, 0), (257, 257, 8, BF, 0), (10000, 1032, 1032, HF, 0), (5001, 4104, 1032, BF, 8),
+         (10000, 520, 4104, BF, 0), (3001, 2056, 2056, HF, 0)]
 
 
 def plans(m, n, k, dtype, pad):
@@ -31,7 +32,7 @@ def test_the_cases_reach_every_tiling():
         for p, (tiling, splits) in enumerate(plans(*c)):
             seen[p].add(tiling)
             split[p] |= splits > 1
-    assert seen[0] == {0, 1, 2, 3, 4, 5} and seen[1] >= {1, 2, 3, 5} and seen[2] >= {1, 2, 3, 5} and all(split)
+    assert seen[0] == {0, 1, 2, 3, 4, 5, 6} and seen[1] >= {1, 2, 3, 5, 6} and seen[2] >= {1, 2, 3, 5, 6} and all(split)
 
 
 @pytest.mark.parametrize("case", CASES)
