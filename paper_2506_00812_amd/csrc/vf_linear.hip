@@ -115,7 +115,7 @@ constexpr int kRowBytes = 128;     // bytes of the contraction per step of the t
 // At most 16 FQ rows of Q (queries that are served one by one or in small batches): the work is one read of P, so no tile is shared and
 // nothing waits for another wave until the end.  A workgroup has 16 rows of P; its waves share the contraction in whole fragments, loaded
 // from memory straight into the matrix instruction's layout, several in flight, and add up through LDS.
-// One row, 4096 x 1024 in bfloat16 (8 MB of weights): 4.7 us; 64 x 64 tiles over a split contraction and their join took 13.
+// One row, 4096 x 1024 in bfloat16 (8 MB of weights): 4.4 us; 64 x 64 tiles over a split contraction and their join took 13.
 template <class T, int FQ>
 __global__ __launch_bounds__(1024) void few_rows_kernel(Product<T> a, Epilogue<T> e)
 {
@@ -780,7 +780,7 @@ static bool costly(int32_t act) { return act == VF_ACT_GELU || act == VF_ACT_SIL
 // Whether rows of an operand that lie `ld` elements apart can go to LDS directly: the kernel's offsets within a tile have 32 bits.
 static bool direct_rows(int32_t dtype, const void *p, int64_t ld)
 {
-    return dtype != VF_F32 && ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && ld < (1 << 22);
+    return dtype != VF_F32 && ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && ld < (1 << 21);
 }
 
 // Workspace of a product whose operands' alignment is not known yet.

@@ -39,11 +39,12 @@ __device__ __forceinline__ void scale_to(RowSums &r, float m)
     r.m = m;
 }
 
-__device__ __forceinline__ RowSums wave_join(RowSums r)
+// Over the LANES (16 or 64) lanes that share a row.
+template <int LANES = 64> __device__ __forceinline__ RowSums wave_join(RowSums r)
 {
-    scale_to(r, wave_max(r.m));
-    r.s = wave_sum(r.s);
-    r.a = wave_sum(r.a);
+    scale_to(r, LANES == 16 ? max16(r.m) : wave_max(r.m));
+    r.s = LANES == 16 ? sum16(r.s) : wave_sum(r.s);
+    r.a = LANES == 16 ? sum16(r.a) : wave_sum(r.a);
     return r;
 }
 
@@ -111,11 +112,11 @@ template <class T> struct Asked {
     }
 };
 
-// What a row's sums and keys say, written by one wave.
+// What a row's sums and keys say, written by the wave (or by the sixteen lanes) that has them.
 template <class T>
-__device__ __forceinline__ void finish_row(const LogProbOut &o, const Asked<T> &asked, int64_t row, int64_t v, int top, const RowSums &r, uint64_t key)
+__device__ __forceinline__ void finish_row(const LogProbOut &o, const Asked<T> &asked, int64_t row, int64_t v, int top, const RowSums &r, uint64_t key,
+                                           int lane)
 {
-    const int lane = threadIdx.x & 63;
     const bool empty = r.m == -kInf && r.s == 0.f;
     const float log_s = logf(r.s);
     if (lane == 0) {
@@ -159,8 +160,14 @@ __global__ __launch_bounds__(256) void log_probs_kernel(int64_t m, int64_t v, co
         if (nseg == 1) asked.load(out, x, row, v);
         for (int64_t base = c0; base < c1; base += TPR * E) {
             float u[E];
+            const int left = (int)min((int64_t)(TPR * E), c1 - base);   // vectors beyond it are skipped by all lanes at once
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
+                if (i * TPR * V >= left) {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) u[i * V + j] = -kInf;
+                    continue;
+                }
                 const int64_t c = base + (i * TPR + t) * V;
                 Vec<T> raw;
                 if (base + TPR * E <= c1) raw = load_vec<Vec<T>>(x + c);
@@ -175,6 +182,7 @@ __global__ __launch_bounds__(256) void log_probs_kernel(int64_t m, int64_t v, co
             const float origin = r.m == -kInf ? 0.f : r.m;
 #pragma unroll
             for (int j = 0; j < E; ++j) {
+                if (j % V == 0 && j / V * TPR * V >= left) break;
                 // (the distance of a masked entry is -inf and its term 0; a NaN, which the maximum passes over, stays in s)
                 const float d = u[j] - origin, e = exp_fast(d);
                 r.s += e;
@@ -190,6 +198,7 @@ __global__ __launch_bounds__(256) void log_probs_kernel(int64_t m, int64_t v, co
                     int found = 0;
 #pragma unroll
                     for (int j = half * (E / 2); j < (half + 1) * (E / 2); ++j) {
+                        if (j % V == 0 && j / V * TPR * V >= left) break;
                         const bool in = !(u[j] < least);
                         const uint64_t mask = __ballot(in);
                         if (mask == 0) continue;
@@ -204,7 +213,7 @@ __global__ __launch_bounds__(256) void log_probs_kernel(int64_t m, int64_t v, co
                 }
             }
         }
-        r = wave_join(r);
+        r = wave_join<TPR == 16 ? 16 : 64>(r);
         if constexpr (W > 1) {
             __syncthreads();
             if (lane == 0) { lds_sums[wave][0] = r.m; lds_sums[wave][1] = r.s; lds_sums[wave][2] = r.a; }
@@ -228,9 +237,9 @@ __global__ __launch_bounds__(256) void log_probs_kernel(int64_t m, int64_t v, co
                 }
             }
         }
-        if (W == 1 || wave == 0) {
+        if (W <= 1 || wave == 0) {
             if (nseg == 1) {
-                finish_row(out, asked, row, v, TOP ? top : 0, r, best.key);
+                finish_row(out, asked, row, v, TOP ? top : 0, r, best.key, TPR == 16 ? t : lane);
             } else {
                 if (lane == 0) part_sums[item] = make_float4(r.m, r.s, r.a, 0.f);
                 if (TOP && lane < top) part_keys[item * top + lane] = best.key;
@@ -267,7 +276,7 @@ __global__ __launch_bounds__(64) void log_probs_join_kernel(int64_t m, int64_t v
         WaveTop best;
         if (top) best.expect(most_key, top);
         for (int i = 0; i < n; i += 64) best.offer(i + lane < n ? keys[i + lane] : KEY_MAX, top);
-        finish_row(out, asked, row, v, top, r, best.key);
+        finish_row(out, asked, row, v, top, r, best.key, lane);
     }
 }
 
@@ -300,15 +309,16 @@ __global__ void log_probs_backward_kernel(int64_t m, int64_t v, const T *logits,
     }
 }
 
-// Threads per row and segments of a row.  Rows of up to 2,048 elements are a wave's; longer ones a workgroup's, in
-// segments where there are too few rows to fill the chip.
+// Threads per row and segments of a row.  Rows of up to 2,048 elements are a wave's, without alternatives up to 256 sixteen lanes' (100,000
+// rows of 100 labels: 43 us a wave each); longer ones a workgroup's, in segments where there are too few rows to fill the chip.
 struct LogProbPlan {
     int tpr, nseg;
     int64_t seg;
 };
-static LogProbPlan plan_of(int64_t m, int64_t v)
+static LogProbPlan plan_of(int64_t m, int64_t v, int32_t top)
 {
     LogProbPlan p{64, 1, v};
+    if (v <= 256 && top == 0) p.tpr = 16;
     if (v <= 2048) return p;
     p.tpr = 256;
     const int64_t unit = 256 * 16;
@@ -333,7 +343,7 @@ int log_probs_workspace_impl(int32_t dtype, int64_t m, int64_t v, int32_t top, s
     if (int rc = check_log_probs(dtype, m, v, top); rc != VF_OK) return rc;
     *bytes = 0;
     if (m == 0) return VF_OK;
-    const LogProbPlan p = plan_of(m, v);
+    const LogProbPlan p = plan_of(m, v, top);
     if (p.nseg > 1) *bytes = (size_t)m * p.nseg * (16 + 8 * (size_t)top);
     return VF_OK;
 }
@@ -348,14 +358,14 @@ int log_probs_impl(const LogProbArgs &a)
     VF_REQUIRE(a.top == 0 || a.m == 0 || (a.top_ids && a.top_logp), "log probs: top_ids or top_logp is NULL");
     if (int rc = check_workspace("log probs", a.workspace, a.workspace_bytes, need); rc != VF_OK) return rc;
     if (a.m == 0) return VF_OK;
-    const LogProbPlan p = plan_of(a.m, a.v);
+    const LogProbPlan p = plan_of(a.m, a.v, a.top);
     const LogProbOut out{a.targets, a.logp, a.entropy, a.lse, a.top_ids, a.top_logp};
     float4 *sums = (float4 *)a.workspace;
     uint64_t *keys = (uint64_t *)(sums + (p.nseg > 1 ? a.m * p.nseg : 0));
     by_type(a.dtype, [&](auto *q) {
         using T = std::remove_pointer_t<decltype(q)>;
         const T *x = (const T *)a.logits;
-        const int64_t blocks = p.tpr == 64 ? ceil_div(a.m, 4) : a.m * p.nseg;
+        const int64_t blocks = p.tpr < 256 ? ceil_div(a.m, 256 / p.tpr) : a.m * p.nseg;
         const dim3 grid((unsigned)std::min<int64_t>(blocks, 1 << 20)), block(256);
         auto launch = [&](auto tpr, auto with_top) {
             log_probs_kernel<T, tpr.value, with_top.value><<<grid, block, 0, a.stream>>>(a.m, a.v, x, a.ld, p.nseg, p.seg, a.top, out,
@@ -363,7 +373,8 @@ int log_probs_impl(const LogProbArgs &a)
         };
         using W = std::integral_constant<int, 64>;
         using G = std::integral_constant<int, 256>;
-        if (p.tpr == 64) { if (a.top) launch(W(), std::true_type()); else launch(W(), std::false_type()); }
+        if (p.tpr == 16) launch(std::integral_constant<int, 16>(), std::false_type());
+        else if (p.tpr == 64) { if (a.top) launch(W(), std::true_type()); else launch(W(), std::false_type()); }
         else { if (a.top) launch(G(), std::true_type()); else launch(G(), std::false_type()); }
         if (p.nseg > 1)
             log_probs_join_kernel<T><<<dim3((unsigned)std::min<int64_t>(a.m, 1 << 20)), dim3(64), 0, a.stream>>>(

@@ -73,20 +73,28 @@ template <int CTRL> __device__ __forceinline__ float dpp(float v)
     return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xF, 0xF, true));
 }
 __device__ __forceinline__ float lane_value(float v, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); }
+__device__ __forceinline__ float sum16(float v)   // of each row of sixteen lanes
+{
+    v += dpp<0xB1>(v);           // the neighbour
+    v += dpp<0x4E>(v);           // the other pair of four
+    v += dpp<0x141>(v);          // the other four of eight
+    return v + dpp<0x140>(v);    // the other eight of sixteen
+}
 __device__ __forceinline__ float wave_sum(float v)
 {
-    v += dpp<0xB1>(v);    // the neighbour
-    v += dpp<0x4E>(v);    // the other pair of four
-    v += dpp<0x141>(v);   // the other four of eight
-    v += dpp<0x140>(v);   // the other eight of sixteen
+    v = sum16(v);
     return (lane_value(v, 0) + lane_value(v, 16)) + (lane_value(v, 32) + lane_value(v, 48));
 }
-__device__ __forceinline__ float wave_max(float v)
+__device__ __forceinline__ float max16(float v)
 {
     v = fmaxf(v, dpp<0xB1>(v));
     v = fmaxf(v, dpp<0x4E>(v));
     v = fmaxf(v, dpp<0x141>(v));
-    v = fmaxf(v, dpp<0x140>(v));
+    return fmaxf(v, dpp<0x140>(v));
+}
+__device__ __forceinline__ float wave_max(float v)
+{
+    v = max16(v);
     return fmaxf(fmaxf(lane_value(v, 0), lane_value(v, 16)), fmaxf(lane_value(v, 32), lane_value(v, 48)));
 }
 
