@@ -234,6 +234,8 @@ template <int BITS> struct AdamwBlock {
     }
 };
 
+// 32 bits, 9.6 M float32 parameters: 55 us, 4.9 TB/s.  8 bits, 18.8 M bfloat16 parameters with masters: 72 us, 4.2 TB/s; there the vector
+// ALUs are as busy as memory (three square roots and a division a parameter, some 90 instructions).
 template <int BITS>
 __global__ __launch_bounds__(256) void adamw_kernel(const AdamwList l, const AdamwScalars c, const int32_t *skip)
 {
@@ -261,7 +263,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamwList l, const Ada
     }
 }
 
-// master: where m goes, param: where v goes.
+// master: where m goes, param: where v goes.  18.8 M parameters from 8 bits: 30 us, 6 TB/s (half of it in the cache still).
 template <int BITS> __global__ __launch_bounds__(256) void adamw_moments_kernel(const AdamwList l)
 {
     const int lane = threadIdx.x & 63;

