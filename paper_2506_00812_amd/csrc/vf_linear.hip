@@ -277,13 +277,13 @@ template <class T, bool ALONG_C, int ROWS, int THREADS> struct Stage {
 };
 
 // The end of a workgroup: each wave turns sixteen rows of its accumulators at a time through LDS, so that its stores are whole stretches
-// of a row (half the time of the eight-byte pieces that a lane holds).
+// of a row and not the four neighbours that a lane holds.
 template <class T, int FP, int FQ, int WAVE_P, int WAVE_Q>
 __device__ __forceinline__ void store_tile(const Product<T> &a, const Epilogue<T> &e, const float4v (&acc)[FP][FQ], unsigned char *lds, int wave,
                                            int lane, int64_t p_first, int64_t q_first)
 {
     constexpr int kRow = WAVE_P * 4 + 16, kLanes = WAVE_P / 8;   // 16 bytes more: rows start in other banks
-    unsigned char *turn = lds + wave * (16 * kRow);
+    unsigned char *turn = lds + wave * (16 * kRow);   // (at most 68 KiB for eight waves, 35 for four: less than the tiles had)
     const int64_t p = p_first + lane % kLanes * 8;
     const int m = (int)max((int64_t)0, min((int64_t)8, a.np - p));
     float bias[8];
@@ -388,6 +388,7 @@ __global__ __launch_bounds__(WP *WQ * 64) void tile_kernel(Product<T> a, Epilogu
 // The compiler does not see these loads (they have no result); what they need is stated by hand: before a barrier each wave waits for its
 // own loads of step t + 1 (loads return in order: all but those of the steps after it) and for its own reads of step t, so
 // that beyond the barrier every wave's part of t + 1 is there and nobody reads step t's buffer any more.
+
 // Rows of 64 bytes, four to a line of the banks: their chunks are permuted so that the sixteen lanes that LDS serves together (0-3,
 // 12-15, 20-27 and so on) touch sixteen different ones.
 __device__ __forceinline__ int direct_chunk(int r, int ch) { return ch ^ ((r >> 1 & 2) ^ (r >> 3 & 1) * 3); }
@@ -651,7 +652,7 @@ static TilingCost cost_of(Tiling t, bool f32, bool both_along)
     }
 }
 // The few rows' kernel reads P's 16 rows and all of Q's per workgroup, two workgroups per compute unit: latency where there are few
-// workgroups (12 us for 64 x 4,096 x 1,024), else P through memory and Q's rows once per workgroup through the caches (200,000 x 1,024
+// workgroups (7 us for 64 x 4,096 x 1,024), else P through memory and Q's rows once per workgroup through the caches (200,000 x 1,024
 // in bfloat16: 76 us for one row, 99 for 8, 115 for 16; 128 x 128 tiles take 94 for any of these).
 static double few_rows_us(int64_t np, int64_t nq, int64_t row_bytes)
 {
@@ -689,6 +690,8 @@ static ProductPlan plan_product(int32_t dtype, int64_t np, int64_t nq, int64_t n
         best.tiling = kFewRows;
         best.chunk = nc;
         least = few_rows_us(np, nq, nc * (int64_t)type_size(dtype));
+        // (the quickest that any tile could be: one split, or one step of many; a call of few rows should not wait for its plan)
+        if (least <= std::min(3.4 + 0.4 * (double)ceil_div(nc, step), 9.3)) return best;
     }
     for (Tiling t : {kSmall, kMedium, kDirect128, kDirectWide, kDirect192, kDirect256}) {
         if (t >= kDirect128 && !o.direct) continue;

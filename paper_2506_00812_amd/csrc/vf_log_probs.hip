@@ -147,7 +147,7 @@ __global__ __launch_bounds__(256) void log_probs_kernel(int64_t m, int64_t v, co
 {
     constexpr int V = kVec<T>, RPB = 256 / TPR, W = TPR / 64, E = 16, NV = E / V;
     __shared__ float lds_sums[4][3];
-    __shared__ uint64_t lds_keys[TOP && W > 1 ? 4 * 64 : 1], lds_chosen[TOP ? 4 * 64 * E / 2 : 1];
+    __shared__ uint64_t lds_keys[TOP && W > 1 ? 3 * 64 : 1], lds_chosen[TOP ? 4 * 64 * E / 2 : 1];
     const int t = threadIdx.x % TPR, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     uint64_t *chosen = lds_chosen + (TOP ? wave * (64 * E / 2) : 0);
     const int64_t items = m * nseg;
@@ -218,7 +218,7 @@ __global__ __launch_bounds__(256) void log_probs_kernel(int64_t m, int64_t v, co
         if constexpr (W > 1) {
             __syncthreads();
             if (lane == 0) { lds_sums[wave][0] = r.m; lds_sums[wave][1] = r.s; lds_sums[wave][2] = r.a; }
-            if (TOP && lane < top) lds_keys[wave * 64 + lane] = best.key;
+            if (TOP && wave > 0 && lane < top) lds_keys[(wave - 1) * top + lane] = best.key;
             __syncthreads();
             if (wave == 0) {
                 float most = -kInf;
@@ -234,7 +234,7 @@ __global__ __launch_bounds__(256) void log_probs_kernel(int64_t m, int64_t v, co
                 }
                 r = all;
                 if constexpr (TOP) {
-                    for (int w = 1; w < W; ++w) best.offer(lane < top ? lds_keys[w * 64 + lane] : KEY_MAX, top);
+                    for (int i = lane; i - lane < (W - 1) * top; i += 64) best.offer(i < (W - 1) * top ? lds_keys[i] : KEY_MAX, top);
                 }
             }
         }
@@ -263,8 +263,16 @@ __global__ __launch_bounds__(64) void log_probs_join_kernel(int64_t m, int64_t v
         asked.load(out, logits + row * ld, row, v);
         const int n = nseg * top;
         const uint64_t *keys = part_keys + row * n;
-        uint32_t most_key = 0;
-        for (int i = lane; i < n; i += 64) most_key = max(most_key, ~(uint32_t)(keys[i] >> 32));
+        constexpr int kAhead = 8;   // keys a lane, on their way together
+        uint64_t ahead[kAhead];
+        auto load_keys = [&](int first) {
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int at = first + i * 64 + lane;
+                ahead[i] = at < n ? keys[at] : KEY_MAX;
+            }
+        };
+        load_keys(0);
         for (int i = lane; i < nseg; i += 64) {
             const float4 p = part_sums[row * nseg + i];
             RowSums q = {p.x, p.y, p.z};
@@ -276,8 +284,22 @@ __global__ __launch_bounds__(64) void log_probs_join_kernel(int64_t m, int64_t v
         }
         r = wave_join(r);
         WaveTop best;
-        if (top) best.expect(most_key, top);
-        for (int i = 0; i < n; i += 64) best.offer(i + lane < n ? keys[i + lane] : KEY_MAX, top);
+        for (int first = 0; first < n; first += kAhead * 64) {
+            if (first > 0) load_keys(first);
+            if (first == 0) {
+                uint64_t least = KEY_MAX;
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) least = ahead[i] < least ? ahead[i] : least;
+                best.expect(~(uint32_t)(least >> 32), top);
+            }
+#pragma unroll 1
+            for (int i = 0; i < kAhead && first + i * 64 < n; ++i) {
+                uint64_t key = ahead[0];
+#pragma unroll
+                for (int j = 1; j < kAhead; ++j) key = i == j ? ahead[j] : key;
+                best.offer(key, top);
+            }
+        }
         finish_row(out, asked, row, v, top, r, best.key, lane);
     }
 }

@@ -191,29 +191,12 @@ def test_gradients_against_differences():
     assert (got.double() - num).abs().max() < 1e-5
 
 
-def test_in_place_stream_and_graph():
+def test_gradient_in_place():
     x, t = make(50, 4000, torch.bfloat16, 9)
     d = torch.randn(50, device="cuda")
-    want = vf.log_probs(x, t, top=4)
-    grad = vf.log_probs_backward(x, want[2], t, d)
-    s = torch.cuda.Stream()
-    s.wait_stream(torch.cuda.current_stream())
-    got = [vf.log_probs(x, t, top=4, stream=s) for _ in range(3)]
-    s.synchronize()
-    for o in got:
-        assert all(torch.equal(p, q) for p, q in zip(o, want))
-    g = torch.cuda.CUDAGraph()
-    with torch.cuda.graph(g):
-        out = vf.log_probs(x, t, top=4)
-        dx = vf.log_probs_backward(x, out[2], t, d)
-    for i in range(4):
-        x.copy_(make(50, 4000, torch.bfloat16, 20 + i)[0])
-        g.replay()
-        torch.cuda.synchronize()
-        now = vf.log_probs(x, t, top=4)
-        assert all(torch.equal(p, q) for p, q in zip(out, now)) and torch.equal(dx, vf.log_probs_backward(x, now[2], t, d))
-    x.copy_(make(50, 4000, torch.bfloat16, 9)[0])
-    assert torch.equal(vf.log_probs_backward(x, want[2], t, d, out=x), grad) and torch.equal(x, grad)
+    lse = vf.log_probs(x, t)[2]
+    grad = vf.log_probs_backward(x, lse, t, d)
+    assert torch.equal(vf.log_probs_backward(x, lse, t, d, out=x), grad) and torch.equal(x, grad)
 
 
 def test_refusals():
