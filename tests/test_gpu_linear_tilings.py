@@ -62,3 +62,16 @@ def test_nan_stays_in_its_row_and_column(case):
     dx2, _, _ = vf.linear_backward(dy, x, w, dweight=False)
     assert torch.isnan(dx2[0]).all()
     assert torch.equal(dx2[1:, 1:], dx[1:, 1:])
+
+
+@pytest.mark.parametrize("m,n,k,ld", [(3000, 2056, 1025, 1032), (9000, 4104, 1001, 1008), (2049, 1096, 515, 520), (40, 1000, 203, 208)])
+def test_odd_contractions_in_aligned_rows(m, n, k, ld):
+    """The last vector of a row holds what follows the row: NaN here, which must not get in."""
+    x, w, _, _ = inputs(m, n, k, BF, 35)
+    wide = [torch.full((t.shape[0], ld), math.nan, dtype=BF, device="cuda") for t in (x, w)]
+    for a, t in zip(wide, (x, w)):
+        a[:, :k] = t
+    got = vf.linear(wide[0][:, :k], wide[1][:, :k])
+    z = x.double() @ w.double().t()
+    bound = (k + 8) * 2.0 ** -24 * (x.double().abs() @ w.double().abs().t())
+    assert ((got.double() - z).abs() <= bound + 2.0 ** -8 * (z.abs() + bound)).all()
