@@ -7,6 +7,7 @@ There is no CPU fallback: if ``libvecflow.so`` is missing, loading fails loudly.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 import struct
 
@@ -560,7 +561,7 @@ def _vector(t, what, T, dev, n):
     """Address of a vector argument; None stays None."""
     if t is None:
         return None
-    if t.dtype != T or t.get_device() != dev or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+    if t.dtype != T or t.get_device() != dev or t.numel() != n or t.dim() != 1 or not t.is_contiguous():
         raise VecflowError(f"{what} must be a contiguous CUDA tensor [{n}] of {T} on the same device")
     return t.data_ptr()
 
@@ -573,9 +574,11 @@ def _empty(like, shape, T, stream):
         return like.new_empty(shape, dtype=T)
 
 
-def _size_of(fn, *args):
+@functools.lru_cache(maxsize=4096)
+def _size_of(name, *args):
+    """What a vf_*_workspace function says for these sizes (it depends on nothing else)."""
     n = C.c_size_t(0)
-    _check(fn(*args, C.byref(n)))
+    _check(getattr(load_library(), name)(*args, C.byref(n)))
     return n.value
 
 
@@ -611,7 +614,7 @@ def linear(x, weight, bias=None, residual=None, activation="none", save=False, o
     else:
         ldy = _matrix(out, "out", T, dev, m, n)
     z = _empty(x, (m, n), T, stream) if save else None
-    nw = _size_of(L.vf_linear_workspace, code, m, n, k, act, 0)
+    nw = _size_of("vf_linear_workspace", code, m, n, k, act, 0)
     _ws, pw = _workspace(x, nw, stream)
     _check(L.vf_linear(code, m, n, k, x.data_ptr(), ldx, weight.data_ptr(), ldw, pb, act,
                        None if residual is None else residual.data_ptr(), ldr, out.data_ptr(), ldy,
@@ -636,7 +639,7 @@ def linear_backward(dy, x, weight, z=None, activation="none", bias=True, dx=True
     gx = _empty(dy, (m, k), T, stream) if dx else None
     gw = _empty(dy, (n, k), T, stream) if dweight else None
     gb = _empty(dy, (n,), T, stream) if bias else None
-    nw = _size_of(L.vf_linear_workspace, code, m, n, k, act, 1)
+    nw = _size_of("vf_linear_workspace", code, m, n, k, act, 1)
     _ws, pw = _workspace(dy, nw, stream)
     _check(L.vf_linear_backward(code, m, n, k, dy.data_ptr(), lddy, x.data_ptr(), ldx, weight.data_ptr(), ldw,
                                 z.data_ptr() if act else None, ldz, act, gx.data_ptr() if dx else None, k,
@@ -687,7 +690,7 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, dx=True, dweight=True, d
     ldo = _matrix(out, "out", T, dev, m, d) if dx else 0
     gw = _empty(dy, (d,), T, stream) if dweight else None
     gb = _empty(dy, (d,), T, stream) if dbias else None
-    nw = _size_of(L.vf_layer_norm_workspace, code, m, d) if dweight or dbias else 0
+    nw = _size_of("vf_layer_norm_workspace", code, m, d) if dweight or dbias else 0
     _ws, pw = _workspace(dy, nw, stream)
     _check(L.vf_layer_norm_backward(code, m, d, dy.data_ptr(), lddy, x.data_ptr(), ldx, pm, pr, pg,
                                     out.data_ptr() if dx else None, ldo, gw.data_ptr() if dweight else None,
@@ -711,7 +714,7 @@ def log_probs(logits, targets=None, top=0, stream=None):
     logp, entropy, lse = _empty(logits, (3, m), f32, stream).unbind(0)
     ids = _empty(logits, (m, top), i32, stream) if top else None
     tlp = _empty(logits, (m, top), f32, stream) if top else None
-    nw = _size_of(L.vf_log_probs_workspace, code, m, v, top)
+    nw = _size_of("vf_log_probs_workspace", code, m, v, top)
     _ws, pw = _workspace(logits, nw, stream)
     _check(L.vf_log_probs(code, m, v, logits.data_ptr(), ld, pt, top, None if targets is None else logp.data_ptr(),
                           entropy.data_ptr(), lse.data_ptr(), ids.data_ptr() if top else None,

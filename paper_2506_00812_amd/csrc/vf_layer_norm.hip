@@ -140,14 +140,15 @@ __global__ __launch_bounds__(1024) void norm_forward_long_kernel(int64_t m, int6
 }
 
 // dx of the rows blockIdx.x * RPB + w, + gridDim.x * RPB, ...; PARTS: every thread also sums its columns' dy h and dy over
-// those rows, and the workgroup leaves one row of both in part [gridDim.x][2][d].  100,000 x 1,024 in bfloat16: 119 us, 5.2 TB/s, and 5 us
+// those rows, and the workgroup leaves one row of both in part [gridDim.x][2][d], or (part NULL: it is the only one) the sums
+// themselves in dweight and dbias.  100,000 x 1,024 in bfloat16: 119 us, 5.2 TB/s, and 5 us
 // for joining the partial rows.
 template <class T, int TPR, int NV, bool PARTS>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_backward_kernel(int64_t m, int d, const T *dy, int64_t lddy,
                                                                                const T *__restrict__ x, int64_t ldx,
                                                                                const float *__restrict__ mean, const float *__restrict__ rstd,
                                                                                const T *__restrict__ weight, T *dx, int64_t lddx,
-                                                                               float *__restrict__ part)
+                                                                               float *__restrict__ part, T *dweight, T *dbias)
 {
     constexpr int V = kVec<T>, RPB = TPR < 256 ? 256 / TPR : 1;
     __shared__ float lds[32];
@@ -244,7 +245,15 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_backward_kernel(in
             if (group == 0) {
 #pragma unroll
                 for (int j = 0; j < V; ++j)
-                    if (c + j < d) { pw[c + j] = aw[i][j]; pb[c + j] = ab[i][j]; }
+                    if (c + j < d) {
+                        if (part) {
+                            pw[c + j] = aw[i][j];
+                            pb[c + j] = ab[i][j];
+                        } else {
+                            if (dweight) dweight[c + j] = (T)aw[i][j];
+                            if (dbias) dbias[c + j] = (T)ab[i][j];
+                        }
+                    }
             }
         }
     }
@@ -333,12 +342,16 @@ static int64_t vectors_of(int32_t dtype, int64_t d) { return ceil_div(d, 16 / (i
 static int64_t parts_of(int32_t dtype, int64_t m, int64_t d)
 {
     const int64_t nv = vectors_of(dtype, d);
+    if (m <= (nv <= 32 ? 32 : nv <= 256 ? 8 : 0)) return 1;   // two rows a wave, or two times four: less than one more launch
     const int64_t most = std::max<int64_t>(512, std::min<int64_t>(1024, m / 16));
     if (nv <= 32) return std::min(ceil_div(m, 16), most);
     if (nv <= 256) return std::min(ceil_div(m, 4), most);
     if (nv <= 2048) return std::min(m, most);
     return std::min<int64_t>(ceil_div(m, 4), 64);
 }
+
+// Whether the only workgroup of the backward pass writes the weights' gradients itself.
+static bool sums_at_once(int32_t dtype, int64_t m, int64_t d) { return vectors_of(dtype, d) <= 256 && parts_of(dtype, m, d) == 1; }
 
 static int check_norm(const NormArgs &a)
 {
@@ -378,7 +391,7 @@ int layer_norm_workspace_impl(int32_t dtype, int64_t m, int64_t d, size_t *bytes
     VF_REQUIRE(bytes != nullptr, "layer norm: bytes is NULL");
     VF_REQUIRE(is_float_type(dtype), "layer norm: dtype must be VF_F32, VF_BF16 or VF_F16");
     VF_REQUIRE(m >= 0 && m <= kMaxExtent && d >= 1 && d <= kMaxRow, "layer norm: sizes out of range");
-    *bytes = (size_t)parts_of(dtype, m, d) * 2 * (size_t)d * 4;
+    *bytes = sums_at_once(dtype, m, d) ? 0 : (size_t)parts_of(dtype, m, d) * 2 * (size_t)d * 4;
     return VF_OK;
 }
 
@@ -390,9 +403,10 @@ int layer_norm_backward_impl(const NormArgs &a)
     VF_REQUIRE(a.y == nullptr || a.ldy >= a.d, "layer norm: lddx is less than d");
     const bool sums = a.dweight != nullptr || a.dbias != nullptr;
     const int64_t parts = parts_of(a.dtype, a.m, a.d);
-    const size_t need = sums ? (size_t)parts * 2 * (size_t)a.d * 4 : 0;
+    const bool at_once = sums_at_once(a.dtype, a.m, a.d);
+    const size_t need = sums && !at_once ? (size_t)parts * 2 * (size_t)a.d * 4 : 0;
     if (int rc = check_workspace("layer norm", a.workspace, a.workspace_bytes, need); rc != VF_OK) return rc;
-    float *part = (float *)a.workspace;
+    float *part = at_once ? nullptr : (float *)a.workspace;
     by_type(a.dtype, [&](auto *p) {
         using T = std::remove_pointer_t<decltype(p)>;
         const T *dy = (const T *)a.dy, *x = (const T *)a.x, *w = (const T *)a.weight;
@@ -405,10 +419,10 @@ int layer_norm_backward_impl(const NormArgs &a)
             const dim3 block(TPR < 256 ? 256 : TPR), grid((unsigned)parts);
             if (sums)
                 norm_backward_kernel<T, TPR, NV, true><<<grid, block, 0, a.stream>>>(a.m, (int)a.d, dy, a.lddy, x, a.ldx, a.mean,
-                                                                                     a.rstd, w, (T *)a.y, a.ldy, part);
+                                                                                     a.rstd, w, (T *)a.y, a.ldy, part, (T *)a.dweight, (T *)a.dbias);
             else if (a.y)
                 norm_backward_kernel<T, TPR, NV, false><<<grid, block, 0, a.stream>>>(a.m, (int)a.d, dy, a.lddy, x, a.ldx, a.mean,
-                                                                                      a.rstd, w, (T *)a.y, a.ldy, part);
+                                                                                      a.rstd, w, (T *)a.y, a.ldy, part, (T *)a.dweight, (T *)a.dbias);
         });
         if (!short_row) {
             if (sums)   // before dx, which may be written over dy
@@ -418,7 +432,7 @@ int layer_norm_backward_impl(const NormArgs &a)
                 norm_backward_long_kernel<T><<<dim3(grid_of(a.m)), dim3(1024), 0, a.stream>>>(a.m, a.d, dy, a.lddy, x, a.ldx, a.mean,
                                                                                                a.rstd, w, (T *)a.y, a.ldy);
         }
-        if (sums)
+        if (sums && !at_once)
             launch_join_parts<T>((int)parts, a.d, 2, part, (T *)a.dweight, (T *)a.dbias, a.stream);
     });
     VF_HIP(hipGetLastError());

@@ -576,11 +576,11 @@ __global__ __launch_bounds__(256) void product_join_kernel(int64_t np, int64_t n
 }
 
 // dz = dy act'(z), and column sums of it: blockIdx.x has 64 vectors of columns, blockIdx.y every gridDim.y-th group of four rows;
-// one partial row each.  Bound by memory: 10,000 x 4,096 in bfloat16 46 us, 5.3 TB/s.  (Computed while the products load their operands,
+// one partial row each, or (dbias given: there is one) the sums themselves.  Bound by memory: 10,000 x 4,096 in bfloat16 46 us, 5.3 TB/s.  (Computed while the products load their operands,
 // the slope would be taken once per tile that reads it.)
 template <class T, int ACT>
 __global__ __launch_bounds__(256) void slope_kernel(int64_t m, int64_t n, const T *__restrict__ dy, int64_t lddy, const T *__restrict__ z,
-                                                    int64_t ldz, T *__restrict__ dz, float *__restrict__ part)
+                                                    int64_t ldz, T *__restrict__ dz, float *__restrict__ part, T *__restrict__ dbias)
 {
     constexpr int V = kVec<T>;
     __shared__ float comb[3][V][64];
@@ -602,7 +602,7 @@ __global__ __launch_bounds__(256) void slope_kernel(int64_t m, int64_t n, const 
             if (dz) store_part(dz + row * n + c, o, cols);
         }
     }
-    if (part == nullptr) return;
+    if (part == nullptr && dbias == nullptr) return;
     if (sub > 0) {
 #pragma unroll
         for (int j = 0; j < V; ++j) comb[sub - 1][j][t] = sum[j];
@@ -611,7 +611,11 @@ __global__ __launch_bounds__(256) void slope_kernel(int64_t m, int64_t n, const 
     if (sub == 0) {
 #pragma unroll
         for (int j = 0; j < V; ++j)
-            if (j < cols) part[(int64_t)blockIdx.y * n + c + j] = (sum[j] + comb[0][j][t]) + (comb[1][j][t] + comb[2][j][t]);
+            if (j < cols) {
+                const float s = (sum[j] + comb[0][j][t]) + (comb[1][j][t] + comb[2][j][t]);
+                if (dbias) dbias[c + j] = (T)s;
+                else part[(int64_t)blockIdx.y * n + c + j] = s;
+            }
     }
 }
 
@@ -817,9 +821,9 @@ static BackwardPlan plan_backward(int32_t dtype, int64_t m, int64_t n, int64_t k
 {
     BackwardPlan b;
     const int64_t across = ceil_div(n, 64 * (16 / (int64_t)type_size(dtype)));
-    b.row_parts = std::max<int64_t>(1, std::min<int64_t>(ceil_div(m, 4), 1024 / std::max<int64_t>(1, std::min<int64_t>(across, 1024))));
+    b.row_parts = m <= 32 ? 1 : std::max<int64_t>(1, std::min<int64_t>(ceil_div(m, 4), 1024 / std::max<int64_t>(1, std::min<int64_t>(across, 1024))));
     b.dz = act == VF_ACT_NONE ? 0 : (size_t)m * n * type_size(dtype);
-    b.parts = (size_t)b.row_parts * n * 4;
+    b.parts = b.row_parts == 1 ? 0 : (size_t)b.row_parts * n * 4;   // (one: the sums are written at once, which saves a launch)
     b.product = std::max(most_bytes(dtype, k, m, n, false, true, false), most_bytes(dtype, k, n, m, false, false, false));
     return b;
 }
@@ -887,10 +891,10 @@ int linear_backward_impl(const LinearArgs &a)
             by_act(a.act, [&](auto act) {
                 slope_kernel<T, act.value><<<dim3((unsigned)across, (unsigned)b.row_parts), dim3(256), 0, a.stream>>>(
                     a.m, a.n, (const T *)a.dy, a.lddy, (const T *)a.z, a.ldz, a.act != VF_ACT_NONE && products ? made : nullptr,
-                    a.dbias ? parts : nullptr);
+                    a.dbias && b.row_parts > 1 ? parts : nullptr, b.row_parts == 1 ? (T *)a.dbias : nullptr);
             });
         }
-        if (a.dbias && a.n > 0)
+        if (a.dbias && a.n > 0 && (!rows || b.row_parts > 1))
             launch_join_parts<T>(rows ? (int)b.row_parts : 0, a.n, 1, parts, (T *)a.dbias, nullptr, a.stream);
         if (a.dx) {
             const Epilogue<T> e{nullptr, VF_ACT_NONE, nullptr, 0, (T *)a.dx, a.lddx, nullptr, 0};
