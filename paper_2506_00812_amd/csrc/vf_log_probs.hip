@@ -249,7 +249,7 @@ __global__ __launch_bounds__(256) void log_probs_kernel(int64_t m, int64_t v, co
     }
 }
 
-// One wave per row joins the segments (one row of 200,000 with eight alternatives: 7 us after the 7 of its 49 segments; both are chains of
+// One wave per row joins the segments (one row of 200,000 with eight alternatives: 5 us after the 8 of its 49 segments; both are chains of
 // dependent loads and list insertions, far from any rate).
 template <class T>
 __global__ __launch_bounds__(64) void log_probs_join_kernel(int64_t m, int64_t v, const T *__restrict__ logits, int64_t ld, int nseg,
