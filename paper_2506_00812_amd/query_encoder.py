@@ -36,8 +36,9 @@ class QueryEncoder:
         start = dict(n1w=const(width, 1.0), n1b=const(width, 0.0), w1=weight(hidden, width), b1=const(hidden, 0.0),
                      w2=weight(width, hidden), b2=const(width, 0.0), n2w=const(width, 1.0), n2b=const(width, 0.0),
                      wv=weight(dim, width), bv=const(dim, 0.0), wl=weight(n_labels, width), bl=const(n_labels, 0.0))
-        if absent is not None:
-            start["bl"][torch.as_tensor(absent, device=device)] = -torch.inf
+        gone = torch.as_tensor(() if absent is None else absent, device=device)
+        if gone.numel():     # (an empty list makes a tensor of floats, which is no index)
+            start["bl"][gone] = -torch.inf
         self.params = {k: v.to(dtype) for k, v in start.items()}
         self.names = list(start)
         self._masters = [start[k] for k in self.names] if dtype != torch.float32 else None
