@@ -71,15 +71,15 @@ class QueryEncoder:
         return vectors, ids, logp, entropy
 
     def gradients(self, x, vectors, labels, label_weight=1.0, entropy_weight=0.0):
-        """(loss [1], {name: gradient}) of mean |vector - target|^2 - label_weight mean log p(label) - entropy_weight mean
-        entropy.  vectors [m, dim]; labels int32 [m], -1 for a query without one."""
-        p, m = self.params, x.shape[0]
+        """(loss, {name: gradient}) of mean |vector - target|^2 - label_weight mean log p(label) - entropy_weight mean
+        entropy.  vectors [m, dim]; labels int32 [m], -1 for a query without one.  Of no queries at all everything is 0."""
+        p, m = self.params, max(x.shape[0], 1)
         g, (x, a, mean1, rstd1, h, z, r, mean2, rstd2) = self._body(x, save=True)
         out = vf.linear(g, p["wv"], p["bv"])
         logits = vf.linear(g, p["wl"], p["bl"])
         logp, entropy, lse = vf.log_probs(logits, labels)
         off = out.float() - vectors.float()
-        loss = off.square().sum(1).mean() - label_weight * logp.mean() - entropy_weight * entropy.mean()
+        loss = off.square().sum(1).mean() - label_weight * logp.mean() - entropy_weight * entropy.mean() if len(x) else off.sum()
         grads = {}
         d_logp = torch.full_like(logp, -label_weight / m)
         d_entropy = torch.full_like(entropy, -entropy_weight / m) if entropy_weight else None
