@@ -20,7 +20,14 @@ __all__ = ["QueryEncoder"]
 class QueryEncoder:
     """width: of the upstream embedding; dim: of the index's vectors; n_labels: its vocabulary.  dtype: of weights and
     activations; below float32 every weight has a float32 master.  state_bits: of the optimiser's moments (32 or 8).
-    absent: ids of labels that no vector carries; they are never predicted (their logits are -inf)."""
+    absent: ids of labels that no vector carries; they are never predicted (their logits are -inf).
+
+    float16 reaches down to 6e-8, above most entries of the logits' gradient (p / queries: a third of it and more would be lost at 10,000 queries
+    and labels).  There the backward pass carries everything times `scale`, a power of two in device memory; the weights' gradients are
+    divided by it in float32.  A step whose gradients are not finite is left out (it still counts for the bias corrections) and
+    halves the scale, GROWTH_STEPS good ones in a row double it."""
+
+    FIRST_SCALE, GROWTH_STEPS = 1024.0, 500
 
     def __init__(self, width, dim, n_labels, hidden=None, dtype=torch.bfloat16, state_bits=32, absent=None, seed=0, device="cuda"):
         hidden = hidden or 4 * width
@@ -48,6 +55,8 @@ class QueryEncoder:
         # no decay for biases and norms
         self._decayed = [k.startswith("w") for k in self.names]
         self.dtype, self.steps = dtype, 0
+        self.scale = torch.full((1,), self.FIRST_SCALE, device=device) if dtype == torch.float16 else None
+        self._good = torch.zeros(1, dtype=torch.int32, device=device)     # steps since the scale changed
 
     # ------------------------------------------------------------------ forward and backward
 
@@ -72,7 +81,8 @@ class QueryEncoder:
 
     def gradients(self, x, vectors, labels, label_weight=1.0, entropy_weight=0.0):
         """(loss, {name: gradient}) of mean |vector - target|^2 - label_weight mean log p(label) - entropy_weight mean
-        entropy.  vectors [m, dim]; labels int32 [m], -1 for a query without one.  Of no queries at all everything is 0."""
+        entropy.  vectors [m, dim]; labels int32 [m], -1 for a query without one.  Of no queries at all everything is 0.  Gradients
+        are of the encoder's dtype, for float16 in float32."""
         p, m = self.params, max(x.shape[0], 1)
         g, (x, a, mean1, rstd1, h, z, r, mean2, rstd2) = self._body(x, save=True)
         out = vf.linear(g, p["wv"], p["bv"])
@@ -83,24 +93,40 @@ class QueryEncoder:
         grads = {}
         d_logp = torch.full_like(logp, -label_weight / m)
         d_entropy = torch.full_like(entropy, -entropy_weight / m) if entropy_weight else None
+        d_out = off * (2.0 / m)
+        if self.scale is not None:
+            for d in (d_logp, d_out) + ((d_entropy,) if entropy_weight else ()):
+                d.mul_(self.scale)
         d_logits = vf.log_probs_backward(logits, lse, labels, d_logp, entropy=entropy if entropy_weight else None,
                                          d_entropy=d_entropy, out=logits)
         dg, grads["wl"], grads["bl"] = vf.linear_backward(d_logits, g, p["wl"])
-        dg2, grads["wv"], grads["bv"] = vf.linear_backward((off * (2.0 / m)).to(self.dtype), g, p["wv"])
+        dg2, grads["wv"], grads["bv"] = vf.linear_backward(d_out.to(self.dtype), g, p["wv"])
         dr, grads["n2w"], grads["n2b"] = vf.layer_norm_backward(dg.add_(dg2), r, mean2, rstd2, p["n2w"])
         dh, grads["w2"], grads["b2"] = vf.linear_backward(dr, h, p["w2"])
         da, grads["w1"], grads["b1"] = vf.linear_backward(dh, a, p["w1"], z=z, activation="gelu")
         # x is an input: only the weights' gradients are wanted of its norm
         _, grads["n1w"], grads["n1b"] = vf.layer_norm_backward(da, x, mean1, rstd1, p["n1w"], dx=False)
+        if self.scale is not None:
+            grads = {k: g.float() / self.scale for k, g in grads.items()}
         return loss, grads
+
+    def _adapt_scale(self, grads):
+        """int32 [1]: whether a gradient is not finite; moves the scale.  Nothing waits for the device."""
+        bad = torch.stack([~torch.isfinite(g).all() for g in grads.values()]).any().reshape(1)
+        self._good.add_(1).masked_fill_(bad, 0)
+        grow = self._good >= self.GROWTH_STEPS
+        self._good.masked_fill_(grow, 0)
+        self.scale.mul_(torch.where(bad, 0.5, torch.where(grow, 2.0, 1.0))).clamp_(1.0, 2.0 ** 24)
+        return bad.int()
 
     def train_step(self, x, vectors, labels, lr=1e-3, weight_decay=0.01, **weights):
         """One step of AdamW on the loss of `gradients`; returns the loss (a CUDA tensor)."""
         loss, grads = self.gradients(x, vectors, labels, **weights)
         self.steps += 1
+        skip = None if self.scale is None else self._adapt_scale(grads)
         vf.adamw_step([self.params[k] for k in self.names], [grads[k] for k in self.names], self._m, self._v, step=self.steps,
                       lr=lr, weight_decay=[weight_decay if d else 0.0 for d in self._decayed], masters=self._masters,
-                      m_scales=self._ms, v_scales=self._vs)
+                      m_scales=self._ms, v_scales=self._vs, skip=skip)
         return loss
 
     # ------------------------------------------------------------------ search
