@@ -362,8 +362,8 @@ int vf_index_stats(const vf_index *index, vf_stats *out);
 /*
  * y = act(z) + residual, z = x w^T + bias.
  *   x [m][k], w [n][k], bias [n] or NULL, residual [m][n] or NULL, y [m][n]; z [m][n] or NULL: the pre-activation, which
- *   vf_linear_backward reads.  y may be the residual's own memory (same ld).  k = 0: z = bias.  n, k <= 2^25; a call of
- *   2^22 output tiles and more (of 64 x 64 at the smallest) is refused.
+ *   vf_linear_backward reads.  y may be the residual's own memory (same ld).  k = 0: z = bias.  n, k <= 2^25; outputs
+ *   that are 2^22 tiles and more in every tiling there is (2^36 elements of 128 x 128 tiles) are refused, before any work is enqueued.
  */
 int vf_linear(int32_t dtype, int64_t m, int64_t n, int64_t k, const void *x, int64_t ldx, const void *w, int64_t ldw,
               const void *bias, int32_t activation, const void *residual, int64_t ldr, void *y, int64_t ldy, void *z,

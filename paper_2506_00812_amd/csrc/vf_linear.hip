@@ -666,6 +666,7 @@ static double few_rows_us(int64_t np, int64_t nq, int64_t row_bytes)
 }
 
 struct ProductPlan {
+    bool fits = true;     // false: no tiling has few enough tiles
     Tiling tiling = kSmall;
     int splits = 1;
     int64_t chunk = 0;    // elements of the contraction per split
@@ -678,6 +679,8 @@ struct Operands {
     bool costly_act;         // an epilogue with GELU or SiLU
     bool direct;             // 2-byte types; rows start on 16 bytes, and an operand contiguous along its rows has whole vectors of them
 };
+
+constexpr int64_t kMaxTiles = 1 << 22;   // and more are not launched: a launch holds fewer than 2^32 threads
 
 // The tiling and the number of splits of the contraction that should take least time.  A split costs its partial sums' way
 // through memory and one more launch (5.5 us: small products come one after the other as fast as the host can launch them); it pays where
@@ -705,6 +708,7 @@ static ProductPlan plan_product(int32_t dtype, int64_t np, int64_t nq, int64_t n
         // (10,000 x 4,096 x 1,024 with GELU: 114 us in tiles of 128 x 256, 124 in 256 x 256; without 93 and 98)
         if (o.costly_act) c.fixed += 9.0 * c.together * c.bp * c.bq / 65536 * (c.together > 1 ? 0.75 : 1);
         const int64_t tiles = ceil_div(np, c.bp) * ceil_div(nq, c.bq);
+        if (tiles >= kMaxTiles) continue;
         for (int64_t splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
             const int64_t chunk = std::max<int64_t>(step, ceil_div(ceil_div(nc, splits), step) * step);
             const int64_t used = std::max<int64_t>(1, ceil_div(nc, chunk));
@@ -725,6 +729,7 @@ static ProductPlan plan_product(int32_t dtype, int64_t np, int64_t nq, int64_t n
             }
         }
     }
+    best.fits = least > 0;
     return best;
 }
 
@@ -771,7 +776,6 @@ static int run_product(int32_t dtype, const T *P, int64_t ldp, int64_t np, const
     }
     const TilingCost c = cost_of(plan.tiling, dtype == VF_F32, PC && QC);
     const int64_t tiles = ceil_div(np, c.bp) * ceil_div(nq, c.bq);
-    VF_REQUIRE(tiles < (1 << 22), "linear: too many output tiles in one call");   // (a launch holds fewer than 2^32 threads)
     const dim3 grid((unsigned)tiles, (unsigned)plan.splits);
     int rc = VF_OK;
     if (plan.tiling == kSmall) {
@@ -830,6 +834,8 @@ static BackwardPlan plan_backward(int32_t dtype, int64_t m, int64_t n, int64_t k
 
 constexpr int64_t kMaxWidth = 1 << 25;   // of n and k: kernels give up to 64 threads to a column, a launch holds fewer than 2^32
 
+static const char *const kTooManyTiles = "linear: too many output tiles in one call";
+
 static int check_sizes(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t act)
 {
     VF_REQUIRE(is_float_type(dtype), "linear: dtype must be VF_F32, VF_BF16 or VF_F16");
@@ -855,6 +861,7 @@ int linear_impl(const LinearArgs &a)
     VF_REQUIRE(a.ldx >= a.k && a.ldw >= a.k, "linear: ldx or ldw is less than k");
     VF_REQUIRE(a.ldy >= a.n && (!a.z || a.ldz >= a.n) && (!a.residual || a.ldr >= a.n), "linear: ldy, ldz or ldr is less than n");
     const ProductPlan plan = plan_product(a.dtype, a.n, a.m, a.k, {true, true, costly(a.act), direct_rows(a.dtype, a.x, a.ldx) && direct_rows(a.dtype, a.w, a.ldw)});
+    VF_REQUIRE(plan.fits, kTooManyTiles);
     if (int rc = check_workspace("linear", a.workspace, a.workspace_bytes, plan.bytes); rc != VF_OK) return rc;
     int rc = VF_OK;
     by_type(a.dtype, [&](auto *t) {
@@ -877,20 +884,30 @@ int linear_backward_impl(const LinearArgs &a)
     VF_REQUIRE(!a.dw || ((a.x || !rows || a.k == 0) && a.ldx >= a.k && a.lddw >= a.k), "linear: dw needs x, and ldx and lddw of at least k");
     const BackwardPlan b = plan_backward(a.dtype, a.m, a.n, a.k, a.act);
     if (int rc = check_workspace("linear", a.workspace, a.workspace_bytes, b.total()); rc != VF_OK) return rc;
+    // both products are planned before anything is launched: a call that is refused has changed nothing
+    const bool none = a.act == VF_ACT_NONE;
+    const void *dz_at = none ? a.dy : a.workspace;
+    const int64_t lddz = none ? a.lddy : a.n;
+    const bool dz_rows = direct_rows(a.dtype, dz_at, lddz);
+    ProductPlan plan_dx, plan_dw;
+    if (a.dx) plan_dx = plan_product(a.dtype, a.k, a.m, a.n, {false, true, false, a.k % 8 == 0 && direct_rows(a.dtype, a.w, a.ldw) && dz_rows});
+    if (a.dw)
+        plan_dw = plan_product(a.dtype, a.k, a.n, a.m,
+                               {false, false, false, a.k % 8 == 0 && a.n % 8 == 0 && direct_rows(a.dtype, a.x, a.ldx) && dz_rows});
+    VF_REQUIRE(plan_dx.fits && plan_dw.fits, kTooManyTiles);
     int rc = VF_OK;
     by_type(a.dtype, [&](auto *t) {
         using T = std::remove_pointer_t<decltype(t)>;
         T *made = (T *)a.workspace;
         float *parts = (float *)((char *)a.workspace + rounded(b.dz));
         float *splits = (float *)((char *)parts + rounded(b.parts));
-        const T *dz = a.act == VF_ACT_NONE ? (const T *)a.dy : made;
-        const int64_t lddz = a.act == VF_ACT_NONE ? a.lddy : a.n;
+        const T *dz = (const T *)dz_at;
         const bool products = (a.dx || a.dw) && a.k > 0;
-        if (rows && (a.dbias || (a.act != VF_ACT_NONE && products))) {
+        if (rows && (a.dbias || (!none && products))) {
             const int64_t across = ceil_div(a.n, 64 * kVec<T>);
             by_act(a.act, [&](auto act) {
                 slope_kernel<T, act.value><<<dim3((unsigned)across, (unsigned)b.row_parts), dim3(256), 0, a.stream>>>(
-                    a.m, a.n, (const T *)a.dy, a.lddy, (const T *)a.z, a.ldz, a.act != VF_ACT_NONE && products ? made : nullptr,
+                    a.m, a.n, (const T *)a.dy, a.lddy, (const T *)a.z, a.ldz, !none && products ? made : nullptr,
                     a.dbias && b.row_parts > 1 ? parts : nullptr, b.row_parts == 1 ? (T *)a.dbias : nullptr);
             });
         }
@@ -898,15 +915,11 @@ int linear_backward_impl(const LinearArgs &a)
             launch_join_parts<T>(rows ? (int)b.row_parts : 0, a.n, 1, parts, (T *)a.dbias, nullptr, a.stream);
         if (a.dx) {
             const Epilogue<T> e{nullptr, VF_ACT_NONE, nullptr, 0, (T *)a.dx, a.lddx, nullptr, 0};
-            const bool direct = a.k % 8 == 0 && direct_rows(a.dtype, a.w, a.ldw) && direct_rows(a.dtype, dz, lddz);
-            rc = run_product<T, false, true>(a.dtype, (const T *)a.w, a.ldw, a.k, dz, lddz, a.m, a.n, e,
-                                             plan_product(a.dtype, a.k, a.m, a.n, {false, true, false, direct}), splits, a.stream);
+            rc = run_product<T, false, true>(a.dtype, (const T *)a.w, a.ldw, a.k, dz, lddz, a.m, a.n, e, plan_dx, splits, a.stream);
         }
         if (a.dw && rc == VF_OK) {
             const Epilogue<T> e{nullptr, VF_ACT_NONE, nullptr, 0, (T *)a.dw, a.lddw, nullptr, 0};
-            const bool direct = a.k % 8 == 0 && a.n % 8 == 0 && direct_rows(a.dtype, a.x, a.ldx) && direct_rows(a.dtype, dz, lddz);
-            rc = run_product<T, false, false>(a.dtype, (const T *)a.x, a.ldx, a.k, dz, lddz, a.n, a.m, e,
-                                              plan_product(a.dtype, a.k, a.n, a.m, {false, false, false, direct}), splits, a.stream);
+            rc = run_product<T, false, false>(a.dtype, (const T *)a.x, a.ldx, a.k, dz, lddz, a.n, a.m, e, plan_dw, splits, a.stream);
         }
     });
     if (rc == VF_OK) VF_HIP(hipGetLastError());
@@ -919,6 +932,7 @@ int debug_linear_impl(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t pr
     VF_REQUIRE(product >= 0 && product <= 2 && tiling && splits, "linear: product must be 0 .. 2, tiling and splits not NULL");
     const Operands o{product == 0, product <= 1, false, direct != 0 && dtype != VF_F32};
     const ProductPlan p = product == 0 ? plan_product(dtype, n, m, k, o) : product == 1 ? plan_product(dtype, k, m, n, o) : plan_product(dtype, k, n, m, o);
+    VF_REQUIRE(p.fits, kTooManyTiles);
     *tiling = p.tiling;
     *splits = p.splits;
     return VF_OK;
