@@ -350,7 +350,8 @@ int vf_index_stats(const vf_index *index, vf_stats *out);
  *     device memory of its own it takes it as `workspace` (16-byte aligned); the *_workspace function says how much (0: none,
  *     NULL is fine), and the memory is free again once the call's work has completed.
  *   - Results do not depend on what else runs: no floating-point atomics, every sum in a fixed order.
- *   - Outputs must not overlap inputs or each other, but for the cases named below.
+ *   - Outputs must not overlap inputs or each other, but for the cases named below.  The matrices of the linear layer and the norm, and
+ *     dlogits, are checked before anything is enqueued (slices with unlike row distances aside); an input that a call does not read may lie anywhere.
  */
 #define VF_BF16 2
 #define VF_F16 3

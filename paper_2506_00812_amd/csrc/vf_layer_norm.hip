@@ -370,6 +370,14 @@ int layer_norm_impl(const NormArgs &a)
     VF_REQUIRE(a.m == 0 || a.y != nullptr, "layer norm: y is NULL");
     VF_REQUIRE(a.ldy >= a.d, "layer norm: ldy is less than d");
     if (a.m == 0) return VF_OK;
+    const size_t size = type_size(a.dtype);
+    const Region x = region(a.x, a.m, a.d, a.ldx, size), y = region(a.y, a.m, a.d, a.ldy, size);
+    const Region mean = region(a.mean, a.m, 4), rstd = region(a.rstd, a.m, 4);
+    VF_REQUIRE(y.same(x) || !overlap(y, x), "layer norm: y overlaps x and is not it");
+    VF_REQUIRE(!overlap(mean, x) && !overlap(rstd, x), "layer norm: mean or rstd overlaps x");
+    for (const Region &in : {region(a.weight, a.d, size), region(a.bias, a.d, size)})
+        VF_REQUIRE(!overlap(y, in) && !overlap(mean, in) && !overlap(rstd, in), "layer norm: an output overlaps weight or bias");
+    VF_REQUIRE(!overlap(mean, y) && !overlap(rstd, y) && !overlap(mean, rstd), "layer norm: y, mean and rstd overlap each other");
     by_type(a.dtype, [&](auto *p) {
         using T = std::remove_pointer_t<decltype(p)>;
         const bool short_row = by_row(vectors_of(a.dtype, a.d), [&](auto tpr, auto nv) {
@@ -406,6 +414,14 @@ int layer_norm_backward_impl(const NormArgs &a)
     const bool at_once = sums_at_once(a.dtype, a.m, a.d);
     const size_t need = sums && !at_once ? (size_t)parts * 2 * (size_t)a.d * 4 : 0;
     if (int rc = check_workspace("layer norm", a.workspace, a.workspace_bytes, need); rc != VF_OK) return rc;
+    const size_t size = type_size(a.dtype);
+    const Region dy = region(a.dy, a.m, a.d, a.lddy, size), dx = region(a.y, a.m, a.d, a.ldy, size);
+    const Region dw = region(a.dweight, a.d, size), db = region(a.dbias, a.d, size);
+    VF_REQUIRE(dx.same(dy) || !overlap(dx, dy), "layer norm: dx overlaps dy and is not it");
+    VF_REQUIRE(!overlap(dw, dy) && !overlap(db, dy), "layer norm: dweight or dbias overlaps dy");
+    for (const Region &in : {region(a.x, a.m, a.d, a.ldx, size), region(a.mean, a.m, 4), region(a.rstd, a.m, 4), region(a.weight, a.d, size)})
+        VF_REQUIRE(!overlap(dx, in) && !overlap(dw, in) && !overlap(db, in), "layer norm: dx, dweight or dbias overlaps an input");
+    VF_REQUIRE(!overlap(dx, dw) && !overlap(dx, db) && !overlap(dw, db), "layer norm: dx, dweight and dbias overlap each other");
     float *part = at_once ? nullptr : (float *)a.workspace;
     by_type(a.dtype, [&](auto *p) {
         using T = std::remove_pointer_t<decltype(p)>;

@@ -863,6 +863,12 @@ int linear_impl(const LinearArgs &a)
     const ProductPlan plan = plan_product(a.dtype, a.n, a.m, a.k, {true, true, costly(a.act), direct_rows(a.dtype, a.x, a.ldx) && direct_rows(a.dtype, a.w, a.ldw)});
     VF_REQUIRE(plan.fits, kTooManyTiles);
     if (int rc = check_workspace("linear", a.workspace, a.workspace_bytes, plan.bytes); rc != VF_OK) return rc;
+    const size_t size = type_size(a.dtype);
+    const Region y = region(a.y, a.m, a.n, a.ldy, size), z = region(a.z, a.m, a.n, a.ldz, size), r = region(a.residual, a.m, a.n, a.ldr, size);
+    for (const Region &in : {region(a.x, a.m, a.k, a.ldx, size), region(a.w, a.n, a.k, a.ldw, size), region(a.bias, a.n, size)})
+        VF_REQUIRE(!overlap(y, in) && !overlap(z, in), "linear: y or z overlaps an input");
+    VF_REQUIRE(y.same(r) || !overlap(y, r), "linear: y overlaps the residual and is not it");
+    VF_REQUIRE(!overlap(z, r) && !overlap(z, y), "linear: z overlaps y or the residual");
     int rc = VF_OK;
     by_type(a.dtype, [&](auto *t) {
         using T = std::remove_pointer_t<decltype(t)>;
@@ -895,6 +901,12 @@ int linear_backward_impl(const LinearArgs &a)
         plan_dw = plan_product(a.dtype, a.k, a.n, a.m,
                                {false, false, false, a.k % 8 == 0 && a.n % 8 == 0 && direct_rows(a.dtype, a.x, a.ldx) && dz_rows});
     VF_REQUIRE(plan_dx.fits && plan_dw.fits, kTooManyTiles);
+    const size_t size = type_size(a.dtype);
+    const Region dx = region(a.dx, a.m, a.k, a.lddx, size), dw = region(a.dw, a.n, a.k, a.lddw, size), db = region(a.dbias, a.n, size);
+    for (const Region &in : {region(a.dy, a.m, a.n, a.lddy, size), region(a.dx ? a.w : nullptr, a.n, a.k, a.ldw, size),
+                             region(a.dw ? a.x : nullptr, a.m, a.k, a.ldx, size), region(a.act != VF_ACT_NONE ? a.z : nullptr, a.m, a.n, a.ldz, size)})
+        VF_REQUIRE(!overlap(dx, in) && !overlap(dw, in) && !overlap(db, in), "linear: dx, dw or dbias overlaps an input");
+    VF_REQUIRE(!overlap(dx, dw) && !overlap(dx, db) && !overlap(dw, db), "linear: dx, dw and dbias overlap each other");
     int rc = VF_OK;
     by_type(a.dtype, [&](auto *t) {
         using T = std::remove_pointer_t<decltype(t)>;

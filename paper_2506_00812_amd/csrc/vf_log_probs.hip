@@ -417,6 +417,10 @@ int log_probs_backward_impl(const LogProbArgs &a)
     VF_REQUIRE((a.entropy == nullptr) == (a.d_entropy == nullptr), "log probs: entropy and d_entropy go together");
     if (a.m == 0) return VF_OK;
     VF_REQUIRE(a.logits && a.lse && a.dlogits, "log probs: logits, lse or dlogits is NULL");
+    const Region x = region(a.logits, a.m, a.v, a.ld, type_size(a.dtype)), dx = region(a.dlogits, a.m, a.v, a.ldd, type_size(a.dtype));
+    VF_REQUIRE(dx.same(x) || !overlap(dx, x), "log probs: dlogits overlaps the logits and is not them");
+    for (const void *in : {(const void *)a.lse, (const void *)a.targets, (const void *)a.d_logp, (const void *)a.entropy, (const void *)a.d_entropy})
+        VF_REQUIRE(!overlap(dx, region(in, a.m, 4)), "log probs: dlogits overlaps an input");
     by_type(a.dtype, [&](auto *q) {
         using T = std::remove_pointer_t<decltype(q)>;
         const int64_t nv = ceil_div(a.v, kVec<T>);

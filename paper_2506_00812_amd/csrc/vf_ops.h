@@ -39,6 +39,35 @@ inline int check_workspace(const char *op, const void *workspace, size_t have, s
     return VF_OK;
 }
 
+// A matrix argument in memory: rows of `width` bytes, `ld` bytes apart.  A vector is one row.
+struct Region {
+    uintptr_t at;
+    int64_t rows, width, ld;
+    bool same(const Region &o) const { return at == o.at && rows == o.rows && width == o.width && ld == o.ld; }
+};
+inline Region region(const void *p, int64_t rows, int64_t cols, int64_t ld, size_t size)
+{
+    if (p == nullptr || cols <= 0) return {0, 0, 0, 0};
+    const int64_t s = (int64_t)size;
+    if (rows == 1 || ld == cols) return {(uintptr_t)p, rows > 0, rows * cols * s, rows * cols * s};
+    return {(uintptr_t)p, rows, cols * s, ld * s};
+}
+inline Region region(const void *p, int64_t n, size_t size) { return region(p, 1, n, n, size); }
+
+// Whether two regions share a byte.  (Of two slices with unlike row distances it is not asked: that takes a walk over their rows.)
+inline bool overlap(Region a, Region b)
+{
+    if (a.rows == 0 || b.rows == 0) return false;
+    if (b.at < a.at) std::swap(a, b);
+    const int64_t d = (int64_t)(b.at - a.at);
+    if (d >= (a.rows - 1) * a.ld + a.width) return false;
+    // b begins in row d / ld of a, or between that one and the next; what begins between them reaches the next one in its first row or never
+    if (a.rows == 1) return true;
+    if (b.rows > 1 && a.ld != b.ld) return false;
+    const int64_t i = d / a.ld, r = d % a.ld;
+    return r < a.width || (i + 1 < a.rows && r + b.width > a.ld);
+}
+
 // A vector at an address that is aligned to an element only: one 16-byte load or store all the same (global memory
 // takes any alignment; rows cut out of a wider matrix start anywhere).
 template <class V, class T> __device__ __forceinline__ V load_vec(const T *p)
