@@ -89,7 +89,7 @@ __device__ __forceinline__ void finish(const Epilogue<T> &e, int64_t q, int64_t 
     if (e.act != VF_ACT_NONE)
         by_act(e.act, [&](auto act) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) v[i] = act_value<act.value>(v[i]);
+            for (int i = 0; i < N; ++i) v[i] = act_value<act.value, T>(v[i]);
         });
     if (e.residual) {
         load_row(e.residual + q * e.ldr + p, n, u);
@@ -595,7 +595,7 @@ __global__ __launch_bounds__(256) void slope_kernel(int64_t m, int64_t n, const 
             if (ACT != VF_ACT_NONE) u = load_part(z + row * ldz + c, cols, (T)0.f);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const float d = ACT == VF_ACT_NONE ? (float)g[j] : (float)g[j] * act_slope<ACT>((float)u[j]);
+                const float d = ACT == VF_ACT_NONE ? (float)g[j] : (float)g[j] * act_slope<ACT, T>((float)u[j]);
                 sum[j] += d;
                 o[j] = (T)d;
             }

@@ -141,47 +141,74 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v)
 __device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * 1.4426950408889634f); }
 __device__ __forceinline__ float rcp_fast(float x) { return __builtin_amdgcn_rcpf(x); }
 
-// Phi(-|z|), the tail of the normal distribution, and exp(-z^2 / 2): Hastings' polynomial in t = 1 / (1 + 0.2316419 |z|) times the
-// density (Abramowitz and Stegun, Handbook of Mathematical Functions, 26.2.17; off by less than 7.5e-8; the coefficients here hold
-// the density's 1 / sqrt(2 pi)).  With erff, three times the instructions, an epilogue of 10,000 x 4,096 outputs took 50 us of a product's
-// 145; with this one 25.
-__device__ __forceinline__ float normal_tail(float z, float &density)
+// Phi(-|z|), the tail of the normal distribution, and exp(-z^2 / 2), for results of type T: a polynomial in t = 1 / (1 + c |z|) times the
+// density.
+//   2 bytes: Hastings' (Abramowitz and Stegun, Handbook of Mathematical Functions, 26.2.17; off by less than 7.5e-8, a 2^13th of what
+//   bfloat16 rounds by; the coefficients here hold the density's 1 / sqrt(2 pi)).  With erff, three times the instructions, an epilogue of
+//   10,000 x 4,096 outputs took 50 us of a product's 145; with this one 25.
+//   float32: Hastings' loses the tail's digits (0.4 % at z = -6).  A fit of our own to Phi(-z) exp(z^2 / 2) / t over all z >= 0, least squares
+//   reweighted towards the largest relative error, 3.2e-8 before rounding (c = 0.32: the best of degree 9), 3.3e-7 after.
+template <class T> __device__ __forceinline__ float normal_tail(float z, float &density)
 {
+    density = __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f);
+    if constexpr (std::is_same_v<T, float>) {
+        const float t = rcp_fast(__builtin_fmaf(0.32f, fabsf(z), 1.f));
+        float s = __builtin_fmaf(t, -0.02107816f, 0.0954072177f);
+    s = __builtin_fmaf(t, s, -0.146707371f);
+    s = __builtin_fmaf(t, s, 0.0653279349f);
+    s = __builtin_fmaf(t, s, -0.00937751681f);
+    s = __builtin_fmaf(t, s, 0.058653947f);
+    s = __builtin_fmaf(t, s, 0.0878291056f);
+    s = __builtin_fmaf(t, s, 0.114622362f);
+    s = __builtin_fmaf(t, s, 0.127660945f);
+    s = __builtin_fmaf(t, s, 0.127661526f);
+        return s * t * density;
+    }
     constexpr float r = 0.39894228040143268f;
     const float t = rcp_fast(__builtin_fmaf(0.2316419f, fabsf(z), 1.f));
-    density = __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f);
     float s = __builtin_fmaf(t, 1.330274429f * r, -1.821255978f * r);
     s = __builtin_fmaf(t, s, 1.781477937f * r);
     s = __builtin_fmaf(t, s, -0.356563782f * r);
     s = __builtin_fmaf(t, s, 0.319381530f * r);
     return s * t * density;
 }
+// 1 / (1 + exp(-z)), for results of type T.  float32: with the exponent in two parts, so that its rounding does not grow with |z|.
+template <class T> __device__ __forceinline__ float sigmoid(float z)
+{
+    if constexpr (std::is_same_v<T, float>) {
+        const float x = z < -128.f ? 128.f : z > 128.f ? -128.f : -z;   // (beyond it is 0 or 1; NaN stays NaN)
+        const float hi = x * 1.4426950408889634f;
+        const float lo = __builtin_fmaf(x, 1.4426950408889634f, -hi) + x * 1.92596299e-8f;   // log2 e is these two numbers
+        return rcp_fast(1.f + __builtin_amdgcn_exp2f(hi) * __builtin_fmaf(lo, 0.69314718f, 1.f));
+    }
+    return rcp_fast(1.f + exp_fast(-z));
+}
 
 // The activations at infinite z are their limits: a factor that vanishes meets the largest finite number, not an infinity.  NaN stays
 // NaN (the other factor still has it).
 constexpr float kFltMax = 3.4028234663852886e38f;
-template <int ACT> __device__ __forceinline__ float act_value(float z)
+template <int ACT, class T> __device__ __forceinline__ float act_value(float z)
 {
     if constexpr (ACT == VF_ACT_NONE) return z;
     if constexpr (ACT == VF_ACT_RELU) return z < 0.f ? 0.f : z;
     if constexpr (ACT == VF_ACT_GELU) {   // z Phi(z) = max(z, 0) - |z| Phi(-|z|)
         float density;
-        const float tail = normal_tail(z, density);
+        const float tail = normal_tail<T>(z, density);
         return __builtin_fmaf(-fminf(fabsf(z), kFltMax), tail, fmaxf(z, 0.f));
     }
-    return fmaxf(z, -kFltMax) * rcp_fast(1.f + exp_fast(-z));
+    return fmaxf(z, -kFltMax) * sigmoid<T>(z);
 }
-template <int ACT> __device__ __forceinline__ float act_slope(float z)
+template <int ACT, class T> __device__ __forceinline__ float act_slope(float z)
 {
     if constexpr (ACT == VF_ACT_NONE) return 1.f;
     if constexpr (ACT == VF_ACT_RELU) return z > 0.f ? 1.f : z != z ? z : 0.f;
     const float u = __builtin_amdgcn_fmed3f(z, -kFltMax, kFltMax);
     if constexpr (ACT == VF_ACT_GELU) {
         float density;
-        const float tail = normal_tail(z, density);
+        const float tail = normal_tail<T>(z, density);
         return __builtin_fmaf(u * 0.39894228040143268f, density, z > 0.f ? 1.f - tail : tail);
     }
-    const float a = rcp_fast(1.f + exp_fast(-z));
+    const float a = sigmoid<T>(z);
     return a * __builtin_fmaf(u, 1.f - a, 1.f);
 }
 // Calls fn with the activation as a constant.
