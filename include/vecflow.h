@@ -425,7 +425,8 @@ int vf_log_probs(int32_t dtype, int64_t m, int64_t v, const void *logits, int64_
                  size_t workspace_bytes, void *hip_stream);
 /*
  * dlogits_j = d_logp (1[j = target] - p_j) - d_entropy p_j (log p_j + entropy), [m][v] of dtype; lse (and entropy) as
- * vf_log_probs left them.  d_logp and targets NULL: no such term; d_entropy and entropy NULL: no such term.  Rows without a label
+ * vf_log_probs left them.  p_j = exp(x_j - lse): lse's own rounding, up to 2^-24 |lse|, is a relative error that all p of a row share (logits
+ * around 10^4: 6e-4; vf_log_probs itself has no such error).  Far from 0 take an offset off the logits first: nothing else depends on it.  d_logp and targets NULL: no such term; d_entropy and entropy NULL: no such term.  Rows without a label
  * left get zeros.  dlogits may be the logits' own memory (same ld).
  */
 int vf_log_probs_backward(int32_t dtype, int64_t m, int64_t v, const void *logits, int64_t ld, const float *lse,

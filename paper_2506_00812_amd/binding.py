@@ -726,7 +726,7 @@ def log_probs(logits, targets=None, top=0, stream=None):
 
 def log_probs_backward(logits, lse, targets=None, d_logp=None, entropy=None, d_entropy=None, out=None, stream=None):
     """Gradient with respect to the logits from those of logp and entropy (vf_log_probs_backward); `out` may be the
-    logits' own memory."""
+    logits' own memory.  p = exp(logits - lse) has lse's rounding, 2^-24 |lse|, as a relative error."""
     L = load_library()
     code, T, dev, handle = _first(logits, "logits", stream)
     ld = _matrix(logits, "logits", T, dev)
