@@ -425,9 +425,10 @@ template <class T, bool ALONG_C, int ROWS> __device__ __forceinline__ Vec<T> dir
 }
 
 // BP x BQ outputs per workgroup of WP x WQ waves.  Bound by the matrix cores' clock under load and by how evenly the tiles fill 256
-// compute units.  bfloat16: 8,192 x 4,096 x 2,048 forward 114 us, dx 103 us in tiles of 256 x 256 (1,200 - 1,330 TFLOP/s, the library's
-// large square products 1,380 - 1,490); 10,000 x 4,096 x 1,024 forward 94 us, dx 73, dw 72 (890 - 1,160; the library 88, 79 and
-// 124).  A smaller tile reads more of its operands per product from L2: 128 x 128 takes 15 - 30 % longer where the tiles are many.
+// compute units.  bfloat16, bare products one after the other: 8,192 x 4,096 x 2,048 forward 114 us, dx 103, dw 134 with its join (the library 96, 104
+// and 131); 10,000 x 4,096 x 1,024 forward 95 us, dx 76, dw 84 with its join (880 - 1,100 TFLOP/s; the library 87 - 95, 82 and 114).  In such
+// a product with GELU and z the matrix cores are busy for a third of the cycles, in its dx and dw for half.  Rows 8,192 apart, along c on
+// both sides, are slow: 8,192^3 forward 1,225 us, dx 809 (the library 673 and 787).  A smaller tile reads more of its operands per product from L2: 128 x 128 takes 15 - 30 % longer where the tiles are many.
 template <class T, bool PC, bool QC, int BP, int BQ, int WP, int WQ, int STEPS>
 __global__ __launch_bounds__(WP *WQ * 64, 2) void direct_kernel(Product<T> a, Epilogue<T> e)
 {
@@ -576,8 +577,11 @@ __global__ __launch_bounds__(256) void product_join_kernel(int64_t np, int64_t n
 }
 
 // dz = dy act'(z), and column sums of it: blockIdx.x has 64 vectors of columns, blockIdx.y every gridDim.y-th group of four rows;
-// one partial row each, or (dbias given: there is one) the sums themselves.  Bound by memory: 10,000 x 4,096 in bfloat16 46 us, 5.3 TB/s.  (Computed while the products load their operands,
-// the slope would be taken once per tile that reads it.)
+// one partial row each, or (dbias given: there is one) the sums themselves.  Bound by memory: 10,000 x 4,096 in bfloat16 47 us, 5.2 TB/s.  (Computed
+// while the products load their operands, the slope would be taken once per tile that reads it.)
+// dz is rounded to T, which the matrix cores take beside w and x; the sums are not.  That rounding is all that dx and dw differ by from ones of
+// an unrounded dz: 0.0024 of their size instead of the 0.0017 of their own rounding (bfloat16).  Two terms per dz would hold it and double both
+// products; a caller who needs more digits calls with float32.
 template <class T, int ACT>
 __global__ __launch_bounds__(256) void slope_kernel(int64_t m, int64_t n, const T *__restrict__ dy, int64_t lddy, const T *__restrict__ z,
                                                     int64_t ldz, T *__restrict__ dz, float *__restrict__ part, T *__restrict__ dbias)
@@ -633,9 +637,9 @@ enum Tiling {
 };
 
 // What a tiling costs, in microseconds: `step` per 128 bytes of the contraction with a compute unit full of `together` workgroups, at
-// least `alone` however few there are; `fixed` per workgroup for its first loads and its stores.  Fitted to 2,000 timings: 40 sizes
-// from 32 x 1,024 x 1,024 to 10,000 x 4,096 x 1,024, each product, every tiling and 1 to 32 splits; the model is within 15 % of half
-// of them, and what it picks takes 3 % longer than the best of all on average.
+// least `alone` however few there are; `fixed` per workgroup for its first loads and its stores.  Fitted to 2,255 timings: 39 sizes
+// from 32 x 1,024 x 1,024 to 8,192 x 4,096 x 2,048, each product, every tiling and 1 to 32 splits; what it picks takes 3.4 % longer than the best of
+// all on average, more than 10 % for 16 of 117 products, 53 % at worst (64 x 4,096 -> 128: 16.3 us for 10.7).
 struct TilingCost {
     int bp, bq, together;
     double step, alone, fixed;
