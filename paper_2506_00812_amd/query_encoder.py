@@ -76,7 +76,8 @@ class QueryEncoder:
         p = self.params
         g = self._body(x)
         vectors = vf.linear(g, p["wv"], p["bv"])
-        _, entropy, _, ids, logp = vf.log_probs(vf.linear(g, p["wl"], p["bl"]), top=top)
+        _, entropy, _, *labels = vf.log_probs(vf.linear(g, p["wl"], p["bl"]), top=top)
+        ids, logp = labels or (entropy.new_empty((len(x), 0), dtype=torch.int32), entropy.new_empty((len(x), 0)))     # (none were asked for)
         return vectors, ids, logp, entropy
 
     def gradients(self, x, vectors, labels, label_weight=1.0, entropy_weight=0.0):

@@ -72,3 +72,12 @@ def test_other_types_have_no_scale():
         x, y, t = batch(16, 24, 12, 10)
         _, grads = enc.gradients(x.to(dtype), y, t)
         assert enc.scale is None and all(g.dtype == dtype for g in grads.values())
+
+
+def test_no_labels_asked_for():
+    enc = QueryEncoder(24, 12, 10, hidden=48, dtype=torch.float32)
+    x, _, _ = batch(16, 24, 12, 10)
+    vectors, ids, logp, entropy = enc.encode(x, top=0)
+    want = enc.encode(x, top=2)
+    assert ids.shape == logp.shape == (16, 0) and ids.dtype == torch.int32 and torch.equal(vectors, want[0])
+    assert (entropy - want[3]).abs().max() < 1e-5
