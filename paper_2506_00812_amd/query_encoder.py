@@ -84,6 +84,10 @@ class QueryEncoder:
         """(loss, {name: gradient}) of mean |vector - target|^2 - label_weight mean log p(label) - entropy_weight mean
         entropy.  vectors [m, dim]; labels int32 [m], -1 for a query without one.  Of no queries at all everything is 0.  Gradients
         are of the encoder's dtype, for float16 in float32."""
+        return self._gradients(x, vectors, labels, label_weight, entropy_weight)[:2]
+
+    def _gradients(self, x, vectors, labels, label_weight=1.0, entropy_weight=0.0):
+        """The same, and for float16 the one tensor that holds all gradients."""
         p, m = self.params, max(x.shape[0], 1)
         g, (x, a, mean1, rstd1, h, z, r, mean2, rstd2) = self._body(x, save=True)
         out = vf.linear(g, p["wv"], p["bv"])
@@ -107,13 +111,15 @@ class QueryEncoder:
         da, grads["w1"], grads["b1"] = vf.linear_backward(dh, a, p["w1"], z=z, activation="gelu")
         # x is an input: only the weights' gradients are wanted of its norm
         _, grads["n1w"], grads["n1b"] = vf.layer_norm_backward(da, x, mean1, rstd1, p["n1w"], dx=False)
-        if self.scale is not None:
-            grads = {k: g.float() / self.scale for k, g in grads.items()}
-        return loss, grads
+        if self.scale is None:
+            return loss, grads, None
+        flat = torch.cat([t.flatten() for t in grads.values()]).float().div_(self.scale)
+        parts = flat.split([t.numel() for t in grads.values()])
+        return loss, {k: part.view_as(t) for (k, t), part in zip(grads.items(), parts)}, flat
 
-    def _adapt_scale(self, grads):
+    def _adapt_scale(self, flat):
         """int32 [1]: whether a gradient is not finite; moves the scale.  Nothing waits for the device."""
-        bad = torch.stack([~torch.isfinite(g).all() for g in grads.values()]).any().reshape(1)
+        bad = ~torch.isfinite(flat).all().reshape(1)
         self._good.add_(1).masked_fill_(bad, 0)
         grow = self._good >= self.GROWTH_STEPS
         self._good.masked_fill_(grow, 0)
@@ -122,9 +128,9 @@ class QueryEncoder:
 
     def train_step(self, x, vectors, labels, lr=1e-3, weight_decay=0.01, **weights):
         """One step of AdamW on the loss of `gradients`; returns the loss (a CUDA tensor)."""
-        loss, grads = self.gradients(x, vectors, labels, **weights)
+        loss, grads, flat = self._gradients(x, vectors, labels, **weights)
         self.steps += 1
-        skip = None if self.scale is None else self._adapt_scale(grads)
+        skip = None if flat is None else self._adapt_scale(flat)
         vf.adamw_step([self.params[k] for k in self.names], [grads[k] for k in self.names], self._m, self._v, step=self.steps,
                       lr=lr, weight_decay=[weight_decay if d else 0.0 for d in self._decayed], masters=self._masters,
                       m_scales=self._ms, v_scales=self._vs, skip=skip)
