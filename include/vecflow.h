@@ -474,6 +474,98 @@ int vf_adamw_moments(const vf_adamw_tensor *tensors, int32_t n_tensors, float *c
                      void *hip_stream);
 
 /*
+ * The gated layer y = act(z_gate) z_up, z = x w^T + bias: both projections, the activation and their product in one pass.
+ *   x [m][k]; w [2 n][k]: the gate's n rows, then those of what it gates; bias [2 n] or NULL, in the same order; y [m][n]; z [m][2 n] or
+ *   NULL: both pre-activations, which vf_gated_linear_backward reads.  k = 0: z = bias.  n <= 2^24, k <= 2^25.  Limits on tiles as in vf_linear.
+ */
+int vf_gated_linear(int32_t dtype, int64_t m, int64_t n, int64_t k, const void *x, int64_t ldx, const void *w, int64_t ldw,
+                    const void *bias, int32_t activation, void *y, int64_t ldy, void *z, int64_t ldz, void *workspace,
+                    size_t workspace_bytes, void *hip_stream);
+/*
+ * Its gradients, from dy [m][n]: dz = [dy z_up act'(z_gate) | dy act(z_gate)], rounded to dtype as an operand; dx = dz w; dw = dz^T x;
+ * dbias = column sums of dz (before that rounding).  Each of dx [m][k], dw [2 n][k], dbias [2 n] may be NULL: it is left out, and what only it
+ * reads (w for dx, x for dw) may be NULL too.  relu'(0) = 0.
+ */
+int vf_gated_linear_backward(int32_t dtype, int64_t m, int64_t n, int64_t k, const void *dy, int64_t lddy, const void *x,
+                             int64_t ldx, const void *w, int64_t ldw, const void *z, int64_t ldz, int32_t activation, void *dx,
+                             int64_t lddx, void *dw, int64_t lddw, void *dbias, void *workspace, size_t workspace_bytes,
+                             void *hip_stream);
+int vf_gated_linear_workspace(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t activation, int32_t backward,
+                              size_t *bytes);
+
+/*
+ * Matrices in 8 bits: codes in OCP e4m3 (4 bits of exponent, 3 of significand, no infinity), and for each 128 columns of a row, its last ones
+ * filled up with codes of zero, a scale byte b that stands for 2^(b - 127).  A value is its code times its scale.
+ *   codes   [rows][ld]: rows start on 16 bytes (ld a multiple of 16) and have ceil(cols / 128) * 128 codes
+ *   scales  [rows][lds]: rows start on 4 bytes (lds a multiple of 4, at least the number of blocks rounded up to 4; bytes behind
+ *           the last block may be read, and mean nothing)
+ * What the library writes has the least scale under which the block's largest finite value is at most 448 (1 for a block of zeros), and the
+ * nearest code, ties to even; what is not finite becomes NaN by itself.
+ */
+#define VF_Q8_BLOCK 128
+/* x [m][d] of dtype in 8 bits, and back (any dtype; bfloat16 and float32 hold the values exactly, but for 2^128, which becomes infinite).  d <= 2^25. */
+int vf_quantize(int32_t dtype, int64_t m, int64_t d, const void *x, int64_t ldx, uint8_t *codes, int64_t ld, uint8_t *scales,
+                int64_t lds, void *hip_stream);
+int vf_dequantize(int32_t dtype, int64_t m, int64_t d, const uint8_t *codes, int64_t ld, const uint8_t *scales, int64_t lds,
+                  void *y, int64_t ldy, void *hip_stream);
+/*
+ * y = act(z) + residual, or where `gated` is 1 act(z_gate) z_up + residual, z = x w^T + bias, of x [m][k] and w [n][k] (gated: [2 n][k], the gate's
+ * rows first) in 8 bits.  dtype is that of bias [n] (gated: [2 n]; or NULL), residual [m][n] (or NULL) and y [m][n].  The output is either y, which may be
+ * the residual's own memory (same ld), or (y NULL) y_codes and y_scales.  n <= 2^24, k <= 2^25.
+ * dtype VF_F32: products to float32's accuracy, at half the rate.  Else they are as good as the matrix cores' sums of products of codes, which are added
+ * eight neighbours at a time to 2^-13 of the largest of them: 1.4e-5 of the result where values are of like size, a hundredth of what bfloat16 rounds by.
+ */
+int vf_linear_quantized(int32_t dtype, int64_t m, int64_t n, int64_t k, const uint8_t *x_codes, int64_t ldx, const uint8_t *x_scales,
+                 int64_t ldxs, const uint8_t *w_codes, int64_t ldw, const uint8_t *w_scales, int64_t ldws, const void *bias,
+                 int32_t activation, int32_t gated, const void *residual, int64_t ldr, void *y, int64_t ldy, uint8_t *y_codes,
+                 int64_t ldyc, uint8_t *y_scales, int64_t ldys, void *workspace, size_t workspace_bytes, void *hip_stream);
+/* quantized: 1 where the output is in 8 bits. */
+int vf_linear_quantized_workspace(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t gated, int32_t quantized, size_t *bytes);
+
+/*
+ * total = x + residual (rounded to dtype; total = x without a residual), y = total rstd weight, rstd = 1 / sqrt(avg(total^2) + eps), per row of
+ * 1 <= d <= 2^24 elements.
+ *   weight [d] or NULL (1); residual, total [m][d]: both or neither; rstd float [m] or NULL.  The output is either y [m][d] or (y NULL) y_codes and
+ *   y_scales, 8 bits straight from float32.  total may be x's or the residual's own memory (same ld); y may be x's own where there is no residual.
+ */
+int vf_rms_norm(int32_t dtype, int64_t m, int64_t d, const void *x, int64_t ldx, const void *residual, int64_t ldr,
+                const void *weight, double eps, void *y, int64_t ldy, uint8_t *y_codes, int64_t ldyc, uint8_t *y_scales,
+                int64_t ldys, void *total, int64_t ldt, float *rstd, void *hip_stream);
+/*
+ * Its gradients.  With h = total rstd and g = dy weight:  dx = rstd (g - h avg(g h)) + d_total, which is the residual's gradient too;
+ * dweight = column sums of dy h.  d_total [m][d], the gradient that reaches total by its other uses, or NULL.  Each of dx and dweight may be NULL.
+ * dx may be dy's or d_total's own memory (same ld).
+ */
+int vf_rms_norm_backward(int32_t dtype, int64_t m, int64_t d, const void *dy, int64_t lddy, const void *total, int64_t ldt,
+                         const float *rstd, const void *weight, const void *d_total, int64_t lddt, void *dx, int64_t lddx,
+                         void *dweight, void *workspace, size_t workspace_bytes, void *hip_stream);
+int vf_rms_norm_workspace(int32_t dtype, int64_t m, int64_t d, size_t *bytes);
+
+/*
+ * Divergence from a teacher that is known by the top entries of its rows (as vf_log_probs gives them), over a vocabulary of v >= 1 labels:
+ *     q = softmax over a row's entries of teacher / temperature;  p = softmax over all labels of logits / temperature
+ *     loss = sum over entries of q (log q - log p at the entry's label)
+ *   ids      int32 [m][top], 1 <= top <= VF_DISTILL_MAX_TOP: labels; -1 is no entry.  The same label twice counts twice
+ *   teacher  float [m][top]: the teacher's logits or log probabilities; -inf is no entry
+ *   loss     float [m]; 0 for a row without entries, NaN for one with an id that is neither a label nor -1
+ *   lse      float [m] or NULL: log sum exp(logits / temperature), which the gradient reads
+ * temperature: 1e-6 .. 1e6.  A logit of -inf is a masked label: an entry at it whose q is not 0 makes the loss +inf.  NaN or +inf in a row's logits or
+ * teacher makes its loss NaN.
+ */
+#define VF_DISTILL_MAX_TOP 256
+int vf_distill(int32_t dtype, int64_t m, int64_t v, const void *logits, int64_t ld, const int32_t *ids, const float *teacher,
+               int32_t top, double temperature, float *loss, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream);
+/*
+ * dlogits_i = d_loss / temperature (p_i - sum of q at i), [m][v] of dtype; lse as vf_distill left it for these logits and temperature (p as in
+ * vf_log_probs_backward: lse's own rounding is a relative error that a row's p share).  Zeros for rows without entries, without a label left,
+ * or with an id that is neither a label nor -1.  dlogits may be the logits' own memory (same ld).
+ */
+int vf_distill_backward(int32_t dtype, int64_t m, int64_t v, const void *logits, int64_t ld, const float *lse, const int32_t *ids,
+                        const float *teacher, int32_t top, double temperature, const float *d_loss, void *dlogits, int64_t ldd,
+                        void *hip_stream);
+int vf_distill_workspace(int32_t dtype, int64_t m, int64_t v, size_t *bytes);
+
+/*
  * Experiment and test switches (not part of the paper's method): launch geometry, which kernels serve which
  * batch sizes, the error-bound scale of the float32 seed proofs.  With index == NULL the process-wide
  * defaults change, which indexes built afterwards start from (the build-time switches "build16",

@@ -10,6 +10,7 @@ import ctypes as C
 import functools
 import os
 import struct
+from typing import NamedTuple
 
 import numpy as np
 
@@ -27,7 +28,10 @@ EXPORTED_SYMBOLS = ("vf_build_index", "vf_search", "vf_search_exact", "vf_index_
                     "vf_serve_poll", "vf_serve_end", "vf_serve_run", "vf_search_ex",
                     "vf_linear", "vf_linear_backward", "vf_linear_workspace", "vf_debug_linear", "vf_layer_norm", "vf_layer_norm_backward",
                     "vf_layer_norm_workspace", "vf_log_probs", "vf_log_probs_backward", "vf_log_probs_workspace",
-                    "vf_adamw_step", "vf_adamw_moments")
+                    "vf_adamw_step", "vf_adamw_moments",
+                    "vf_gated_linear", "vf_gated_linear_backward", "vf_gated_linear_workspace", "vf_quantize", "vf_dequantize", "vf_linear_quantized",
+                    "vf_linear_quantized_workspace", "vf_rms_norm", "vf_rms_norm_backward", "vf_rms_norm_workspace", "vf_distill", "vf_distill_backward",
+                    "vf_distill_workspace")
 
 ALLOC_FN = C.CFUNCTYPE(C.c_void_p, C.c_size_t, C.c_void_p)
 FREE_FN = C.CFUNCTYPE(None, C.c_void_p, C.c_void_p)
@@ -143,7 +147,20 @@ def load_library():
                 vf_log_probs_backward=[i32, i64, i64, p, i64, p, p, p, p, p, p, i64, p],
                 vf_log_probs_workspace=[i32, i64, i64, i32, C.POINTER(sz)],
                 vf_adamw_step=[p, i32, C.POINTER(VfAdamwParams), p, p],
-                vf_adamw_moments=[p, i32, p, p, p]).items():
+                vf_adamw_moments=[p, i32, p, p, p],
+                vf_gated_linear=[i32, i64, i64, i64, p, i64, p, i64, p, i32, p, i64, p, i64, p, sz, p],
+                vf_gated_linear_backward=[i32, i64, i64, i64, p, i64, p, i64, p, i64, p, i64, i32, p, i64, p, i64, p, p, sz, p],
+                vf_gated_linear_workspace=[i32, i64, i64, i64, i32, i32, C.POINTER(sz)],
+                vf_quantize=[i32, i64, i64, p, i64, p, i64, p, i64, p],
+                vf_dequantize=[i32, i64, i64, p, i64, p, i64, p, i64, p],
+                vf_linear_quantized=[i32, i64, i64, i64, p, i64, p, i64, p, i64, p, i64, p, i32, i32, p, i64, p, i64, p, i64, p, i64, p, sz, p],
+                vf_linear_quantized_workspace=[i32, i64, i64, i64, i32, i32, C.POINTER(sz)],
+                vf_rms_norm=[i32, i64, i64, p, i64, p, i64, p, C.c_double, p, i64, p, i64, p, i64, p, i64, p, p],
+                vf_rms_norm_backward=[i32, i64, i64, p, i64, p, i64, p, p, p, i64, p, i64, p, p, sz, p],
+                vf_rms_norm_workspace=[i32, i64, i64, C.POINTER(sz)],
+                vf_distill=[i32, i64, i64, p, i64, p, p, i32, C.c_double, p, p, p, sz, p],
+                vf_distill_backward=[i32, i64, i64, p, i64, p, p, p, i32, C.c_double, p, p, i64, p],
+                vf_distill_workspace=[i32, i64, i64, C.POINTER(sz)]).items():
             getattr(L, name).restype = C.c_int
             getattr(L, name).argtypes = args
         L.vf_index_free.restype = None
@@ -512,6 +529,8 @@ def search_exact(index: Index, queries, qlabel_offsets, qlabel_ids, k, stream=No
 ACTIVATIONS = dict(none=0, relu=1, gelu=2, silu=3)
 ADAMW_BLOCK = 256
 LOG_PROBS_MAX_TOP = 64
+Q8_BLOCK = 128
+DISTILL_MAX_TOP = 256
 
 # Filled on first use (torch is imported lazily here): torch, the codes of its float types, the current stream's handle.
 _torch = _codes = _raw_stream = None
@@ -842,3 +861,254 @@ def adamw_moments(ms, vs, m_scales=None, v_scales=None, stream=None):
     handle = _raw_stream(dev) if stream is None else stream.cuda_stream
     _check(load_library().vf_adamw_moments(items, count, ptrs[0], ptrs[1], handle))
     return outs[0], outs[1]
+
+
+def gated_linear(x, weight, bias=None, activation="silu", save=False, out=None, stream=None):
+    """act(x Wg^T + bg) (x Wu^T + bu) for x [m, k] and weight [2 n, k], the rows of Wg and then those of Wu, bias [2 n] alike
+    (vf_gated_linear).  save=True: (y, z) with both pre-activations z [m, 2 n], which gated_linear_backward reads."""
+    L = load_library()
+    code, T, dev, handle = _first(x, "x", stream)
+    act = _activation(activation)
+    ldx = _matrix(x, "x", T, dev)
+    m, k = x.shape
+    ldw = _matrix(weight, "weight", T, dev, None, k)
+    n, odd = divmod(weight.shape[0], 2)
+    if odd:
+        raise VecflowError("weight must have an even number of rows: the gate's and then those of what it gates")
+    pb = _vector(bias, "bias", T, dev, 2 * n)
+    if out is None:
+        out, ldy = _empty(x, (m, n), T, stream), n
+    else:
+        ldy = _matrix(out, "out", T, dev, m, n)
+    z = _empty(x, (m, 2 * n), T, stream) if save else None
+    nw = _size_of("vf_gated_linear_workspace", code, m, n, k, act, 0)
+    _ws, pw = _workspace(x, nw, stream)
+    _check(L.vf_gated_linear(code, m, n, k, x.data_ptr(), ldx, weight.data_ptr(), ldw, pb, act, out.data_ptr(), ldy,
+                             z.data_ptr() if save else None, 2 * n, pw, nw, handle))
+    return (out, z) if save else out
+
+
+def gated_linear_backward(dy, x, weight, z, activation="silu", bias=True, dx=True, dweight=True, stream=None):
+    """Gradients (dx, dweight, dbias) of gated_linear from dy [m, n] and its pre-activations z [m, 2 n]
+    (vf_gated_linear_backward).  What is not asked for is None."""
+    L = load_library()
+    code, T, dev, handle = _first(dy, "dy", stream)
+    act = _activation(activation)
+    lddy = _matrix(dy, "dy", T, dev)
+    m, n = dy.shape
+    ldx = _matrix(x, "x", T, dev, m)
+    k = x.shape[1]
+    ldw = _matrix(weight, "weight", T, dev, 2 * n, k)
+    ldz = _matrix(z, "z", T, dev, m, 2 * n)
+    gx = _empty(dy, (m, k), T, stream) if dx else None
+    gw = _empty(dy, (2 * n, k), T, stream) if dweight else None
+    gb = _empty(dy, (2 * n,), T, stream) if bias else None
+    nw = _size_of("vf_gated_linear_workspace", code, m, n, k, act, 1)
+    _ws, pw = _workspace(dy, nw, stream)
+    _check(L.vf_gated_linear_backward(code, m, n, k, dy.data_ptr(), lddy, x.data_ptr(), ldx, weight.data_ptr(), ldw, z.data_ptr(), ldz, act,
+                                      gx.data_ptr() if dx else None, k, gw.data_ptr() if dweight else None, k,
+                                      gb.data_ptr() if bias else None, pw, nw, handle))
+    return gx, gw, gb
+
+
+class Q8(NamedTuple):
+    """A matrix of `cols` columns in 8 bits: codes float8_e4m3fn [rows, cols rounded up to 128], scales uint8 [rows, a multiple of 4]; byte b of a
+    row's block of 128 columns stands for 2^(b - 127)."""
+    codes: object
+    scales: object
+    cols: int
+
+
+def _q8_empty(like, rows, cols, stream):
+    blocks = -(-cols // Q8_BLOCK)
+    return Q8(_empty(like, (rows, blocks * Q8_BLOCK), _torch.float8_e4m3fn, stream), _empty(like, (rows, -(-blocks // 4) * 4), _torch.uint8, stream), cols)
+
+
+def _q8(q, what, dev, rows=None, cols=None):
+    """(address of the codes, their ld, address of the scales, their ld) of a matrix in 8 bits."""
+    if not isinstance(q, Q8):
+        raise VecflowError(f"{what} must be a Q8")
+    n, d = q.codes.shape[0], q.cols
+    if d < 0 or (rows is not None and n != rows) or (cols is not None and d != cols):
+        raise VecflowError(f"{what} must have shape [{n if rows is None else rows}, {d if cols is None else cols}], not [{n}, {d}]")
+    blocks = -(-d // Q8_BLOCK)
+    ld = _matrix(q.codes, f"{what}: codes", _torch.float8_e4m3fn, dev, n, blocks * Q8_BLOCK)
+    lds = _matrix(q.scales, f"{what}: scales", _torch.uint8, dev, n, -(-blocks // 4) * 4)
+    return q.codes.data_ptr(), ld, q.scales.data_ptr(), lds
+
+
+def _no_q8():
+    return None, 0, None, 0
+
+
+def quantize(x, stream=None):
+    """x [m, d] in 8 bits, a Q8 (vf_quantize)."""
+    L = load_library()
+    code, T, dev, handle = _first(x, "x", stream)
+    ldx = _matrix(x, "x", T, dev)
+    m, d = x.shape
+    q = _q8_empty(x, m, d, stream)
+    _check(L.vf_quantize(code, m, d, x.data_ptr(), ldx, *_q8(q, "the output", dev), handle))
+    return q
+
+
+def _first_q8(q, what, dtype, stream):
+    """(type code of the wide side, device, stream handle) of a call whose first operand is in 8 bits."""
+    if not isinstance(q, Q8):
+        raise VecflowError(f"{what} must be a Q8")
+    if _torch is None:
+        _use_torch()
+    code = _codes.get(dtype)
+    if code is None:
+        raise VecflowError(f"{what}: unsupported dtype {dtype}")
+    dev = q.codes.get_device()
+    if dev < 0 or dev != _torch.cuda.current_device():
+        raise VecflowError(f"{what} must be of CUDA tensors on the current device")
+    return code, dev, _raw_stream(dev) if stream is None else stream.cuda_stream
+
+
+def dequantize(q, dtype, out=None, stream=None):
+    """The values of a Q8 in float32, bfloat16 (both exact) or float16 (vf_dequantize)."""
+    L = load_library()
+    code, dev, handle = _first_q8(q, "q", dtype, stream)
+    at = _q8(q, "q", dev)
+    m, d = q.codes.shape[0], q.cols
+    if out is None:
+        out, ldy = _empty(q.codes, (m, d), dtype, stream), d
+    else:
+        ldy = _matrix(out, "out", dtype, dev, m, d)
+    _check(L.vf_dequantize(code, m, d, *at, out.data_ptr(), ldy, handle))
+    return out
+
+
+def linear_q8(x, weight, bias=None, residual=None, activation="none", gated=False, dtype=None, quantize=False, out=None, stream=None):
+    """act(x weight^T + bias) + residual of Q8 operands x [m, k] and weight [n, k] (vf_linear_quantized).  gated=True: act(gate) up + residual, with
+    weight [2 n, k] and bias [2 n] as in gated_linear.  dtype: of bias, residual and output (bfloat16 if nothing says otherwise); quantize=True: the output
+    is a Q8.  `out`: where a wide output goes, the residual's own memory if need be."""
+    L = load_library()
+    if _torch is None:
+        _use_torch()
+    if dtype is None:
+        dtype = next((t.dtype for t in (bias, residual, out) if t is not None), _torch.bfloat16)
+    code, dev, handle = _first_q8(x, "x", dtype, stream)
+    act = _activation(activation)
+    px = _q8(x, "x", dev)
+    m, k = x.codes.shape[0], x.cols
+    pw8 = _q8(weight, "weight", dev, None, k)
+    rows = weight.codes.shape[0]
+    n, odd = divmod(rows, 2) if gated else (rows, 0)
+    if odd:
+        raise VecflowError("weight must have an even number of rows: the gate's and then those of what it gates")
+    pb = _vector(bias, "bias", dtype, dev, rows)
+    ldr = 0 if residual is None else _matrix(residual, "residual", dtype, dev, m, n)
+    if quantize:
+        if out is not None:
+            raise VecflowError("out is for a wide output")
+        y = _q8_empty(x.codes, m, n, stream)
+        py, ldy, po = None, 0, _q8(y, "the output", dev)
+    else:
+        y = _empty(x.codes, (m, n), dtype, stream) if out is None else out
+        ldy = _matrix(y, "out", dtype, dev, m, n)
+        py, po = y.data_ptr(), _no_q8()
+    nw = _size_of("vf_linear_quantized_workspace", code, m, n, k, int(gated), int(quantize))
+    _ws, pw = _workspace(x.codes, nw, stream)
+    _check(L.vf_linear_quantized(code, m, n, k, *px, *pw8, pb, act, int(gated), None if residual is None else residual.data_ptr(), ldr, py, ldy, *po, pw, nw,
+                          handle))
+    return y
+
+
+def rms_norm(x, weight=None, residual=None, eps=1e-6, save=False, quantize=False, out=None, out_total=None, stream=None):
+    """total / sqrt(avg(total^2) + eps) weight per row, total = x + residual for x [m, d] (vf_rms_norm): y, with a residual (y, total),
+    with save=True rstd float32 [m] behind.  quantize=True: y is a Q8.  `out_total` may be x's or the residual's own memory, `out` x's where there is no
+    residual."""
+    L = load_library()
+    code, T, dev, handle = _first(x, "x", stream)
+    ldx = _matrix(x, "x", T, dev)
+    m, d = x.shape
+    pg = _vector(weight, "weight", T, dev, d)
+    pr, ldr, total, pt, ldt = None, 0, None, None, 0
+    if residual is not None:
+        pr, ldr = residual.data_ptr(), _matrix(residual, "residual", T, dev, m, d)
+        total = _empty(x, (m, d), T, stream) if out_total is None else out_total
+        pt, ldt = total.data_ptr(), _matrix(total, "out_total", T, dev, m, d)
+    elif out_total is not None:
+        raise VecflowError("out_total needs a residual")
+    if quantize:
+        if out is not None:
+            raise VecflowError("out is for a wide output")
+        y = _q8_empty(x, m, d, stream)
+        py, ldy, po = None, 0, _q8(y, "the output", dev)
+    else:
+        y = _empty(x, (m, d), T, stream) if out is None else out
+        py, ldy, po = y.data_ptr(), _matrix(y, "out", T, dev, m, d), _no_q8()
+    rstd = _empty(x, (m,), _torch.float32, stream) if save else None
+    _check(L.vf_rms_norm(code, m, d, x.data_ptr(), ldx, pr, ldr, pg, eps, py, ldy, *po, pt, ldt, rstd.data_ptr() if save else None, handle))
+    if total is None:
+        return (y, rstd) if save else y
+    return (y, total, rstd) if save else (y, total)
+
+
+def rms_norm_backward(dy, total, rstd, weight=None, d_total=None, dx=True, dweight=True, out=None, stream=None):
+    """Gradients (dx, dweight) of rms_norm from dy [m, d] (vf_rms_norm_backward); dx is the residual's gradient too.  d_total [m, d]: the gradient that
+    reaches total by its other uses.  What is not asked for is None.  `out`: where dx goes, dy's or d_total's own memory if need be."""
+    L = load_library()
+    code, T, dev, handle = _first(dy, "dy", stream)
+    lddy = _matrix(dy, "dy", T, dev)
+    m, d = dy.shape
+    ldt = _matrix(total, "total", T, dev, m, d)
+    pr, pg = _vector(rstd, "rstd", _torch.float32, dev, m), _vector(weight, "weight", T, dev, d)
+    pdt, lddt = (None, 0) if d_total is None else (d_total.data_ptr(), _matrix(d_total, "d_total", T, dev, m, d))
+    if dx and out is None:
+        out = _empty(dy, (m, d), T, stream)
+    ldo = _matrix(out, "out", T, dev, m, d) if dx else 0
+    gw = _empty(dy, (d,), T, stream) if dweight else None
+    nw = _size_of("vf_rms_norm_workspace", code, m, d) if dweight else 0
+    _ws, pw = _workspace(dy, nw, stream)
+    _check(L.vf_rms_norm_backward(code, m, d, dy.data_ptr(), lddy, total.data_ptr(), ldt, pr, pg, pdt, lddt, out.data_ptr() if dx else None, ldo,
+                                  gw.data_ptr() if dweight else None, pw, nw, handle))
+    return out if dx else None, gw
+
+
+def _entries(ids, teacher, dev, m):
+    """(address of the ids, of the teacher's values, entries per row)."""
+    if ids.dim() != 2 or teacher.shape != ids.shape or ids.shape[0] != m:
+        raise VecflowError(f"ids and teacher must have the same shape [{m}, top]")
+    top = ids.shape[1]
+    if not 1 <= top <= DISTILL_MAX_TOP:
+        raise VecflowError(f"top must be 1 .. {DISTILL_MAX_TOP}")
+    for t, what, kind in ((ids, "ids", _torch.int32), (teacher, "teacher", _torch.float32)):
+        if t.dtype != kind or t.get_device() != dev or not t.is_contiguous():
+            raise VecflowError(f"{what} must be a contiguous CUDA tensor of {kind} on the same device")
+    return ids.data_ptr(), teacher.data_ptr(), top
+
+
+def distill(logits, ids, teacher, temperature=1.0, stream=None):
+    """Divergence of softmax(logits / temperature), logits [m, v], from a teacher known by ids int32 [m, top] (-1: none) and its logits or log
+    probabilities there, float32 [m, top] (vf_distill): (loss, lse), float32 [m]."""
+    L = load_library()
+    code, T, dev, handle = _first(logits, "logits", stream)
+    ld = _matrix(logits, "logits", T, dev)
+    m, v = logits.shape
+    pi, pt, top = _entries(ids, teacher, dev, m)
+    loss, lse = _empty(logits, (2, m), _torch.float32, stream).unbind(0)
+    nw = _size_of("vf_distill_workspace", code, m, v)
+    _ws, pw = _workspace(logits, nw, stream)
+    _check(L.vf_distill(code, m, v, logits.data_ptr(), ld, pi, pt, top, temperature, loss.data_ptr(), lse.data_ptr(), pw, nw, handle))
+    return loss, lse
+
+
+def distill_backward(logits, lse, ids, teacher, d_loss, temperature=1.0, out=None, stream=None):
+    """Gradient with respect to the logits from that of the loss, float32 [m] (vf_distill_backward); `out` may be the logits' own
+    memory."""
+    L = load_library()
+    code, T, dev, handle = _first(logits, "logits", stream)
+    ld = _matrix(logits, "logits", T, dev)
+    m, v = logits.shape
+    pi, pt, top = _entries(ids, teacher, dev, m)
+    if out is None:
+        out, ldd = _empty(logits, (m, v), T, stream), v
+    else:
+        ldd = _matrix(out, "out", T, dev, m, v)
+    _check(L.vf_distill_backward(code, m, v, logits.data_ptr(), ld, _vector(lse, "lse", _torch.float32, dev, m), pi, pt, top, temperature,
+                                 _vector(d_loss, "d_loss", _torch.float32, dev, m), out.data_ptr(), ldd, handle))
+    return out

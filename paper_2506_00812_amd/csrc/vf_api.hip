@@ -341,3 +341,130 @@ extern "C" int vf_adamw_moments(const vf_adamw_tensor *tensors, int32_t n_tensor
 {
     return guarded([&] { return adamw_moments_impl(tensors, n_tensors, m_out, v_out, (hipStream_t)hip_stream); });
 }
+
+extern "C" int vf_gated_linear(int32_t dtype, int64_t m, int64_t n, int64_t k, const void *x, int64_t ldx, const void *w, int64_t ldw,
+                               const void *bias, int32_t activation, void *y, int64_t ldy, void *z, int64_t ldz, void *workspace,
+                               size_t workspace_bytes, void *hip_stream)
+{
+    return guarded([&] {
+        LinearArgs a{};
+        a.dtype = dtype; a.act = activation; a.m = m; a.n = n; a.k = k;
+        a.x = x; a.ldx = ldx; a.w = w; a.ldw = ldw; a.bias = bias; a.y = y; a.ldy = ldy; a.z = z; a.ldz = ldz;
+        a.workspace = workspace; a.workspace_bytes = workspace_bytes; a.stream = (hipStream_t)hip_stream;
+        return gated_linear_impl(a);
+    });
+}
+
+extern "C" int vf_gated_linear_backward(int32_t dtype, int64_t m, int64_t n, int64_t k, const void *dy, int64_t lddy, const void *x,
+                                        int64_t ldx, const void *w, int64_t ldw, const void *z, int64_t ldz, int32_t activation,
+                                        void *dx, int64_t lddx, void *dw, int64_t lddw, void *dbias, void *workspace,
+                                        size_t workspace_bytes, void *hip_stream)
+{
+    return guarded([&] {
+        LinearArgs a{};
+        a.dtype = dtype; a.act = activation; a.m = m; a.n = n; a.k = k;
+        a.dy = dy; a.lddy = lddy; a.x = x; a.ldx = ldx; a.w = w; a.ldw = ldw; a.z = const_cast<void *>(z); a.ldz = ldz;
+        a.dx = dx; a.lddx = lddx; a.dw = dw; a.lddw = lddw; a.dbias = dbias;
+        a.workspace = workspace; a.workspace_bytes = workspace_bytes; a.stream = (hipStream_t)hip_stream;
+        return gated_linear_backward_impl(a);
+    });
+}
+
+extern "C" int vf_gated_linear_workspace(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t activation, int32_t backward,
+                                         size_t *bytes)
+{
+    return guarded([&] { return gated_linear_workspace_impl(dtype, m, n, k, activation, backward, bytes); });
+}
+
+extern "C" int vf_quantize(int32_t dtype, int64_t m, int64_t d, const void *x, int64_t ldx, uint8_t *codes, int64_t ld, uint8_t *scales,
+                           int64_t lds, void *hip_stream)
+{
+    return guarded([&] { return quantize_impl(dtype, m, d, x, ldx, Q8Arg{codes, scales, ld, lds}, (hipStream_t)hip_stream); });
+}
+
+extern "C" int vf_dequantize(int32_t dtype, int64_t m, int64_t d, const uint8_t *codes, int64_t ld, const uint8_t *scales, int64_t lds,
+                             void *y, int64_t ldy, void *hip_stream)
+{
+    return guarded([&] { return dequantize_impl(dtype, m, d, Q8Arg{codes, scales, ld, lds}, y, ldy, (hipStream_t)hip_stream); });
+}
+
+extern "C" int vf_linear_quantized(int32_t dtype, int64_t m, int64_t n, int64_t k, const uint8_t *x_codes, int64_t ldx, const uint8_t *x_scales,
+                            int64_t ldxs, const uint8_t *w_codes, int64_t ldw, const uint8_t *w_scales, int64_t ldws, const void *bias,
+                            int32_t activation, int32_t gated, const void *residual, int64_t ldr, void *y, int64_t ldy, uint8_t *y_codes,
+                            int64_t ldyc, uint8_t *y_scales, int64_t ldys, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    return guarded([&] {
+        LinearQ8Args a{};
+        a.dtype = dtype; a.act = activation; a.gated = gated; a.m = m; a.n = n; a.k = k;
+        a.x = Q8Arg{x_codes, x_scales, ldx, ldxs}; a.w = Q8Arg{w_codes, w_scales, ldw, ldws}; a.out = Q8Arg{y_codes, y_scales, ldyc, ldys};
+        a.bias = bias; a.residual = residual; a.ldr = ldr; a.y = y; a.ldy = ldy;
+        a.workspace = workspace; a.workspace_bytes = workspace_bytes; a.stream = (hipStream_t)hip_stream;
+        return linear_q8_impl(a);
+    });
+}
+
+extern "C" int vf_linear_quantized_workspace(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t gated, int32_t quantized, size_t *bytes)
+{
+    return guarded([&] { return linear_q8_workspace_impl(dtype, m, n, k, gated, quantized, bytes); });
+}
+
+extern "C" int vf_rms_norm(int32_t dtype, int64_t m, int64_t d, const void *x, int64_t ldx, const void *residual, int64_t ldr,
+                           const void *weight, double eps, void *y, int64_t ldy, uint8_t *y_codes, int64_t ldyc, uint8_t *y_scales,
+                           int64_t ldys, void *total, int64_t ldt, float *rstd, void *hip_stream)
+{
+    return guarded([&] {
+        RmsArgs a{};
+        a.dtype = dtype; a.m = m; a.d = d; a.x = x; a.ldx = ldx; a.residual = residual; a.ldr = ldr; a.weight = weight; a.eps = eps;
+        a.y = y; a.ldy = ldy; a.codes = y_codes; a.ldc = ldyc; a.scales = y_scales; a.lds = ldys; a.total = total; a.ldt = ldt;
+        a.rstd = rstd; a.stream = (hipStream_t)hip_stream;
+        return rms_norm_impl(a);
+    });
+}
+
+extern "C" int vf_rms_norm_backward(int32_t dtype, int64_t m, int64_t d, const void *dy, int64_t lddy, const void *total, int64_t ldt,
+                                    const float *rstd, const void *weight, const void *d_total, int64_t lddt, void *dx, int64_t lddx,
+                                    void *dweight, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    return guarded([&] {
+        RmsArgs a{};
+        a.dtype = dtype; a.m = m; a.d = d; a.dy = dy; a.lddy = lddy; a.x = total; a.ldx = ldt; a.rstd = const_cast<float *>(rstd);
+        a.weight = weight; a.residual = d_total; a.ldr = lddt; a.y = dx; a.ldy = lddx; a.dweight = dweight;
+        a.workspace = workspace; a.workspace_bytes = workspace_bytes; a.stream = (hipStream_t)hip_stream;
+        return rms_norm_backward_impl(a);
+    });
+}
+
+extern "C" int vf_rms_norm_workspace(int32_t dtype, int64_t m, int64_t d, size_t *bytes)
+{
+    return guarded([&] { return rms_norm_workspace_impl(dtype, m, d, bytes); });
+}
+
+extern "C" int vf_distill(int32_t dtype, int64_t m, int64_t v, const void *logits, int64_t ld, const int32_t *ids, const float *teacher,
+                          int32_t top, double temperature, float *loss, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    return guarded([&] {
+        DistillArgs a{};
+        a.dtype = dtype; a.top = top; a.m = m; a.v = v; a.logits = logits; a.ld = ld; a.ids = ids; a.teacher = teacher;
+        a.temperature = temperature; a.loss = loss; a.lse = lse;
+        a.workspace = workspace; a.workspace_bytes = workspace_bytes; a.stream = (hipStream_t)hip_stream;
+        return distill_impl(a);
+    });
+}
+
+extern "C" int vf_distill_backward(int32_t dtype, int64_t m, int64_t v, const void *logits, int64_t ld, const float *lse, const int32_t *ids,
+                                   const float *teacher, int32_t top, double temperature, const float *d_loss, void *dlogits, int64_t ldd,
+                                   void *hip_stream)
+{
+    return guarded([&] {
+        DistillArgs a{};
+        a.dtype = dtype; a.top = top; a.m = m; a.v = v; a.logits = logits; a.ld = ld; a.lse = const_cast<float *>(lse); a.ids = ids;
+        a.teacher = teacher; a.temperature = temperature; a.d_loss = d_loss; a.dlogits = dlogits; a.ldd = ldd;
+        a.stream = (hipStream_t)hip_stream;
+        return distill_backward_impl(a);
+    });
+}
+
+extern "C" int vf_distill_workspace(int32_t dtype, int64_t m, int64_t v, size_t *bytes)
+{
+    return guarded([&] { return distill_workspace_impl(dtype, m, v, bytes); });
+}

@@ -8,30 +8,6 @@
 
 namespace vf {
 
-// Sums over the TPR threads that share a row, the same in each of them.  TPR = 64: one wave, no barrier; 16: a row of the wave's lanes.
-template <int TPR, int N> __device__ __forceinline__ void row_sums(float (&v)[N], float *lds)
-{
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = TPR == 16 ? sum16(v[i]) : wave_sum(v[i]);
-    if constexpr (TPR > 64) {
-        constexpr int W = TPR / 64;
-        const int wave = threadIdx.x >> 6;
-        __syncthreads();   // the last row's sums have been read
-        if ((threadIdx.x & 63) == 0) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) lds[wave * N + i] = v[i];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            float s = 0.f;
-#pragma unroll
-            for (int w = 0; w < W; ++w) s += lds[w * N + i];
-            v[i] = s;
-        }
-    }
-}
-
 // Rows of up to TPR * NV vectors: thread t of a row holds vectors t, t + TPR, ...  10,000 x 1,024 in float32: 17 us, 4.8 TB/s (a large
 // copy moves 4.9).
 template <class T, int TPR, int NV>
@@ -312,26 +288,6 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(int64_t m, int64_t d,
     if (sub < 2 && c < d)
         part[((int64_t)blockIdx.y * 2 + sub) * d + c] = (comb[sub][0][t] + comb[sub][1][t]) + (comb[sub][2][t] + comb[sub][3][t]);
 }
-
-// Calls fn(threads per row, vectors per thread) as constants for rows of nv vectors; false: no such kernel, the row is too long.
-// A wave takes rows of up to four vectors a lane by itself; beyond that the row's sums would keep too many registers.  Rows of up to 32
-// vectors, the index's own dimensions among them, take sixteen lanes each: a wave's instructions then serve four rows.
-template <class F> static bool by_row(int64_t nv, F &&fn)
-{
-    if (nv <= 16) fn(std::integral_constant<int, 16>(), std::integral_constant<int, 1>());
-    else if (nv <= 32) fn(std::integral_constant<int, 16>(), std::integral_constant<int, 2>());
-    else if (nv <= 64) fn(std::integral_constant<int, 64>(), std::integral_constant<int, 1>());
-    else if (nv <= 128) fn(std::integral_constant<int, 64>(), std::integral_constant<int, 2>());
-    else if (nv <= 256) fn(std::integral_constant<int, 64>(), std::integral_constant<int, 4>());
-    else if (nv <= 512) fn(std::integral_constant<int, 256>(), std::integral_constant<int, 2>());
-    else if (nv <= 1024) fn(std::integral_constant<int, 256>(), std::integral_constant<int, 4>());
-    else if (nv <= 2048) fn(std::integral_constant<int, 512>(), std::integral_constant<int, 4>());
-    else return false;
-    return true;
-}
-
-// A launch holds fewer than 2^32 threads: kernels loop over the rows beyond so many workgroups.
-static unsigned grid_of(int64_t blocks) { return (unsigned)std::min<int64_t>(blocks, 1 << 20); }
 
 constexpr int64_t kMaxRow = 1 << 24;   // elements of a row
 

@@ -220,6 +220,30 @@ template <class F> __host__ __device__ __forceinline__ void by_act(int act, F &&
     else fn(std::integral_constant<int, VF_ACT_SILU>());
 }
 
+// Sums over the TPR threads that share a row, the same in each of them.  TPR = 64: one wave, no barrier; 16: a row of the wave's lanes.
+template <int TPR, int N> __device__ __forceinline__ void row_sums(float (&v)[N], float *lds)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = TPR == 16 ? sum16(v[i]) : wave_sum(v[i]);
+    if constexpr (TPR > 64) {
+        constexpr int W = TPR / 64;
+        const int wave = threadIdx.x >> 6;
+        __syncthreads();   // the last row's sums have been read
+        if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) lds[wave * N + i] = v[i];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float s = 0.f;
+#pragma unroll
+            for (int w = 0; w < W; ++w) s += lds[w * N + i];
+            v[i] = s;
+        }
+    }
+}
+
 // Column sums from partial rows part [parts][sums][d]: 16 columns and one of the sums per workgroup, 64 threads to a column (2,048
 // columns of 1,024 rows 18 us with 16 threads to a column, 5 with 64); parts = 0: zeros.
 template <class T>
@@ -256,6 +280,26 @@ template <class T> void launch_join_parts(int parts, int64_t d, int sums, const 
     join_parts_kernel<T><<<dim3((unsigned)ceil_div(d, 16), (unsigned)sums), dim3(1024), 0, s>>>(parts, d, part, out0, out1);
 }
 
+// Calls fn(threads per row, vectors per thread) as constants for rows of nv vectors; false: no such kernel, the row is too long.
+// A wave takes rows of up to four vectors a lane by itself; beyond that the row's sums would keep too many registers.  Rows of up to 32
+// vectors, the index's own dimensions among them, take sixteen lanes each: a wave's instructions then serve four rows.
+template <class F> bool by_row(int64_t nv, F &&fn)
+{
+    if (nv <= 16) fn(std::integral_constant<int, 16>(), std::integral_constant<int, 1>());
+    else if (nv <= 32) fn(std::integral_constant<int, 16>(), std::integral_constant<int, 2>());
+    else if (nv <= 64) fn(std::integral_constant<int, 64>(), std::integral_constant<int, 1>());
+    else if (nv <= 128) fn(std::integral_constant<int, 64>(), std::integral_constant<int, 2>());
+    else if (nv <= 256) fn(std::integral_constant<int, 64>(), std::integral_constant<int, 4>());
+    else if (nv <= 512) fn(std::integral_constant<int, 256>(), std::integral_constant<int, 2>());
+    else if (nv <= 1024) fn(std::integral_constant<int, 256>(), std::integral_constant<int, 4>());
+    else if (nv <= 2048) fn(std::integral_constant<int, 512>(), std::integral_constant<int, 4>());
+    else return false;
+    return true;
+}
+
+// A launch holds fewer than 2^32 threads: kernels loop over the rows beyond so many workgroups.
+inline unsigned grid_of(int64_t blocks) { return (unsigned)std::min<int64_t>(blocks, 1 << 20); }
+
 // ---------------------------------------------------------------- entry points' bodies
 
 struct LinearArgs {
@@ -271,6 +315,10 @@ struct LinearArgs {
 };
 int linear_impl(const LinearArgs &a);
 int linear_backward_impl(const LinearArgs &a);
+bool linear_backward_fits(const LinearArgs &a);   // whether its products (activation none) have few enough tiles
+int gated_linear_impl(const LinearArgs &a);       // n outputs of 2 n rows of w
+int gated_linear_backward_impl(const LinearArgs &a);
+int gated_linear_workspace_impl(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t act, int32_t backward, size_t *bytes);
 int debug_linear_impl(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t product, int32_t direct, int32_t *tiling, int32_t *splits);
 int linear_workspace_impl(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t act, int32_t backward, size_t *bytes);
 
@@ -289,6 +337,63 @@ struct NormArgs {
 int layer_norm_impl(const NormArgs &a);
 int layer_norm_backward_impl(const NormArgs &a);
 int layer_norm_workspace_impl(int32_t dtype, int64_t m, int64_t d, size_t *bytes);
+
+struct RmsArgs {
+    int32_t dtype;
+    int64_t m, d;
+    const void *x, *residual, *dy, *weight;   // backward: the sum, its gradient by the residual's path
+    int64_t ldx, ldr, lddy, ldy, ldt;
+    double eps;
+    void *y, *total, *dweight;   // y: the gradient dx in the backward pass
+    float *rstd;
+    uint8_t *codes, *scales;
+    int64_t ldc, lds;
+    void *workspace;
+    size_t workspace_bytes;
+    hipStream_t stream;
+};
+int rms_norm_impl(const RmsArgs &a);
+int rms_norm_backward_impl(const RmsArgs &a);
+int rms_norm_workspace_impl(int32_t dtype, int64_t m, int64_t d, size_t *bytes);
+
+// A matrix in 8 bits (vf_q8.h).
+struct Q8Arg {
+    const uint8_t *codes, *scales;
+    int64_t ld, lds;
+};
+struct LinearQ8Args {
+    int32_t dtype, act, gated;
+    int64_t m, n, k;
+    Q8Arg x, w, out;
+    const void *bias, *residual;
+    int64_t ldr, ldy;
+    void *y;
+    void *workspace;
+    size_t workspace_bytes;
+    hipStream_t stream;
+};
+int linear_q8_impl(const LinearQ8Args &a);
+int linear_q8_workspace_impl(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t gated, int32_t quantized, size_t *bytes);
+int quantize_impl(int32_t dtype, int64_t m, int64_t d, const void *x, int64_t ldx, const Q8Arg &out, hipStream_t s);
+int dequantize_impl(int32_t dtype, int64_t m, int64_t d, const Q8Arg &in, void *y, int64_t ldy, hipStream_t s);
+
+struct DistillArgs {
+    int32_t dtype, top;
+    int64_t m, v, ld, ldd;
+    const void *logits;
+    const int32_t *ids;
+    const float *teacher;
+    double temperature;
+    float *loss, *lse;
+    const float *d_loss;
+    void *dlogits;
+    void *workspace;
+    size_t workspace_bytes;
+    hipStream_t stream;
+};
+int distill_impl(const DistillArgs &a);
+int distill_backward_impl(const DistillArgs &a);
+int distill_workspace_impl(int32_t dtype, int64_t m, int64_t v, size_t *bytes);
 
 struct LogProbArgs {
     int32_t dtype, top;
