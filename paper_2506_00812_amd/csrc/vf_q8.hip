@@ -2,6 +2,7 @@
 // P = w, Q = x, both along the contraction; P takes the matrix instruction's first operand, so that a lane's accumulators are
 // neighbours in a row of the output.  The instruction multiplies codes and applies both rows' scales; a lane's 32 codes may be any of a
 // step's, so long as both operands' lanes take the same ones.
+#include "vf_product.h"
 #include "vf_q8.h"
 
 namespace vf {
@@ -54,7 +55,9 @@ struct Q8Product {
     Q8Arg P, Q;
     int64_t np, nq;   // outputs of a row (rows of P; of each of its halves where it is gated), rows of Q
     int64_t blocks;   // of 128 of the contraction
-    float *part;      // [nq][np], gated [nq][2 np]
+    int64_t chunk;    // blocks per split
+    int splits;       // 0: the kernel has the epilogue; else its sums go to part, and the join has it
+    float *part;      // [splits][nq][np], gated [splits][nq][2 np]
 };
 
 template <class T> struct Q8Epilogue {
@@ -100,35 +103,385 @@ __device__ __forceinline__ float16v mma32(const int8v &p, int sp, const int8v &q
     }
 }
 
-// The sums alone, 32 x 32 a wave straight from memory, sixteen rows at a time of both halves where it is gated.
-template <bool EXACT, bool GATED>
-__global__ __launch_bounds__(256) void q8_simple_kernel(Q8Product a)
+// ---------------------------------------------------------------- few rows
+
+// At most 16 FQ rows of Q: one read of P, sixteen rows of it (of each half) a workgroup, whose waves share the contraction block by block, loaded from memory straight
+// into the matrix instruction's layout, and add up through LDS.  Bound by memory and latency; the codes are multiplied as bfloat16, which costs nothing
+// here and keeps every digit.
+template <class T, int FQ, bool GATED>
+__global__ __launch_bounds__(GATED ? 512 : 1024) void q8_few_rows_kernel(Q8Product a, Q8Epilogue<T> e)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    constexpr int OUT = GATED ? 16 : 32;
-    const int64_t tiles_p = (a.np + 2 * OUT - 1) / (2 * OUT);
-    const int64_t p0 = (blockIdx.x % tiles_p * 2 + (wave & 1)) * OUT, q0 = (blockIdx.x / tiles_p * 2 + (wave >> 1)) * 32;
-    int64_t rp = min(p0 + (GATED ? lane & 15 : lane & 31), a.np - 1);
-    if (GATED && (lane & 16)) rp += a.np;
-    const int64_t rq = min(q0 + (lane & 31), a.nq - 1);
-    const uint8_t *P = a.P.codes + rp * a.P.ld + (lane >> 5) * 32, *Q = a.Q.codes + rq * a.Q.ld + (lane >> 5) * 32;
-    const uint8_t *SP = a.P.scales + rp * a.P.lds, *SQ = a.Q.scales + rq * a.Q.lds;
-    float16v acc = {};
-    for (int64_t b = 0; b < a.blocks; ++b) {
-        const int sp = SP[b], sq = SQ[b];
+    constexpr int G = GATED ? 2 : 1;
+    __shared__ __align__(16) float4v sums[16 / G][G * FQ][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    const int64_t p0 = (int64_t)blockIdx.x * 16;
+    int64_t rp[G], rq[FQ];   // (rows beyond the last repeat it: their results are not kept)
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-            acc = mma32<EXACT>(load_vec<int8v>(P + b * 128 + h * 64), sp, load_vec<int8v>(Q + b * 128 + h * 64), sq, acc);
-    }
-    const int64_t q = q0 + (lane & 31);
-    if (q >= a.nq) return;
-    float *to = a.part + q * a.np * (GATED ? 2 : 1);
+    for (int g = 0; g < G; ++g) rp[g] = g * a.np + min(p0 + (lane & 15), a.np - 1);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const int r = 8 * (i / 4) + 4 * (lane >> 5) + i % 4;
-        const int64_t p = p0 + (GATED ? r & 15 : r);
-        if (p < a.np) to[GATED && r >= 16 ? a.np + p : p] = acc[i];
+    for (int j = 0; j < FQ; ++j) rq[j] = min((int64_t)(j * 16 + (lane & 15)), a.nq - 1);
+    float4v acc[G][FQ] = {};
+    const int at = (lane >> 4) * 32;
+    for (int64_t b = wave; b < a.blocks; b += waves) {
+        int8v cp[G], cq[FQ];
+        int sp[G], sq[FQ];
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            cp[g] = load_vec<int8v>(a.P.codes + rp[g] * a.P.ld + b * kBlock + at);
+            sp[g] = a.P.scales[rp[g] * a.P.lds + b];
+        }
+#pragma unroll
+        for (int j = 0; j < FQ; ++j) {
+            cq[j] = load_vec<int8v>(a.Q.codes + rq[j] * a.Q.ld + b * kBlock + at);
+            sq[j] = a.Q.scales[rq[j] * a.Q.lds + b];
+        }
+        Vec<bf16> vp[G][4];
+#pragma unroll
+        for (int g = 0; g < G; ++g) decode(cp[g], scale_value(sp[g]), vp[g]);
+#pragma unroll
+        for (int j = 0; j < FQ; ++j) {
+            Vec<bf16> vq[4];
+            decode(cq[j], scale_value(sq[j]), vq);
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int g = 0; g < G; ++g) acc[g][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vp[g][u], vq[u], acc[g][j], 0, 0, 0);
+        }
     }
+#pragma unroll
+    for (int j = 0; j < FQ; ++j)
+#pragma unroll
+        for (int g = 0; g < G; ++g) sums[wave][g * FQ + j][lane] = acc[g][j];
+    __syncthreads();
+    for (int j = wave; j < FQ; j += waves) {
+        float v[G][4] = {};
+        for (int w = 0; w < waves; ++w)
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                const float4v u = sums[w][g * FQ + j][lane];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[g][i] += u[i];
+            }
+        const int64_t q = j * 16 + (lane & 15), p = p0 + (lane >> 4) * 4;
+        if (q >= a.nq || p >= a.np) continue;
+        const int n = (int)min((int64_t)4, a.np - p);
+        if (a.splits > 0) {   // the join has the epilogue
+#pragma unroll
+            for (int g = 0; g < G; ++g) store_row(a.part + q * a.np * G + g * a.np + p, n, v[g]);
+            continue;
+        }
+        float bias[G][4], r[4];
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) bias[g][i] = 0.f;
+            if (e.bias) load_row(e.bias + g * a.np + p, n, bias[g]);
+        }
+        by_act(e.act, [&](auto act) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[0][i] = act_value<act.value, T>(v[0][i] + bias[0][i]);
+                if constexpr (GATED) v[0][i] *= v[1][i] + bias[1][i];
+            }
+        });
+        if (e.residual) {
+            load_row(e.residual + q * e.ldr + p, n, r);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[0][i] += r[i];
+        }
+        store_row(e.y + q * e.ldy + p, n, v[0]);
+    }
+}
+
+// ---------------------------------------------------------------- tiles
+
+// Row r of a tile of a gated P, counted in rows of one half: thirty-two of the gate, thirty-two of the other, and so on.
+__device__ __forceinline__ int half_row32(int r) { return (r >> 6) * 32 + (r & 31); }
+
+// Rows of 64 bytes, four to a line of the banks: their chunks are permuted so that the sixteen lanes that LDS serves together (0-3,
+// 12-15, 20-27 and so on), sixteen of a fragment's thirty-two rows, touch sixteen different ones.
+__device__ __forceinline__ int q8_chunk(int r, int ch) { return ch ^ (r >> 2 & 3); }
+
+__device__ __forceinline__ int8v q8_fragment(const unsigned char *tile, int r0, int lane)
+{
+    typedef int int4v __attribute__((ext_vector_type(4)));
+    const int r = r0 + (lane & 31), ch = (lane >> 5) * 2;
+    const int4v lo = *(const int4v *)(tile + r * 64 + (q8_chunk(r, ch) << 4)), hi = *(const int4v *)(tile + r * 64 + (q8_chunk(r, ch + 1) << 4));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// Four bytes a lane from its own address to LDS at `to` + 4 lane.
+__device__ __forceinline__ void request4(const void *from, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(from) : "memory", "m0");
+}
+
+// BP x BQ sums per workgroup of WP x WQ waves, straight to LDS, STEPS steps of 64 of the contraction deep, as direct_kernel in vf_product.h has them: while
+// step t's fragments are multiplied, those of step t + 1 are read, and steps up to t + STEPS - 1 are on their way.  The
+// scales of four blocks, eight steps, come a 32-bit word a row; a word's next byte is shifted down every other step.
+template <class T, bool EXACT, bool GATED, int BP, int BQ, int WP, int WQ, int STEPS>
+__global__ __launch_bounds__(WP *WQ * 64, 2) void q8_tile_kernel(Q8Product a, Q8Epilogue<T> e)
+{
+    constexpr int G = GATED ? 2 : 1, OUT = BP / G, WAVES = WP * WQ, FP = BP / WP / 32, FQ = BQ / WQ / 32;
+    static_assert(FP % G == 0, "");
+    constexpr int NP = BP / 16, NQ = BQ / 16;   // loads of a step; where they do not divide among the waves the last one is made twice
+    constexpr int LP = (NP + WAVES - 1) / WAVES, LQ = (NQ + WAVES - 1) / WAVES, LOADS = LP + LQ;
+    constexpr int NS = (BP + BQ) / 64, LS = (NS + WAVES - 1) / WAVES, kStep = (BP + BQ) * 64;
+    extern __shared__ __align__(16) unsigned char tiles[];   // [STEPS][P, Q][rows of 64 bytes], [2][P, Q] words of scales
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t tiles_p = (a.np + OUT - 1) / OUT;
+    const int64_t n = gridDim.x, xcd = blockIdx.x & 7, run = n / 8, left = n % 8;
+    const int64_t tile = xcd * run + min(xcd, left) + (blockIdx.x >> 3);
+    const int64_t p0 = tile % tiles_p * OUT, q0 = tile / tiles_p * BQ;
+    const int64_t b_first = (int64_t)blockIdx.y * a.chunk;
+    const int blocks = (int)max((int64_t)0, min(a.blocks - b_first, a.chunk)), steps = 2 * blocks;
+
+    const uint8_t *P = a.P.codes + p0 * a.P.ld + b_first * kBlock, *Q = a.Q.codes + q0 * a.Q.ld + b_first * kBlock;
+    uint32_t off_p[LP], off_q[LQ];
+#pragma unroll
+    for (int i = 0; i < LP; ++i) {
+        const int r = min(wave * LP + i, NP - 1) * 16 + (lane >> 2);
+        off_p[i] = (uint32_t)(min((int64_t)(GATED ? half_row32(r) : r), a.np - 1 - p0) * a.P.ld) + (q8_chunk(r, lane & 3) << 4);
+    }
+#pragma unroll
+    for (int i = 0; i < LQ; ++i) {
+        const int r = min(wave * LQ + i, NQ - 1) * 16 + (lane >> 2);
+        off_q[i] = (uint32_t)(min((int64_t)r, a.nq - 1 - q0) * a.Q.ld) + (q8_chunk(r, lane & 3) << 4);
+    }
+    const uint8_t *scales[LS];
+#pragma unroll
+    for (int i = 0; i < LS; ++i) {
+        int r = min(wave * LS + i, NS - 1) * 64 + lane;
+        if (r < BP) {
+            int64_t row = min(p0 + (GATED ? half_row32(r) : r), a.np - 1);
+            if (GATED && (r & 32)) row += a.np;
+            scales[i] = a.P.scales + row * a.P.lds + b_first;
+        } else {
+            scales[i] = a.Q.scales + min(q0 + r - BP, a.nq - 1) * a.Q.lds + b_first;
+        }
+    }
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)tiles;
+    const unsigned char *words = tiles + STEPS * kStep;
+    auto buffer_of = [](int t) { return (STEPS & (STEPS - 1)) == 0 ? t & (STEPS - 1) : t % STEPS; };
+    auto request_some = [&](int t, int first, int last) {   // loads first .. last - 1 of a step's
+        const uint32_t at = buffer_of(t) * kStep;
+        const uint8_t *p = P + t * 64, *q = Q + t * 64;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            if (i < first || i >= last) continue;
+            if (i < LP) {
+                const int piece = min(wave * LP + i, NP - 1);
+                request(GATED && (piece & 2) ? p + a.np * a.P.ld : p, off_p[i], lds0 + at + piece * 1024);
+            } else {
+                request(q, off_q[i - LP], lds0 + BP * 64 + at + min(wave * LQ + i - LP, NQ - 1) * 1024);
+            }
+        }
+    };
+    auto request_scales = [&](int group) {   // of blocks 4 group .. 4 group + 3
+#pragma unroll
+        for (int i = 0; i < LS; ++i)
+            request4(scales[i] + group * 4, lds0 + STEPS * kStep + (group & 1) * ((BP + BQ) * 4) + min(wave * LS + i, NS - 1) * 256);
+    };
+    const int wp = wave % WP * (FP * 32), wq = wave / WP * (FQ * 32);
+    float16v acc[FP][FQ] = {};
+    int8v fp[FP], fq[2][FQ];
+    int sp[FP], sq[FQ];
+    auto read_scales = [&](int group) {
+        const int *w = (const int *)(words + (group & 1) * ((BP + BQ) * 4)) + (lane & 31);
+#pragma unroll
+        for (int i = 0; i < FP; ++i) sp[i] = w[wp + i * 32];
+#pragma unroll
+        for (int j = 0; j < FQ; ++j) sq[j] = w[BP + wq + j * 32];
+    };
+    // A step in parts, one for each fragment of P: its matrix instructions, then the same fragment of the next step into the registers that they have read; Q's
+    // fragments have two sets.  Step t + STEPS - 1 goes into the buffer of step t - 1, whose fragments everybody has used before this step's barrier: the last reads
+    // of a step's own may still be on their way there.  MORE: step t + STEPS - 1 exists.
+    auto one_step = [&](auto more, int t, int set) {
+        constexpr int kParts = FP, kTail = 2 * FQ;   // LDS reads of Q's fragments
+        __builtin_amdgcn_sched_barrier(0);
+        if (more.value || t + STEPS - 2 < steps) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((STEPS - 3) * LOADS) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+        const bool request_more = more.value || t + STEPS - 1 < steps;
+        const unsigned char *at = tiles + buffer_of(t + 1) * kStep;   // (beyond the last step: a buffer's old contents, not used)
+#pragma unroll
+        for (int g = 0; g < kParts; ++g) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (request_more) request_some(t + STEPS - 1, g * LOADS / kParts, (g + 1) * LOADS / kParts);
+#pragma unroll
+            for (int j = 0; j < FQ; ++j) acc[g][j] = mma32<EXACT>(fp[g], sp[g], fq[set][j], sq[j], acc[g][j]);
+            // (here, and the sums in their own registers: the compiler would gather the step's matrix instructions at its end, and keep all of its reads until then)
+#pragma unroll
+            for (int j = 0; j < FQ; ++j) asm volatile("" : "+a"(acc[g][j])::"memory");
+#pragma unroll
+            for (int f = g * FQ / kParts; f < (g + 1) * FQ / kParts; ++f) fq[set ^ 1][f] = q8_fragment(at + BP * 64, wq + f * 32, lane);
+            fp[g] = q8_fragment(at, wp + g * 32, lane);
+        }
+    };
+    if (steps > 0) {
+        request_scales(0);
+        for (int t = 0; t < min(steps, STEPS - 1); ++t) request_some(t, 0, LOADS);
+        if (steps >= STEPS - 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STEPS - 2) * LOADS) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        asm volatile("s_barrier" ::: "memory");
+#pragma unroll
+        for (int j = 0; j < FQ; ++j) fq[0][j] = q8_fragment(tiles + BP * 64, wq + j * 32, lane);
+#pragma unroll
+        for (int i = 0; i < FP; ++i) fp[i] = q8_fragment(tiles, wp + i * 32, lane);
+        read_scales(0);
+    }
+    // The words of the next four blocks are asked for at the first of four, into the half that the last four have left (their words were read before this
+    // block's first barrier), and read at the fourth's end: eight steps' waits lie between.
+    auto one_block = [&](auto more, int b) {
+        const bool next = (b & 3) == 0 && b + 4 < blocks;
+        one_step(more, 2 * b, 0);
+        if (next) request_scales(b / 4 + 1);
+        one_step(more, 2 * b + 1, 1);
+        if ((b & 3) == 3) {
+            read_scales(b / 4 + 1);   // (after the last block: old words, not used)
+        } else {
+#pragma unroll
+            for (int i = 0; i < FP; ++i) sp[i] = (int)((uint32_t)sp[i] >> 8);
+#pragma unroll
+            for (int j = 0; j < FQ; ++j) sq[j] = (int)((uint32_t)sq[j] >> 8);
+        }
+    };
+    int b = 0;
+    for (; 2 * b + STEPS < steps; ++b) one_block(std::true_type(), b);
+    for (; b < blocks; ++b) one_block(std::false_type(), b);
+
+    // ---- the end: bias, activation and gate where the sums lie: a lane has row lane % 32 of Q and four neighbours of P, sixteen times eight apart
+    __syncthreads();
+    float *bias = (float *)tiles;                       // [G][OUT]
+    float *most = bias + BP;                            // [WP][BQ]
+    unsigned char *turn = (unsigned char *)(most + WP * BQ) + wave * (32 * 272);
+    const bool raw = a.splits > 0;
+    if (!raw) {
+        for (int i = threadIdx.x; i < BP; i += WAVES * 64) {
+            const int64_t p = p0 + i % OUT;
+            bias[i] = e.bias && p < a.np ? (float)e.bias[(i / OUT) * a.np + p] : 0.f;
+        }
+        __syncthreads();
+        by_act(e.act, [&](auto act) {
+#pragma unroll
+            for (int i = 0; i < FP; i += G)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    __builtin_amdgcn_sched_barrier(0);   // (all at once would not fit the registers)
+                    const int p = (wp + i * 32) / G + g * 8 + (lane >> 5) * 4;
+                    const float4v bg = *(const float4v *)(bias + p), bu = GATED ? *(const float4v *)(bias + OUT + p) : bg;
+#pragma unroll
+                    for (int j = 0; j < FQ; ++j)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            float v = act_value<act.value, T>(acc[i][j][g * 4 + c] + bg[c]);
+                            if constexpr (GATED) v *= acc[i + 1][j][g * 4 + c] + bu[c];
+                            acc[i / G][j][g * 4 + c] = v;
+                        }
+                }
+        });
+    }
+    constexpr int FO = FP / G;                          // fragments of outputs
+    const int64_t p_first = p0 + wp / G;
+    if constexpr (OUT % kBlock == 0) if (!raw && e.y == nullptr) {
+        // 8 bits: the largest value of a row's 128 outputs, which lanes 32 apart and (gated) two waves share, then codes, turned through LDS into whole stretches of a row
+        constexpr int kShare = 128 / (FO * 32);         // waves that share a block
+        float top[FQ];
+#pragma unroll
+        for (int j = 0; j < FQ; ++j) {
+            top[j] = 0.f;
+#pragma unroll
+            for (int i = 0; i < FO; ++i)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const int64_t p = p_first + i * 32 + g * 8 + (lane >> 5) * 4 + c;
+                        if (p >= a.np) acc[i][j][g * 4 + c] = 0.f;
+                        top[j] = fmaxf(top[j], finite_size(acc[i][j][g * 4 + c]));
+                    }
+            top[j] = fmaxf(top[j], __shfl_xor(top[j], 32, 64));
+            if (kShare > 1 && lane < 32) most[(wave % WP) * BQ + wq + j * 32 + lane] = top[j];
+        }
+        if constexpr (kShare > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < FQ; ++j) {
+                const int first = wave % WP / kShare * kShare;
+#pragma unroll
+                for (int w = 0; w < kShare; ++w) top[j] = fmaxf(top[j], most[(first + w) * BQ + wq + j * 32 + (lane & 31)]);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < FQ; ++j) {
+            const int byte = scale_byte(top[j]);
+            const float inverse = inverse_scale(byte);
+            const int64_t q = q0 + wq + j * 32 + (lane & 31);
+            if (lane < 32 && q < a.nq && p_first < a.np && wave % WP % kShare == 0) e.scales[q * e.lds + p_first / kBlock] = (uint8_t)byte;
+            constexpr int kRow = FO * 32 + 16;
+            wave_sync<true>();
+#pragma unroll
+            for (int i = 0; i < FO; ++i)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    int u = __builtin_amdgcn_cvt_pk_fp8_f32(acc[i][j][g * 4] * inverse, acc[i][j][g * 4 + 1] * inverse, 0, false);
+                    u = __builtin_amdgcn_cvt_pk_fp8_f32(acc[i][j][g * 4 + 2] * inverse, acc[i][j][g * 4 + 3] * inverse, u, true);
+                    *(int *)(turn + (lane & 31) * kRow + i * 32 + g * 8 + (lane >> 5) * 4) = u;
+                }
+            wave_sync<true>();
+            constexpr int kLanes = FO * 2;              // lanes to a row, sixteen codes each
+            for (int r = lane / kLanes; r < 32; r += 64 / kLanes) {
+                const int64_t row = q0 + wq + j * 32 + r, p = p_first + lane % kLanes * 16;
+                if (row < a.nq && p < (a.np + kBlock - 1) / kBlock * kBlock) store_vec(e.codes + row * e.ldc + p, *(const uint4 *)(turn + r * kRow + lane % kLanes * 16));
+            }
+        }
+        return;
+    }
+    // a wide type (or the sums): 64 columns of 32 rows at a time, eight columns a lane
+#pragma unroll
+    for (int j = 0; j < FQ; ++j)
+#pragma unroll
+        for (int h = 0; h < FP; h += 2) {
+            if (!raw && h >= FO) continue;
+            constexpr int kRow = 272;
+            const bool two = h + 1 < (raw ? FP : FO);
+            wave_sync<true>();
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (i == 0 || two)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g)
+                        *(float4v *)(turn + (lane & 31) * kRow + i * 128 + (g * 8 + (lane >> 5) * 4) * 4) =
+                            float4v{acc[h + i < FP ? h + i : h][j][g * 4], acc[h + i < FP ? h + i : h][j][g * 4 + 1], acc[h + i < FP ? h + i : h][j][g * 4 + 2],
+                                    acc[h + i < FP ? h + i : h][j][g * 4 + 3]};
+            wave_sync<true>();
+            const int lanes = two ? 8 : 4, col = lane % lanes * 8;
+            int64_t p = p_first + h * 32 + col;
+            int64_t to_half = 0;
+            if (raw && GATED) {   // fragment h is the gate's, the next one the other half's
+                p = p_first + h / 2 * 32 + col % 32;
+                to_half = col >= 32 ? a.np : 0;
+            }
+            const int m = (int)max((int64_t)0, min((int64_t)8, a.np - p));
+#pragma unroll 1
+            for (int r = lane / lanes; r < 32; r += 64 / lanes) {
+                const int64_t q = q0 + wq + j * 32 + r;
+                float v[8];
+                *(float4v *)v = *(const float4v *)(turn + r * kRow + col * 4);
+                *(float4v *)(v + 4) = *(const float4v *)(turn + r * kRow + col * 4 + 16);
+                if (q >= a.nq || m == 0) continue;
+                if (raw) {
+                    store8(a.part + ((int64_t)blockIdx.y * a.nq + q) * (G * a.np) + to_half + p, m, v);
+                } else {
+                    if (e.residual) {
+                        float u[8];
+                        load8(e.residual + q * e.ldr + p, m, u);
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) v[c] += u[c];
+                    }
+                    store8(e.y + q * e.ldy + p, m, v);
+                }
+            }
+        }
 }
 
 // The epilogue: eight outputs a thread, sixteen neighbouring lanes have a block of 128.
@@ -145,6 +498,11 @@ __global__ __launch_bounds__(256) void q8_join_kernel(Q8Product a, Q8Epilogue<T>
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             load8(a.part + q * a.np * G + g * a.np + p, n, v[g]);
+            for (int s = 1; s < a.splits; ++s) {
+                load8(a.part + ((int64_t)s * a.nq + q) * a.np * G + g * a.np + p, n, u);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[g][j] += u[j];
+            }
             if (e.bias) {
                 load8(e.bias + g * a.np + p, n, u);
 #pragma unroll
@@ -169,8 +527,6 @@ __global__ __launch_bounds__(256) void q8_join_kernel(Q8Product a, Q8Epilogue<T>
 }
 
 // ---------------------------------------------------------------- host side
-
-constexpr int64_t kMaxTiles = 1 << 22;   // and more are not launched: a launch holds fewer than 2^32 threads
 
 static int check_matrix(const char *op, int32_t dtype, int64_t m, int64_t d, const void *x, int64_t ld)
 {
@@ -213,6 +569,120 @@ int dequantize_impl(int32_t dtype, int64_t m, int64_t d, const Q8Arg &in, void *
     return VF_OK;
 }
 
+// The kernels of a product, by the sums that a workgroup computes.
+enum Q8Tiling {
+    kQ8Few,      // 16 rows of P, all rows of Q (at most 64)
+    kQ8Slim,     // 256 x 64, four waves
+    kQ8Square,   // 128 x 128, four waves; not for a gated output in 8 bits, which needs both halves of 128 outputs
+    kQ8Long,     // 256 x 128, four waves
+    kQ8Large,    // 256 x 256, eight waves
+};
+struct Q8Plan {
+    bool fits = true;     // false: no tiling has few enough tiles
+    Q8Tiling tiling = kQ8Few;
+    int splits = 0;       // 0: no join
+    int64_t chunk = 0;
+    size_t bytes = 0;
+};
+
+struct Q8Cost {
+    int bp, bq, together;
+    double step, alone, fixed;   // us per block of 128 with a full compute unit, at least `alone`; per workgroup
+};
+static Q8Cost q8_cost(Q8Tiling t, bool exact)
+{
+    switch (t) {
+    case kQ8Slim: return exact ? Q8Cost{256, 64, 2, 1.3, 0.7, 5.0} : Q8Cost{256, 64, 2, 0.9, 0.5, 5.0};
+    case kQ8Square: return exact ? Q8Cost{128, 128, 3, 1.9, 0.7, 5.0} : Q8Cost{128, 128, 3, 1.3, 0.5, 5.0};
+    case kQ8Long: return Q8Cost{256, 128, 2, 1.5, 0.8, 6.0};
+    default: return Q8Cost{256, 256, 1, 1.2, 0.8, 8.0};
+    }
+}
+
+// quantized: the output is in 8 bits; residual: there is one.
+static Q8Plan plan_q8(int32_t dtype, int64_t m, int64_t n, int64_t k, bool gated, bool quantized, bool residual)
+{
+    Q8Plan best;
+    const bool exact = dtype == VF_F32;
+    const int64_t blocks = ceil_div(k, kBlock), rows = gated ? 2 * n : n;
+    const size_t sums = (size_t)m * rows * 4;
+    if (m <= 64) {
+        best.splits = quantized ? 1 : 0;
+        best.chunk = blocks;
+        best.bytes = quantized ? sums : 0;
+        best.fits = ceil_div(n, 16) < kMaxTiles;
+        return best;
+    }
+    double least = 0;
+    for (Q8Tiling t : {kQ8Slim, kQ8Square, kQ8Long, kQ8Large}) {
+        if (exact && (t == kQ8Long || t == kQ8Large)) continue;
+        const Q8Cost c = q8_cost(t, exact);
+        const int64_t tiles = ceil_div(n, gated ? c.bp / 2 : c.bp) * ceil_div(m, c.bq);
+        if (tiles >= kMaxTiles) continue;
+        const bool joined = quantized && (residual || (gated && t == kQ8Square));   // the epilogue is the join's
+        for (int64_t splits : {1, 2, 3, 4, 6, 8, 12, 16}) {
+            const int64_t chunk = std::max<int64_t>(4, ceil_div(ceil_div(blocks, splits), 4) * 4);   // whole words of scales
+            const int64_t used = std::max<int64_t>(1, ceil_div(blocks, chunk));
+            if (splits > 1 && tiles * splits > 2048) break;
+            if (used != splits) continue;
+            const int64_t per_cu = ceil_div(tiles * used, 256), rounds = ceil_div(per_cu, c.together);
+            const double steps = (double)std::min(chunk, blocks);
+            const double last = (double)(per_cu - (rounds - 1) * c.together) / c.together;
+            double us = (double)(rounds - 1) * (steps * c.step + c.fixed) + steps * std::max(c.alone, c.step * last) + c.fixed;
+            if (used > 1 || joined) us += 5.5 + (double)used * sums * 2 / 4e6;
+            if (least == 0 || us < least) {
+                least = us;
+                best.tiling = t;
+                best.splits = used > 1 || joined ? (int)used : 0;
+                best.chunk = chunk;
+                best.bytes = best.splits ? sums * best.splits : 0;
+            }
+        }
+    }
+    best.fits = least > 0;
+    return best;
+}
+
+template <class T, bool EXACT, bool GATED, int BP, int BQ, int WP, int WQ, int STEPS>
+static int launch_q8(const Q8Product &a, const Q8Epilogue<T> &e, hipStream_t s)
+{
+    constexpr size_t lds = std::max<size_t>((size_t)STEPS * (BP + BQ) * 64 + 2 * (BP + BQ) * 4, (size_t)(BP + WP * BQ) * 4 + WP * WQ * 32 * 272);
+    static std::atomic<uint64_t> done{0};
+    if constexpr (lds > 64 * 1024)
+        if (int rc = allow_lds((const void *)q8_tile_kernel<T, EXACT, GATED, BP, BQ, WP, WQ, STEPS>, lds, done); rc != VF_OK) return rc;
+    const int64_t tiles = ceil_div(a.np, GATED ? BP / 2 : BP) * ceil_div(a.nq, BQ);
+    q8_tile_kernel<T, EXACT, GATED, BP, BQ, WP, WQ, STEPS><<<dim3((unsigned)tiles, (unsigned)std::max(a.splits, 1)), dim3(WP * WQ * 64), lds, s>>>(a, e);
+    return VF_OK;
+}
+
+template <class T, bool GATED> static int run_q8(const Q8Product &a, const Q8Epilogue<T> &e, Q8Tiling t, hipStream_t s)
+{
+    constexpr bool kExact = std::is_same_v<T, float>;
+    int rc = VF_OK;
+    if (t == kQ8Few) {
+        const int waves = (int)std::max<int64_t>(1, std::min<int64_t>(GATED ? 8 : 16, a.blocks));
+        const dim3 grid((unsigned)ceil_div(a.np, 16)), block(waves * 64);
+        if (a.nq <= 16) q8_few_rows_kernel<T, 1, GATED><<<grid, block, 0, s>>>(a, e);
+        else if (a.nq <= 32) q8_few_rows_kernel<T, 2, GATED><<<grid, block, 0, s>>>(a, e);
+        else q8_few_rows_kernel<T, 4, GATED><<<grid, block, 0, s>>>(a, e);
+    } else if (t == kQ8Slim) {
+        rc = launch_q8<T, kExact, GATED, 256, 64, 4, 1, 3>(a, e, s);
+    } else if (t == kQ8Square) {
+        rc = launch_q8<T, kExact, GATED, 128, 128, 2, 2, 3>(a, e, s);
+    } else if constexpr (!kExact) {
+        if (t == kQ8Long) rc = launch_q8<T, false, GATED, 256, 128, 2, 2, 3>(a, e, s);
+        else rc = launch_q8<T, false, GATED, 256, 256, 2, 4, 4>(a, e, s);
+    }
+    if (rc != VF_OK) return rc;
+    if (a.splits > 0) {
+        const dim3 join(grid_of(ceil_div(a.nq * ceil_div(a.np, kBlock), 16)));
+        if (e.y == nullptr) q8_join_kernel<T, GATED, true><<<join, dim3(256), 0, s>>>(a, e);
+        else q8_join_kernel<T, GATED, false><<<join, dim3(256), 0, s>>>(a, e);
+    }
+    VF_HIP(hipGetLastError());
+    return VF_OK;
+}
+
 static int check_q8_sizes(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t act)
 {
     VF_REQUIRE(is_float_type(dtype), "linear in 8 bits: dtype must be VF_F32, VF_BF16 or VF_F16");
@@ -225,7 +695,8 @@ int linear_q8_workspace_impl(int32_t dtype, int64_t m, int64_t n, int64_t k, int
 {
     VF_REQUIRE(bytes != nullptr, "linear in 8 bits: bytes is NULL");
     if (int rc = check_q8_sizes(dtype, m, n, k, 0); rc != VF_OK) return rc;
-    *bytes = (size_t)m * n * (gated ? 2 : 1) * 4;
+    VF_REQUIRE((gated == 0 || gated == 1) && (quantized == 0 || quantized == 1), "linear in 8 bits: gated and quantized must be 0 or 1");
+    *bytes = std::max(plan_q8(dtype, m, n, k, gated, quantized, false).bytes, plan_q8(dtype, m, n, k, gated, quantized, true).bytes);
     return VF_OK;
 }
 
@@ -243,9 +714,10 @@ int linear_q8_impl(const LinearQ8Args &a)
     VF_REQUIRE(!a.residual || a.ldr >= a.n, "linear in 8 bits: ldr is less than n");
     if (q8)
         if (int rc = check_q8("linear in 8 bits: the output", a.out, a.m, a.n); rc != VF_OK) return rc;
-    size_t need = 0;
-    if (int rc = linear_q8_workspace_impl(a.dtype, a.m, a.n, a.k, a.gated, q8, &need); rc != VF_OK) return rc;
-    if (int rc = check_workspace("linear in 8 bits", a.workspace, a.workspace_bytes, need); rc != VF_OK) return rc;
+    VF_REQUIRE(a.x.ld < (1 << 24) && a.w.ld < (1 << 24), "linear in 8 bits: rows of codes lie 2^24 bytes apart or more");   // (offsets within a tile have 32 bits)
+    const Q8Plan plan = plan_q8(a.dtype, a.m, a.n, a.k, a.gated, q8, a.residual != nullptr);
+    VF_REQUIRE(plan.fits, "linear in 8 bits: too many output tiles in one call");
+    if (int rc = check_workspace("linear in 8 bits", a.workspace, a.workspace_bytes, plan.bytes); rc != VF_OK) return rc;
     const size_t size = type_size(a.dtype);
     const Region y = region(a.y, a.m, a.n, a.ldy, size), r = region(a.residual, a.m, a.n, a.ldr, size), codes = codes_region(a.out, a.m, a.n),
                  scales = scales_region(a.out, a.m, a.n);
@@ -253,23 +725,14 @@ int linear_q8_impl(const LinearQ8Args &a)
         VF_REQUIRE(!overlap(y, in) && !overlap(codes, in) && !overlap(scales, in), "linear in 8 bits: an output overlaps an input");
     VF_REQUIRE(y.same(r) || !overlap(y, r), "linear in 8 bits: y overlaps the residual and is not it");
     VF_REQUIRE(!overlap(codes, r) && !overlap(scales, r) && !overlap(codes, scales), "linear in 8 bits: codes or scales overlap the residual or each other");
-    VF_REQUIRE(ceil_div(rows, 64) * ceil_div(a.m, 64) < kMaxTiles, "linear in 8 bits: too many output tiles in one call");
-    const Q8Product p{a.w, a.x, a.n, a.m, ceil_div(a.k, kBlock), (float *)a.workspace};
+    const Q8Product p{a.w, a.x, a.n, a.m, ceil_div(a.k, kBlock), plan.chunk, plan.splits, (float *)a.workspace};
+    int rc = VF_OK;
     by_type(a.dtype, [&](auto *t) {
         using T = std::remove_pointer_t<decltype(t)>;
-        constexpr bool kExact = std::is_same_v<T, float>;
         const Q8Epilogue<T> e{(const T *)a.bias, a.act, (const T *)a.residual, a.ldr, (T *)a.y, a.ldy, (uint8_t *)a.out.codes, (uint8_t *)a.out.scales, a.out.ld, a.out.lds};
-        const dim3 grid((unsigned)(ceil_div(rows, 64) * ceil_div(a.m, 64))), join(grid_of(ceil_div(a.m * ceil_div(a.n, kBlock), 16)));
-        auto run = [&](auto gated) {
-            q8_simple_kernel<kExact, gated.value><<<grid, dim3(256), 0, a.stream>>>(p);
-            if (q8) q8_join_kernel<T, gated.value, true><<<join, dim3(256), 0, a.stream>>>(p, e);
-            else q8_join_kernel<T, gated.value, false><<<join, dim3(256), 0, a.stream>>>(p, e);
-        };
-        if (a.gated) run(std::true_type());
-        else run(std::false_type());
+        rc = a.gated ? run_q8<T, true>(p, e, plan.tiling, a.stream) : run_q8<T, false>(p, e, plan.tiling, a.stream);
     });
-    VF_HIP(hipGetLastError());
-    return VF_OK;
+    return rc;
 }
 
 }  // namespace vf
