@@ -349,139 +349,109 @@ __global__ __launch_bounds__(WP *WQ * 64, 2) void q8_tile_kernel(Q8Product a, Q8
     for (; 2 * b + STEPS < steps; ++b) one_block(std::true_type(), b);
     for (; b < blocks; ++b) one_block(std::false_type(), b);
 
-    // ---- the end: bias, activation and gate where the sums lie: a lane has row lane % 32 of Q and four neighbours of P, sixteen times eight apart
+    // The end: each wave turns thirty-two rows of its sums at a time through LDS, so that a lane has eight neighbours of a row and a row's lanes whole stretches of it.
+    // (Bias, activation and gate where the sums lie would save half of the way through LDS; it was three times the code, every line of it run
+    // once a tile, and sums that did not fit the registers.)
+    constexpr int COLS = FP * 32, kRow = COLS * 4 + 16, kLanes = COLS / 8 / G;   // 16 bytes more: rows start in other banks
+    constexpr int kShare = kBlock / (COLS / G);      // waves that share a block of outputs (0: a wave has more than one)
+    static_assert(kShare >= 1, "");
+    unsigned char *turn = tiles + wave * (32 * kRow);
+    float *most = (float *)(tiles + WAVES * 32 * kRow);   // [WP][BQ]
+    const bool raw = a.splits > 0, q8 = e.y == nullptr;
+    const int64_t p = p0 + wp / G + lane % kLanes * 8;
+    const int m = (int)max((int64_t)0, min((int64_t)8, a.np - p));
+    const int col = GATED ? (lane % kLanes >> 2) * 64 + (lane & 3) * 8 : lane % kLanes * 8;   // of the sums; the other half's are 32 further
+    float bias[G][8];
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c) bias[g][c] = 0.f;
+        if (e.bias && !raw) load8(e.bias + g * a.np + p, m, bias[g]);
+    }
     __syncthreads();
-    float *bias = (float *)tiles;                       // [G][OUT]
-    float *most = bias + BP;                            // [WP][BQ]
-    unsigned char *turn = (unsigned char *)(most + WP * BQ) + wave * (32 * 272);
-    const bool raw = a.splits > 0;
-    if (!raw) {
-        for (int i = threadIdx.x; i < BP; i += WAVES * 64) {
-            const int64_t p = p0 + i % OUT;
-            bias[i] = e.bias && p < a.np ? (float)e.bias[(i / OUT) * a.np + p] : 0.f;
-        }
-        __syncthreads();
-        by_act(e.act, [&](auto act) {
 #pragma unroll
-            for (int i = 0; i < FP; i += G)
+    for (int j = 0; j < FQ; ++j) {
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    __builtin_amdgcn_sched_barrier(0);   // (all at once would not fit the registers)
-                    const int p = (wp + i * 32) / G + g * 8 + (lane >> 5) * 4;
-                    const float4v bg = *(const float4v *)(bias + p), bu = GATED ? *(const float4v *)(bias + OUT + p) : bg;
+        for (int i = 0; i < FP; ++i)
 #pragma unroll
-                    for (int j = 0; j < FQ; ++j)
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            float v = act_value<act.value, T>(acc[i][j][g * 4 + c] + bg[c]);
-                            if constexpr (GATED) v *= acc[i + 1][j][g * 4 + c] + bu[c];
-                            acc[i / G][j][g * 4 + c] = v;
-                        }
-                }
-        });
-    }
-    constexpr int FO = FP / G;                          // fragments of outputs
-    const int64_t p_first = p0 + wp / G;
-    if constexpr (OUT % kBlock == 0) if (!raw && e.y == nullptr) {
-        // 8 bits: the largest value of a row's 128 outputs, which lanes 32 apart and (gated) two waves share, then codes, turned through LDS into whole stretches of a row
-        constexpr int kShare = 128 / (FO * 32);         // waves that share a block
-        float top[FQ];
-#pragma unroll
-        for (int j = 0; j < FQ; ++j) {
-            top[j] = 0.f;
-#pragma unroll
-            for (int i = 0; i < FO; ++i)
-#pragma unroll
-                for (int g = 0; g < 4; ++g)
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const int64_t p = p_first + i * 32 + g * 8 + (lane >> 5) * 4 + c;
-                        if (p >= a.np) acc[i][j][g * 4 + c] = 0.f;
-                        top[j] = fmaxf(top[j], finite_size(acc[i][j][g * 4 + c]));
-                    }
-            top[j] = fmaxf(top[j], __shfl_xor(top[j], 32, 64));
-            if (kShare > 1 && lane < 32) most[(wave % WP) * BQ + wq + j * 32 + lane] = top[j];
-        }
-        if constexpr (kShare > 1) {
-            __syncthreads();
-#pragma unroll
-            for (int j = 0; j < FQ; ++j) {
-                const int first = wave % WP / kShare * kShare;
-#pragma unroll
-                for (int w = 0; w < kShare; ++w) top[j] = fmaxf(top[j], most[(first + w) * BQ + wq + j * 32 + (lane & 31)]);
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < FQ; ++j) {
-            const int byte = scale_byte(top[j]);
-            const float inverse = inverse_scale(byte);
-            const int64_t q = q0 + wq + j * 32 + (lane & 31);
-            if (lane < 32 && q < a.nq && p_first < a.np && wave % WP % kShare == 0) e.scales[q * e.lds + p_first / kBlock] = (uint8_t)byte;
-            constexpr int kRow = FO * 32 + 16;
-            wave_sync<true>();
-#pragma unroll
-            for (int i = 0; i < FO; ++i)
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    int u = __builtin_amdgcn_cvt_pk_fp8_f32(acc[i][j][g * 4] * inverse, acc[i][j][g * 4 + 1] * inverse, 0, false);
-                    u = __builtin_amdgcn_cvt_pk_fp8_f32(acc[i][j][g * 4 + 2] * inverse, acc[i][j][g * 4 + 3] * inverse, u, true);
-                    *(int *)(turn + (lane & 31) * kRow + i * 32 + g * 8 + (lane >> 5) * 4) = u;
-                }
-            wave_sync<true>();
-            constexpr int kLanes = FO * 2;              // lanes to a row, sixteen codes each
-            for (int r = lane / kLanes; r < 32; r += 64 / kLanes) {
-                const int64_t row = q0 + wq + j * 32 + r, p = p_first + lane % kLanes * 16;
-                if (row < a.nq && p < (a.np + kBlock - 1) / kBlock * kBlock) store_vec(e.codes + row * e.ldc + p, *(const uint4 *)(turn + r * kRow + lane % kLanes * 16));
-            }
-        }
-        return;
-    }
-    // a wide type (or the sums): 64 columns of 32 rows at a time, eight columns a lane
-#pragma unroll
-    for (int j = 0; j < FQ; ++j)
-#pragma unroll
-        for (int h = 0; h < FP; h += 2) {
-            if (!raw && h >= FO) continue;
-            constexpr int kRow = 272;
-            const bool two = h + 1 < (raw ? FP : FO);
-            wave_sync<true>();
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-                if (i == 0 || two)
-#pragma unroll
-                    for (int g = 0; g < 4; ++g)
-                        *(float4v *)(turn + (lane & 31) * kRow + i * 128 + (g * 8 + (lane >> 5) * 4) * 4) =
-                            float4v{acc[h + i < FP ? h + i : h][j][g * 4], acc[h + i < FP ? h + i : h][j][g * 4 + 1], acc[h + i < FP ? h + i : h][j][g * 4 + 2],
-                                    acc[h + i < FP ? h + i : h][j][g * 4 + 3]};
-            wave_sync<true>();
-            const int lanes = two ? 8 : 4, col = lane % lanes * 8;
-            int64_t p = p_first + h * 32 + col;
-            int64_t to_half = 0;
-            if (raw && GATED) {   // fragment h is the gate's, the next one the other half's
-                p = p_first + h / 2 * 32 + col % 32;
-                to_half = col >= 32 ? a.np : 0;
-            }
-            const int m = (int)max((int64_t)0, min((int64_t)8, a.np - p));
+            for (int g = 0; g < 4; ++g)
+                *(float4v *)(turn + (lane & 31) * kRow + (i * 32 + g * 8 + (lane >> 5) * 4) * 4) =
+                    float4v{acc[i][j][g * 4], acc[i][j][g * 4 + 1], acc[i][j][g * 4 + 2], acc[i][j][g * 4 + 3]};
+        wave_sync<true>();
 #pragma unroll 1
-            for (int r = lane / lanes; r < 32; r += 64 / lanes) {
-                const int64_t q = q0 + wq + j * 32 + r;
-                float v[8];
-                *(float4v *)v = *(const float4v *)(turn + r * kRow + col * 4);
-                *(float4v *)(v + 4) = *(const float4v *)(turn + r * kRow + col * 4 + 16);
-                if (q >= a.nq || m == 0) continue;
-                if (raw) {
-                    store8(a.part + ((int64_t)blockIdx.y * a.nq + q) * (G * a.np) + to_half + p, m, v);
-                } else {
-                    if (e.residual) {
-                        float u[8];
-                        load8(e.residual + q * e.ldr + p, m, u);
+        for (int r = lane / kLanes; r < 32; r += 64 / kLanes) {
+            const int64_t q = q0 + wq + j * 32 + r;
+            float v[G][8];
 #pragma unroll
-                        for (int c = 0; c < 8; ++c) v[c] += u[c];
-                    }
-                    store8(e.y + q * e.ldy + p, m, v);
+            for (int g = 0; g < G; ++g) {
+                const unsigned char *from = turn + r * kRow + (col + g * 32) * 4;
+                *(float4v *)v[g] = *(const float4v *)from;
+                *(float4v *)(v[g] + 4) = *(const float4v *)(from + 16);
+            }
+            if (raw) {
+                if (q < a.nq) {
+#pragma unroll
+                    for (int g = 0; g < G; ++g) store8(a.part + ((int64_t)blockIdx.y * a.nq + q) * (G * a.np) + g * a.np + p, m, v[g]);
+                }
+                continue;
+            }
+            by_act(e.act, [&](auto act) {
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    v[0][c] = act_value<act.value, T>(v[0][c] + bias[0][c]);
+                    if constexpr (GATED) v[0][c] *= v[1][c] + bias[1][c];
+                }
+            });
+            if (e.residual && q < a.nq) {
+                float u[8];
+                load8(e.residual + q * e.ldr + p, m, u);
+#pragma unroll
+                for (int c = 0; c < 8; ++c) v[0][c] += u[c];
+            }
+            if (!q8) {
+                if (q < a.nq) store8(e.y + q * e.ldy + p, m, v[0]);
+                continue;
+            }
+            if constexpr (OUT % kBlock == 0) {
+#pragma unroll
+                for (int c = 0; c < 8; ++c) v[0][c] = c < m ? v[0][c] : 0.f;
+                if constexpr (kShare == 1) {
+                    if (q < a.nq && p0 + wp / G < a.np) keep_block(v[0], e.codes + q * e.ldc + p, e.scales + q * e.lds + p / kBlock);
+                } else {   // back to where the sums were, until the other waves have their share of the row's largest value
+                    unsigned char *to = turn + r * kRow + col * 4;
+                    *(float4v *)to = *(const float4v *)v[0];
+                    *(float4v *)(to + 16) = *(const float4v *)(v[0] + 4);
+                    float top = most_of8(v[0]);
+                    top = fmaxf(top, dpp<0xB1>(top));
+                    top = fmaxf(top, dpp<0x4E>(top));
+                    if constexpr (kLanes == 8) top = fmaxf(top, dpp<0x141>(top));
+                    if (lane % kLanes == 0) most[wave % WP * BQ + wq + j * 32 + r] = top;
                 }
             }
         }
+        if constexpr (OUT % kBlock == 0 && kShare > 1) {
+            if (!raw && q8) {
+                __syncthreads();
+#pragma unroll 1
+                for (int r = lane / kLanes; r < 32; r += 64 / kLanes) {
+                    const int64_t q = q0 + wq + j * 32 + r;
+                    float v[8], top = 0.f;
+                    const unsigned char *from = turn + r * kRow + col * 4;
+                    *(float4v *)v = *(const float4v *)from;
+                    *(float4v *)(v + 4) = *(const float4v *)(from + 16);
+#pragma unroll
+                    for (int w = 0; w < kShare; ++w) top = fmaxf(top, most[(wave % WP / kShare * kShare + w) * BQ + wq + j * 32 + r]);
+                    const int byte = scale_byte(top);
+                    // (the block's columns beyond the last output are filled up with zeros; blocks beyond the last one are not written)
+                    if (q < a.nq && p < (a.np + kBlock - 1) / kBlock * kBlock) {
+                        store_vec(e.codes + q * e.ldc + p, encode8(v, inverse_scale(byte)));
+                        if (lane % kLanes == 0 && wave % WP % kShare == 0) e.scales[q * e.lds + p / kBlock] = (uint8_t)byte;
+                    }
+                }
+            }
+        }
+        wave_sync<true>();
+    }
 }
 
 // The epilogue: eight outputs a thread, sixteen neighbouring lanes have a block of 128.
@@ -599,8 +569,8 @@ static Q8Cost q8_cost(Q8Tiling t, bool exact)
     }
 }
 
-// quantized: the output is in 8 bits; residual: there is one.
-static Q8Plan plan_q8(int32_t dtype, int64_t m, int64_t n, int64_t k, bool gated, bool quantized, bool residual)
+// quantized: the output is in 8 bits.
+static Q8Plan plan_q8(int32_t dtype, int64_t m, int64_t n, int64_t k, bool gated, bool quantized)
 {
     Q8Plan best;
     const bool exact = dtype == VF_F32;
@@ -619,7 +589,7 @@ static Q8Plan plan_q8(int32_t dtype, int64_t m, int64_t n, int64_t k, bool gated
         const Q8Cost c = q8_cost(t, exact);
         const int64_t tiles = ceil_div(n, gated ? c.bp / 2 : c.bp) * ceil_div(m, c.bq);
         if (tiles >= kMaxTiles) continue;
-        const bool joined = quantized && (residual || (gated && t == kQ8Square));   // the epilogue is the join's
+        const bool joined = quantized && gated && t == kQ8Square;   // the epilogue is the join's
         for (int64_t splits : {1, 2, 3, 4, 6, 8, 12, 16}) {
             const int64_t chunk = std::max<int64_t>(4, ceil_div(ceil_div(blocks, splits), 4) * 4);   // whole words of scales
             const int64_t used = std::max<int64_t>(1, ceil_div(blocks, chunk));
@@ -646,7 +616,7 @@ static Q8Plan plan_q8(int32_t dtype, int64_t m, int64_t n, int64_t k, bool gated
 template <class T, bool EXACT, bool GATED, int BP, int BQ, int WP, int WQ, int STEPS>
 static int launch_q8(const Q8Product &a, const Q8Epilogue<T> &e, hipStream_t s)
 {
-    constexpr size_t lds = std::max<size_t>((size_t)STEPS * (BP + BQ) * 64 + 2 * (BP + BQ) * 4, (size_t)(BP + WP * BQ) * 4 + WP * WQ * 32 * 272);
+    constexpr size_t lds = std::max<size_t>((size_t)STEPS * (BP + BQ) * 64 + 2 * (BP + BQ) * 4, (size_t)WP * WQ * 32 * (BP / WP * 4 + 16) + WP * BQ * 4);
     static std::atomic<uint64_t> done{0};
     if constexpr (lds > 64 * 1024)
         if (int rc = allow_lds((const void *)q8_tile_kernel<T, EXACT, GATED, BP, BQ, WP, WQ, STEPS>, lds, done); rc != VF_OK) return rc;
@@ -696,7 +666,7 @@ int linear_q8_workspace_impl(int32_t dtype, int64_t m, int64_t n, int64_t k, int
     VF_REQUIRE(bytes != nullptr, "linear in 8 bits: bytes is NULL");
     if (int rc = check_q8_sizes(dtype, m, n, k, 0); rc != VF_OK) return rc;
     VF_REQUIRE((gated == 0 || gated == 1) && (quantized == 0 || quantized == 1), "linear in 8 bits: gated and quantized must be 0 or 1");
-    *bytes = std::max(plan_q8(dtype, m, n, k, gated, quantized, false).bytes, plan_q8(dtype, m, n, k, gated, quantized, true).bytes);
+    *bytes = plan_q8(dtype, m, n, k, gated, quantized).bytes;
     return VF_OK;
 }
 
@@ -715,7 +685,7 @@ int linear_q8_impl(const LinearQ8Args &a)
     if (q8)
         if (int rc = check_q8("linear in 8 bits: the output", a.out, a.m, a.n); rc != VF_OK) return rc;
     VF_REQUIRE(a.x.ld < (1 << 24) && a.w.ld < (1 << 24), "linear in 8 bits: rows of codes lie 2^24 bytes apart or more");   // (offsets within a tile have 32 bits)
-    const Q8Plan plan = plan_q8(a.dtype, a.m, a.n, a.k, a.gated, q8, a.residual != nullptr);
+    const Q8Plan plan = plan_q8(a.dtype, a.m, a.n, a.k, a.gated, q8);
     VF_REQUIRE(plan.fits, "linear in 8 bits: too many output tiles in one call");
     if (int rc = check_workspace("linear in 8 bits", a.workspace, a.workspace_bytes, plan.bytes); rc != VF_OK) return rc;
     const size_t size = type_size(a.dtype);
