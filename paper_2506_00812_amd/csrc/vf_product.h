@@ -377,6 +377,17 @@ __device__ __forceinline__ void store_tile(const Product<T> &a, const Epilogue<T
     }
 }
 
+// Where workgroup `group` of `groups` works: tile number p of P and q of Q, of tiles_p and tiles_q.  Neighbouring workgroups go to the eight XCDs in turn: each XCD
+// takes a run of tiles, and a run goes through bands of H tiles of Q, so that the tiles in work at the same time share what its L2 has to fetch from either operand.
+template <int H> __device__ __forceinline__ void place_tile(int64_t group, int64_t groups, int64_t tiles_p, int64_t tiles_q, int64_t &p, int64_t &q)
+{
+    const int64_t xcd = group & 7, run = groups / 8, left = groups % 8;
+    const int64_t tile = xcd * run + min(xcd, left) + (group >> 3);
+    const int64_t band = tile / (H * tiles_p), at = tile - band * (H * tiles_p), high = min((int64_t)H, tiles_q - band * H);
+    p = at / high;
+    q = band * H + (at - p * high);
+}
+
 // BP x BQ outputs per workgroup of WP x WQ waves; two tiles of each operand in LDS, one being read while the other is filled through
 // registers, which takes any alignment.  128 x 128 outputs by eight waves, 10,000 x 4,096 x 1,024: float32 123 - 132 TFLOP/s (the library's
 // product 137 - 154), bfloat16 with rows that start anywhere 530 - 720; four waves reach half of that (one wave per SIMD waits
@@ -389,10 +400,10 @@ __global__ __launch_bounds__(WP *WQ * 64) void tile_kernel(Product<T> a, Epilogu
     extern __shared__ __align__(16) unsigned char tiles[];   // [2][(BP + BQ) * kRowBytes]
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t tiles_p = (a.np + OUT - 1) / OUT;
-    // neighbouring workgroups go to the eight XCDs in turn: each XCD takes a run of neighbouring tiles, whose operands its L2 holds
-    const int64_t n = gridDim.x, xcd = blockIdx.x & 7, run = n / 8, left = n % 8;
-    const int64_t tile = xcd * run + min(xcd, left) + (blockIdx.x >> 3);
-    const int64_t p0 = tile % tiles_p * OUT, q0 = tile / tiles_p * BQ;
+    int64_t p0, q0;
+    place_tile<8>(blockIdx.x, gridDim.x, tiles_p, (a.nq + BQ - 1) / BQ, p0, q0);
+    p0 *= OUT;
+    q0 *= BQ;
     const int64_t c_first = (int64_t)blockIdx.y * a.chunk, c_end = min(a.nc, c_first + a.chunk);
     const bool p_whole = PC || p0 + BP <= a.np, q_whole = QC || q0 + BQ <= a.nq;
 
@@ -502,9 +513,10 @@ __global__ __launch_bounds__(WP *WQ * 64, 2) void direct_kernel(Product<T> a, Ep
     extern __shared__ __align__(16) unsigned char tiles[];   // [STEPS][P, Q][rows of 64 bytes, or 32 lines]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t tiles_p = (a.np + OUT - 1) / OUT;
-    const int64_t n = gridDim.x, xcd = blockIdx.x & 7, run = n / 8, left = n % 8;
-    const int64_t tile = xcd * run + min(xcd, left) + (blockIdx.x >> 3);
-    const int64_t p0 = tile % tiles_p * OUT, q0 = tile / tiles_p * BQ;
+    int64_t p0, q0;
+    place_tile<(BP * BQ > 32768 ? 4 : 8)>(blockIdx.x, gridDim.x, tiles_p, (a.nq + BQ - 1) / BQ, p0, q0);
+    p0 *= OUT;
+    q0 *= BQ;
     const int64_t c_first = (int64_t)blockIdx.y * a.chunk, c_end = min(a.nc, c_first + a.chunk);
     const int steps = (int)max((int64_t)0, (c_end - c_first) / BC);
 

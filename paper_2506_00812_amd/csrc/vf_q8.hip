@@ -230,9 +230,10 @@ __global__ __launch_bounds__(WP *WQ * 64, 2) void q8_tile_kernel(Q8Product a, Q8
     extern __shared__ __align__(16) unsigned char tiles[];   // [STEPS][P, Q][rows of 64 bytes], [2][P, Q] words of scales
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t tiles_p = (a.np + OUT - 1) / OUT;
-    const int64_t n = gridDim.x, xcd = blockIdx.x & 7, run = n / 8, left = n % 8;
-    const int64_t tile = xcd * run + min(xcd, left) + (blockIdx.x >> 3);
-    const int64_t p0 = tile % tiles_p * OUT, q0 = tile / tiles_p * BQ;
+    int64_t p0, q0;
+    place_tile<(BP * BQ > 32768 ? 4 : 8)>(blockIdx.x, gridDim.x, tiles_p, (a.nq + BQ - 1) / BQ, p0, q0);
+    p0 *= OUT;
+    q0 *= BQ;
     const int64_t b_first = (int64_t)blockIdx.y * a.chunk;
     const int blocks = (int)max((int64_t)0, min(a.blocks - b_first, a.chunk)), steps = 2 * blocks;
 
