@@ -920,25 +920,28 @@ class Q8(NamedTuple):
 
 
 def _q8_empty(like, rows, cols, stream):
+    """A new matrix in 8 bits, and what _q8 says of it."""
     blocks = -(-cols // Q8_BLOCK)
-    return Q8(_empty(like, (rows, blocks * Q8_BLOCK), _torch.float8_e4m3fn, stream), _empty(like, (rows, -(-blocks // 4) * 4), _torch.uint8, stream), cols)
+    width, words = blocks * Q8_BLOCK, -(-blocks // 4) * 4
+    codes, scales = _empty(like, (rows, width), _torch.float8_e4m3fn, stream), _empty(like, (rows, words), _torch.uint8, stream)
+    return Q8(codes, scales, cols), (codes.data_ptr(), width, scales.data_ptr(), words)
 
 
 def _q8(q, what, dev, rows=None, cols=None):
     """(address of the codes, their ld, address of the scales, their ld) of a matrix in 8 bits."""
     if not isinstance(q, Q8):
         raise VecflowError(f"{what} must be a Q8")
-    n, d = q.codes.shape[0], q.cols
+    codes, scales, d = q
+    n = codes.shape[0]
     if d < 0 or (rows is not None and n != rows) or (cols is not None and d != cols):
         raise VecflowError(f"{what} must have shape [{n if rows is None else rows}, {d if cols is None else cols}], not [{n}, {d}]")
     blocks = -(-d // Q8_BLOCK)
-    ld = _matrix(q.codes, f"{what}: codes", _torch.float8_e4m3fn, dev, n, blocks * Q8_BLOCK)
-    lds = _matrix(q.scales, f"{what}: scales", _torch.uint8, dev, n, -(-blocks // 4) * 4)
-    return q.codes.data_ptr(), ld, q.scales.data_ptr(), lds
+    ld = _matrix(codes, f"{what}: codes", _torch.float8_e4m3fn, dev, n, blocks * Q8_BLOCK)
+    lds = _matrix(scales, f"{what}: scales", _torch.uint8, dev, n, -(-blocks // 4) * 4)
+    return codes.data_ptr(), ld, scales.data_ptr(), lds
 
 
-def _no_q8():
-    return None, 0, None, 0
+_NO_Q8 = (None, 0, None, 0)
 
 
 def quantize(x, stream=None):
@@ -947,8 +950,8 @@ def quantize(x, stream=None):
     code, T, dev, handle = _first(x, "x", stream)
     ldx = _matrix(x, "x", T, dev)
     m, d = x.shape
-    q = _q8_empty(x, m, d, stream)
-    _check(L.vf_quantize(code, m, d, x.data_ptr(), ldx, *_q8(q, "the output", dev), handle))
+    q, at = _q8_empty(x, m, d, stream)
+    _check(L.vf_quantize(code, m, d, x.data_ptr(), ldx, *at, handle))
     return q
 
 
@@ -1004,12 +1007,12 @@ def linear_q8(x, weight, bias=None, residual=None, activation="none", gated=Fals
     if quantize:
         if out is not None:
             raise VecflowError("out is for a wide output")
-        y = _q8_empty(x.codes, m, n, stream)
-        py, ldy, po = None, 0, _q8(y, "the output", dev)
+        y, po = _q8_empty(x.codes, m, n, stream)
+        py, ldy = None, 0
     else:
         y = _empty(x.codes, (m, n), dtype, stream) if out is None else out
         ldy = _matrix(y, "out", dtype, dev, m, n)
-        py, po = y.data_ptr(), _no_q8()
+        py, po = y.data_ptr(), _NO_Q8
     nw = _size_of("vf_linear_quantized_workspace", code, m, n, k, int(gated), int(quantize))
     _ws, pw = _workspace(x.codes, nw, stream)
     _check(L.vf_linear_quantized(code, m, n, k, *px, *pw8, pb, act, int(gated), None if residual is None else residual.data_ptr(), ldr, py, ldy, *po, pw, nw,
@@ -1036,11 +1039,11 @@ def rms_norm(x, weight=None, residual=None, eps=1e-6, save=False, quantize=False
     if quantize:
         if out is not None:
             raise VecflowError("out is for a wide output")
-        y = _q8_empty(x, m, d, stream)
-        py, ldy, po = None, 0, _q8(y, "the output", dev)
+        y, po = _q8_empty(x, m, d, stream)
+        py, ldy = None, 0
     else:
         y = _empty(x, (m, d), T, stream) if out is None else out
-        py, ldy, po = y.data_ptr(), _matrix(y, "out", T, dev, m, d), _no_q8()
+        py, ldy, po = y.data_ptr(), _matrix(y, "out", T, dev, m, d), _NO_Q8
     rstd = _empty(x, (m,), _torch.float32, stream) if save else None
     _check(L.vf_rms_norm(code, m, d, x.data_ptr(), ldx, pr, ldr, pg, eps, py, ldy, *po, pt, ldt, rstd.data_ptr() if save else None, handle))
     if total is None:

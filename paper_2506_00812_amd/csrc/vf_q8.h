@@ -39,9 +39,14 @@ __device__ __forceinline__ float finite_size(float v)
 }
 __device__ __forceinline__ float most_of8(const float (&v)[8])
 {
-    float most = finite_size(v[0]);
+    float most = 0.f;
 #pragma unroll
-    for (int j = 1; j < 8; ++j) most = fmaxf(most, finite_size(v[j]));
+    for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(v[j]));   // (passes over NaN)
+    if (most > kFltMax) {   // only what is finite counts
+        most = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) most = fmaxf(most, finite_size(v[j]));
+    }
     return most;
 }
 // Sixteen neighbouring lanes have a block, eight columns each (zeros beyond the row): their codes, and from the first lane the scale.
@@ -53,7 +58,7 @@ __device__ __forceinline__ void keep_block(const float (&v)[8], uint8_t *codes, 
     if ((threadIdx.x & 15) == 0) *scale = (uint8_t)byte;
 }
 
-// Eight neighbours of a row as float32, n of which exist; the others are `fill`.
+// Eight neighbours of a row as float32, n of which exist; the others are `fill`.  A part of them comes as four, two and one, the last of them first.
 template <class T> __device__ __forceinline__ void load8(const T *p, int n, float (&v)[8], float fill = 0.f)
 {
     if (n >= 8) {
@@ -64,27 +69,59 @@ template <class T> __device__ __forceinline__ void load8(const T *p, int n, floa
 #pragma unroll
             for (int j = 0; j < V; ++j) v[i * V + j] = (float)u[j];
         }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = j < n ? (float)p[j] : fill;
+        return;
     }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = fill;
+    if (n <= 0) return;
+    auto some = [&](auto count) {
+        constexpr int N = count.value;
+        using S = T __attribute__((ext_vector_type(N)));
+        if (n & N) {
+            const S u = load_vec<S>(p + (n & ~(2 * N - 1)));
+#pragma unroll
+            for (int j = 7; j >= N; --j) v[j] = v[j - N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[j] = (float)u[j];
+        }
+    };
+    some(std::integral_constant<int, 1>());
+    some(std::integral_constant<int, 2>());
+    some(std::integral_constant<int, 4>());
 }
 template <class T> __device__ __forceinline__ void store8(T *p, int n, const float (&v)[8])
 {
+    T u[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) u[j] = (T)v[j];
     if (n >= 8) {
         constexpr int V = kVec<T>;
 #pragma unroll
         for (int i = 0; i < 8 / V; ++i) {
-            Vec<T> u;
+            Vec<T> w;
 #pragma unroll
-            for (int j = 0; j < V; ++j) u[j] = (T)v[i * V + j];
-            store_vec(p + i * V, u);
+            for (int j = 0; j < V; ++j) w[j] = u[i * V + j];
+            store_vec(p + i * V, w);
         }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (j < n) p[j] = (T)v[j];
+        return;
     }
+    if (n <= 0) return;
+    auto some = [&](auto count) {
+        constexpr int N = count.value;
+        using S = T __attribute__((ext_vector_type(N)));
+        if (n & N) {
+            S w;
+#pragma unroll
+            for (int j = 0; j < N; ++j) w[j] = u[j];
+            store_vec(p, w);
+            p += N;
+#pragma unroll
+            for (int j = 0; j < N; ++j) u[j] = u[j + N];   // (what is left has fewer than N)
+        }
+    };
+    some(std::integral_constant<int, 4>());
+    some(std::integral_constant<int, 2>());
+    some(std::integral_constant<int, 1>());
 }
 
 // The operand of an entry point.

@@ -202,11 +202,12 @@ __device__ __forceinline__ int half_row32(int r) { return (r >> 6) * 32 + (r & 3
 // 12-15, 20-27 and so on), sixteen of a fragment's thirty-two rows, touch sixteen different ones.
 __device__ __forceinline__ int q8_chunk(int r, int ch) { return ch ^ (r >> 2 & 3); }
 
-__device__ __forceinline__ int8v q8_fragment(const unsigned char *tile, int r0, int lane)
+// The fragment whose lanes have rows `row` of the tile.
+__device__ __forceinline__ int8v q8_fragment(const unsigned char *tile, int row, int lane)
 {
     typedef int int4v __attribute__((ext_vector_type(4)));
-    const int r = r0 + (lane & 31), ch = (lane >> 5) * 2;
-    const int4v lo = *(const int4v *)(tile + r * 64 + (q8_chunk(r, ch) << 4)), hi = *(const int4v *)(tile + r * 64 + (q8_chunk(r, ch + 1) << 4));
+    const int ch = (lane >> 5) * 2;
+    const int4v lo = *(const int4v *)(tile + row * 64 + (q8_chunk(row, ch) << 4)), hi = *(const int4v *)(tile + row * 64 + (q8_chunk(row, ch + 1) << 4));
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
@@ -220,10 +221,9 @@ __device__ __forceinline__ void request4(const void *from, uint32_t to)
 // step t's fragments are multiplied, those of step t + 1 are read, and steps up to t + STEPS - 1 are on their way.  The
 // scales of four blocks, eight steps, come a 32-bit word a row; a word's next byte is shifted down every other step.
 template <class T, bool EXACT, bool GATED, int BP, int BQ, int WP, int WQ, int STEPS>
-__global__ __launch_bounds__(WP *WQ * 64, 2) void q8_tile_kernel(Q8Product a, Q8Epilogue<T> e)
+__global__ __launch_bounds__(WP *WQ * 64, BP *BQ == 16384 ? 3 : 2) void q8_tile_kernel(Q8Product a, Q8Epilogue<T> e)
 {
     constexpr int G = GATED ? 2 : 1, OUT = BP / G, WAVES = WP * WQ, FP = BP / WP / 32, FQ = BQ / WQ / 32;
-    static_assert(FP % G == 0, "");
     constexpr int NP = BP / 16, NQ = BQ / 16;   // loads of a step; where they do not divide among the waves the last one is made twice
     constexpr int LP = (NP + WAVES - 1) / WAVES, LQ = (NQ + WAVES - 1) / WAVES, LOADS = LP + LQ;
     constexpr int NS = (BP + BQ) / 64, LS = (NS + WAVES - 1) / WAVES, kStep = (BP + BQ) * 64;
@@ -283,22 +283,26 @@ __global__ __launch_bounds__(WP *WQ * 64, 2) void q8_tile_kernel(Q8Product a, Q8
         for (int i = 0; i < LS; ++i)
             request4(scales[i] + group * 4, lds0 + STEPS * kStep + (group & 1) * ((BP + BQ) * 4) + min(wave * LS + i, NS - 1) * 256);
     };
-    const int wp = wave % WP * (FP * 32), wq = wave / WP * (FQ * 32);
+    const int wp = wave % WP * (FP * 32), wq = wave / WP * (FQ * 32), row = lane & 31;
+    // Two workgroups share a compute unit: the second of each begins later, by some two thirds of a loop alone, so that one's matrix instructions have the time in
+    // which the other's outputs are computed and written (10,000 x 4,096 x 1,024, gated into 8 bits: 103 us, side by side 112).
+    if (BP * BQ == 32768 && (blockIdx.x >> 8) == 1 && gridDim.x > 512)
+        for (int i = 0; i < blocks; ++i) __builtin_amdgcn_s_sleep(32);
     float16v acc[FP][FQ] = {};
     int8v fp[FP], fq[2][FQ];
     int sp[FP], sq[FQ];
     auto read_scales = [&](int group) {
-        const int *w = (const int *)(words + (group & 1) * ((BP + BQ) * 4)) + (lane & 31);
+        const int *w = (const int *)(words + (group & 1) * ((BP + BQ) * 4));
 #pragma unroll
-        for (int i = 0; i < FP; ++i) sp[i] = w[wp + i * 32];
+        for (int i = 0; i < FP; ++i) sp[i] = w[wp + i * 32 + row];
 #pragma unroll
-        for (int j = 0; j < FQ; ++j) sq[j] = w[BP + wq + j * 32];
+        for (int j = 0; j < FQ; ++j) sq[j] = w[BP + wq + j * 32 + row];
     };
     // A step in parts, one for each fragment of P: its matrix instructions, then the same fragment of the next step into the registers that they have read; Q's
     // fragments have two sets.  Step t + STEPS - 1 goes into the buffer of step t - 1, whose fragments everybody has used before this step's barrier: the last reads
     // of a step's own may still be on their way there.  MORE: step t + STEPS - 1 exists.
     auto one_step = [&](auto more, int t, int set) {
-        constexpr int kParts = FP, kTail = 2 * FQ;   // LDS reads of Q's fragments
+        constexpr int kParts = FP;
         __builtin_amdgcn_sched_barrier(0);
         if (more.value || t + STEPS - 2 < steps) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((STEPS - 3) * LOADS) : "memory");
         else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
@@ -308,14 +312,16 @@ __global__ __launch_bounds__(WP *WQ * 64, 2) void q8_tile_kernel(Q8Product a, Q8
         for (int g = 0; g < kParts; ++g) {
             __builtin_amdgcn_sched_barrier(0);
             if (request_more) request_some(t + STEPS - 1, g * LOADS / kParts, (g + 1) * LOADS / kParts);
+            // (the next step begins with these: read early, they are there by then)
+#pragma unroll
+            for (int f = 0; f < FQ; ++f)
+                if (min(f, kParts - 1) == g) fq[set ^ 1][f] = q8_fragment(at + BP * 64, wq + f * 32 + row, lane);
 #pragma unroll
             for (int j = 0; j < FQ; ++j) acc[g][j] = mma32<EXACT>(fp[g], sp[g], fq[set][j], sq[j], acc[g][j]);
             // (here, and the sums in their own registers: the compiler would gather the step's matrix instructions at its end, and keep all of its reads until then)
 #pragma unroll
             for (int j = 0; j < FQ; ++j) asm volatile("" : "+a"(acc[g][j])::"memory");
-#pragma unroll
-            for (int f = g * FQ / kParts; f < (g + 1) * FQ / kParts; ++f) fq[set ^ 1][f] = q8_fragment(at + BP * 64, wq + f * 32, lane);
-            fp[g] = q8_fragment(at, wp + g * 32, lane);
+            fp[g] = q8_fragment(at, wp + g * 32 + row, lane);
         }
     };
     if (steps > 0) {
@@ -325,9 +331,9 @@ __global__ __launch_bounds__(WP *WQ * 64, 2) void q8_tile_kernel(Q8Product a, Q8
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         asm volatile("s_barrier" ::: "memory");
 #pragma unroll
-        for (int j = 0; j < FQ; ++j) fq[0][j] = q8_fragment(tiles + BP * 64, wq + j * 32, lane);
+        for (int j = 0; j < FQ; ++j) fq[0][j] = q8_fragment(tiles + BP * 64, wq + j * 32 + row, lane);
 #pragma unroll
-        for (int i = 0; i < FP; ++i) fp[i] = q8_fragment(tiles, wp + i * 32, lane);
+        for (int i = 0; i < FP; ++i) fp[i] = q8_fragment(tiles, wp + i * 32 + row, lane);
         read_scales(0);
     }
     // The words of the next four blocks are asked for at the first of four, into the half that the last four have left (their words were read before this
@@ -350,37 +356,35 @@ __global__ __launch_bounds__(WP *WQ * 64, 2) void q8_tile_kernel(Q8Product a, Q8
     for (; 2 * b + STEPS < steps; ++b) one_block(std::true_type(), b);
     for (; b < blocks; ++b) one_block(std::false_type(), b);
 
-    // The end: each wave turns thirty-two rows of its sums at a time through LDS, so that a lane has eight neighbours of a row and a row's lanes whole stretches of it.
-    // (Bias, activation and gate where the sums lie would save half of the way through LDS; it was three times the code, every line of it run
-    // once a tile, and sums that did not fit the registers.)
-    constexpr int COLS = FP * 32, kRow = COLS * 4 + 16, kLanes = COLS / 8 / G;   // 16 bytes more: rows start in other banks
-    constexpr int kShare = kBlock / (COLS / G);      // waves that share a block of outputs (0: a wave has more than one)
-    static_assert(kShare >= 1, "");
-    unsigned char *turn = tiles + wave * (32 * kRow);
-    float *most = (float *)(tiles + WAVES * 32 * kRow);   // [WP][BQ]
+    // The end: thirty-two rows of sums at a time are turned through LDS, all of a row's by the waves that have them, so that a lane has eight neighbours, a row's lanes
+    // whole stretches of it and sixteen of them a block of 128 with its scale.  (Written from where the sums lie it was eight times the code, which runs once a
+    // tile and comes from memory each time: 10,000 x 4,096 x 1,024 with GELU 93 us, 78 this way.)
+    constexpr int kRow = BP * 4 + 16, kLanes = OUT / 8, kRows = 32 / WP;   // 16 bytes more: rows start in other banks; rows of a wave
+    static_assert(kLanes <= 64 && kRows % (64 / kLanes) == 0, "");
+    unsigned char *turn = tiles + wave / WP * (32 * kRow);
     const bool raw = a.splits > 0, q8 = e.y == nullptr;
-    const int64_t p = p0 + wp / G + lane % kLanes * 8;
+    const int64_t p = p0 + lane % kLanes * 8;
     const int m = (int)max((int64_t)0, min((int64_t)8, a.np - p));
     const int col = GATED ? (lane % kLanes >> 2) * 64 + (lane & 3) * 8 : lane % kLanes * 8;   // of the sums; the other half's are 32 further
     float bias[G][8];
+    if (e.bias && !raw) {
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
-#pragma unroll
-        for (int c = 0; c < 8; ++c) bias[g][c] = 0.f;
-        if (e.bias && !raw) load8(e.bias + g * a.np + p, m, bias[g]);
+        for (int g = 0; g < G; ++g) load8(e.bias + g * a.np + p, m, bias[g]);
     }
-    __syncthreads();
 #pragma unroll
     for (int j = 0; j < FQ; ++j) {
+        __syncthreads();   // the last step's fragments, or the last rows, have been read
 #pragma unroll
         for (int i = 0; i < FP; ++i)
 #pragma unroll
             for (int g = 0; g < 4; ++g)
-                *(float4v *)(turn + (lane & 31) * kRow + (i * 32 + g * 8 + (lane >> 5) * 4) * 4) =
+                *(float4v *)(turn + row * kRow + (wp + i * 32 + g * 8 + (lane >> 5) * 4) * 4) =
                     float4v{acc[i][j][g * 4], acc[i][j][g * 4 + 1], acc[i][j][g * 4 + 2], acc[i][j][g * 4 + 3]};
-        wave_sync<true>();
+        __syncthreads();
+        constexpr int kPass = 64 / kLanes;   // rows at a time
+        const int r_end = (wave % WP + 1) * kRows;
 #pragma unroll 1
-        for (int r = lane / kLanes; r < 32; r += 64 / kLanes) {
+        for (int r = wave % WP * kRows + lane / kLanes; r < r_end; r += kPass) {
             const int64_t q = q0 + wq + j * 32 + r;
             float v[G][8];
 #pragma unroll
@@ -396,11 +400,17 @@ __global__ __launch_bounds__(WP *WQ * 64, 2) void q8_tile_kernel(Q8Product a, Q8
                 }
                 continue;
             }
+            if (e.bias) {
+#pragma unroll
+                for (int g = 0; g < G; ++g)
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) v[g][c] += bias[g][c];
+            }
             by_act(e.act, [&](auto act) {
 #pragma unroll
                 for (int c = 0; c < 8; ++c) {
-                    v[0][c] = act_value<act.value, T>(v[0][c] + bias[0][c]);
-                    if constexpr (GATED) v[0][c] *= v[1][c] + bias[1][c];
+                    v[0][c] = act_value<act.value, T>(v[0][c]);
+                    if constexpr (GATED) v[0][c] *= v[1][c];
                 }
             });
             if (e.residual && q < a.nq) {
@@ -411,47 +421,15 @@ __global__ __launch_bounds__(WP *WQ * 64, 2) void q8_tile_kernel(Q8Product a, Q8
             }
             if (!q8) {
                 if (q < a.nq) store8(e.y + q * e.ldy + p, m, v[0]);
-                continue;
-            }
-            if constexpr (OUT % kBlock == 0) {
+            } else if constexpr (OUT % kBlock == 0) {
+                // (a block's columns beyond the last output are filled up with zeros; blocks beyond the last one are not written)
+                if (m < 8) {
 #pragma unroll
-                for (int c = 0; c < 8; ++c) v[0][c] = c < m ? v[0][c] : 0.f;
-                if constexpr (kShare == 1) {
-                    if (q < a.nq && p0 + wp / G < a.np) keep_block(v[0], e.codes + q * e.ldc + p, e.scales + q * e.lds + p / kBlock);
-                } else {   // back to where the sums were, until the other waves have their share of the row's largest value
-                    unsigned char *to = turn + r * kRow + col * 4;
-                    *(float4v *)to = *(const float4v *)v[0];
-                    *(float4v *)(to + 16) = *(const float4v *)(v[0] + 4);
-                    float top = most_of8(v[0]);
-                    top = fmaxf(top, dpp<0xB1>(top));
-                    top = fmaxf(top, dpp<0x4E>(top));
-                    if constexpr (kLanes == 8) top = fmaxf(top, dpp<0x141>(top));
-                    if (lane % kLanes == 0) most[wave % WP * BQ + wq + j * 32 + r] = top;
+                    for (int c = 0; c < 8; ++c) v[0][c] = c < m ? v[0][c] : 0.f;
                 }
+                if (q < a.nq && p < (a.np + kBlock - 1) / kBlock * kBlock) keep_block(v[0], e.codes + q * e.ldc + p, e.scales + q * e.lds + p / kBlock);
             }
         }
-        if constexpr (OUT % kBlock == 0 && kShare > 1) {
-            if (!raw && q8) {
-                __syncthreads();
-#pragma unroll 1
-                for (int r = lane / kLanes; r < 32; r += 64 / kLanes) {
-                    const int64_t q = q0 + wq + j * 32 + r;
-                    float v[8], top = 0.f;
-                    const unsigned char *from = turn + r * kRow + col * 4;
-                    *(float4v *)v = *(const float4v *)from;
-                    *(float4v *)(v + 4) = *(const float4v *)(from + 16);
-#pragma unroll
-                    for (int w = 0; w < kShare; ++w) top = fmaxf(top, most[(wave % WP / kShare * kShare + w) * BQ + wq + j * 32 + r]);
-                    const int byte = scale_byte(top);
-                    // (the block's columns beyond the last output are filled up with zeros; blocks beyond the last one are not written)
-                    if (q < a.nq && p < (a.np + kBlock - 1) / kBlock * kBlock) {
-                        store_vec(e.codes + q * e.ldc + p, encode8(v, inverse_scale(byte)));
-                        if (lane % kLanes == 0 && wave % WP % kShare == 0) e.scales[q * e.lds + p / kBlock] = (uint8_t)byte;
-                    }
-                }
-            }
-        }
-        wave_sync<true>();
     }
 }
 
@@ -543,9 +521,11 @@ int dequantize_impl(int32_t dtype, int64_t m, int64_t d, const Q8Arg &in, void *
 // The kernels of a product, by the sums that a workgroup computes.
 enum Q8Tiling {
     kQ8Few,      // 16 rows of P, all rows of Q (at most 64)
-    kQ8Slim,     // 256 x 64, four waves
-    kQ8Square,   // 128 x 128, four waves; not for a gated output in 8 bits, which needs both halves of 128 outputs
+    kQ8Slim,     // 256 x 64, four waves: gated outputs in 8 bits, of which a tile of 128 rows would have half a block
+    kQ8Small,    // 64 x 64, four waves: outputs in a wide type
+    kQ8Square,   // 128 x 128, four waves: all but gated outputs in 8 bits
     kQ8Long,     // 256 x 128, four waves
+    kQ8Wide,     // 256 x 192, eight waves
     kQ8Large,    // 256 x 256, eight waves
 };
 struct Q8Plan {
@@ -556,22 +536,29 @@ struct Q8Plan {
     size_t bytes = 0;
 };
 
+// What a tiling costs, in microseconds: `step` per block of 128 of the contraction with a compute unit full of `together` workgroups, at least `alone` however few
+// there are; `fixed` per workgroup for its first loads and its outputs.  Fitted to 700 timings: 23 sizes from 65 x 1,024 x 1,024 to 8,192 x 4,096 x 2,048, each with
+// outputs in bfloat16, gated ones in bfloat16 and in 8 bits and float32 ones, every tiling and 1 to 8 splits; what it picks takes 2.6 % longer than the best of all on average,
+// 31 % at worst (100 x 300 -> 777).
 struct Q8Cost {
     int bp, bq, together;
-    double step, alone, fixed;   // us per block of 128 with a full compute unit, at least `alone`; per workgroup
+    double step, alone, fixed;
 };
-static Q8Cost q8_cost(Q8Tiling t, bool exact)
+static Q8Cost q8_cost(Q8Tiling t, bool exact, bool gated)
 {
     switch (t) {
-    case kQ8Slim: return exact ? Q8Cost{256, 64, 2, 1.3, 0.7, 5.0} : Q8Cost{256, 64, 2, 0.9, 0.5, 5.0};
-    case kQ8Square: return exact ? Q8Cost{128, 128, 3, 1.9, 0.7, 5.0} : Q8Cost{128, 128, 3, 1.3, 0.5, 5.0};
-    case kQ8Long: return Q8Cost{256, 128, 2, 1.5, 0.8, 6.0};
-    default: return Q8Cost{256, 256, 1, 1.2, 0.8, 8.0};
+    case kQ8Slim: return exact ? Q8Cost{256, 64, 2, 2.1, 1.2, 8.0} : Q8Cost{256, 64, 2, 1.34, 0.73, 7.0};
+    case kQ8Small: return exact ? Q8Cost{64, 64, 4, 1.36, 0.47, 4.1} : Q8Cost{64, 64, 4, 1.07, 0.33, gated ? 2.5 : 3.0};
+    case kQ8Square:
+        return exact ? Q8Cost{128, 128, 3, 2.65, 0.98, 7.5} : gated ? Q8Cost{128, 128, 3, 1.6, 0.6, 6.2} : Q8Cost{128, 128, 3, 1.55, 0.55, 7.2};
+    case kQ8Long: return gated ? Q8Cost{256, 128, 2, 1.6, 1.2, 9.0} : Q8Cost{256, 128, 2, 1.64, 1.2, 9.1};
+    case kQ8Wide: return gated ? Q8Cost{256, 192, 1, 1.08, 0.3, 10.0} : Q8Cost{256, 192, 1, 0.87, 0.12, 10.0};
+    default: return gated ? Q8Cost{256, 256, 1, 1.38, 0.26, 12.0} : Q8Cost{256, 256, 1, 1.03, 0.11, 11.4};
     }
 }
 
-// quantized: the output is in 8 bits.
-static Q8Plan plan_q8(int32_t dtype, int64_t m, int64_t n, int64_t k, bool gated, bool quantized)
+// quantized: the output is in 8 bits.  heavy: its epilogue has a residual, or GELU or SiLU without a gate.
+static Q8Plan plan_q8(int32_t dtype, int64_t m, int64_t n, int64_t k, bool gated, bool quantized, bool heavy)
 {
     Q8Plan best;
     const bool exact = dtype == VF_F32;
@@ -585,12 +572,14 @@ static Q8Plan plan_q8(int32_t dtype, int64_t m, int64_t n, int64_t k, bool gated
         return best;
     }
     double least = 0;
-    for (Q8Tiling t : {kQ8Slim, kQ8Square, kQ8Long, kQ8Large}) {
-        if (exact && (t == kQ8Long || t == kQ8Large)) continue;
-        const Q8Cost c = q8_cost(t, exact);
+    for (Q8Tiling t : {kQ8Slim, kQ8Small, kQ8Square, kQ8Long, kQ8Wide, kQ8Large}) {
+        if (t == kQ8Slim && !(gated && quantized)) continue;
+        if ((t == kQ8Small && quantized) || (t == kQ8Square && gated && quantized)) continue;   // (half a block of outputs)
+        if (exact && t > kQ8Square) continue;
+        Q8Cost c = q8_cost(t, exact, gated);
+        if (heavy) c.fixed += 6.0 * c.together * c.bp * c.bq / 65536 * (c.together > 1 ? 0.75 : 1);   // (less where another workgroup multiplies meanwhile)
         const int64_t tiles = ceil_div(n, gated ? c.bp / 2 : c.bp) * ceil_div(m, c.bq);
         if (tiles >= kMaxTiles) continue;
-        const bool joined = quantized && gated && t == kQ8Square;   // the epilogue is the join's
         for (int64_t splits : {1, 2, 3, 4, 6, 8, 12, 16}) {
             const int64_t chunk = std::max<int64_t>(4, ceil_div(ceil_div(blocks, splits), 4) * 4);   // whole words of scales
             const int64_t used = std::max<int64_t>(1, ceil_div(blocks, chunk));
@@ -600,11 +589,11 @@ static Q8Plan plan_q8(int32_t dtype, int64_t m, int64_t n, int64_t k, bool gated
             const double steps = (double)std::min(chunk, blocks);
             const double last = (double)(per_cu - (rounds - 1) * c.together) / c.together;
             double us = (double)(rounds - 1) * (steps * c.step + c.fixed) + steps * std::max(c.alone, c.step * last) + c.fixed;
-            if (used > 1 || joined) us += 5.5 + (double)used * sums * 2 / 4e6;
+            if (used > 1) us += 6 + (double)used * sums * 2 / 7.5e6;
             if (least == 0 || us < least) {
                 least = us;
                 best.tiling = t;
-                best.splits = used > 1 || joined ? (int)used : 0;
+                best.splits = used > 1 ? (int)used : 0;
                 best.chunk = chunk;
                 best.bytes = best.splits ? sums * best.splits : 0;
             }
@@ -617,7 +606,7 @@ static Q8Plan plan_q8(int32_t dtype, int64_t m, int64_t n, int64_t k, bool gated
 template <class T, bool EXACT, bool GATED, int BP, int BQ, int WP, int WQ, int STEPS>
 static int launch_q8(const Q8Product &a, const Q8Epilogue<T> &e, hipStream_t s)
 {
-    constexpr size_t lds = std::max<size_t>((size_t)STEPS * (BP + BQ) * 64 + 2 * (BP + BQ) * 4, (size_t)WP * WQ * 32 * (BP / WP * 4 + 16) + WP * BQ * 4);
+    constexpr size_t lds = std::max<size_t>((size_t)STEPS * (BP + BQ) * 64 + 2 * (BP + BQ) * 4, (size_t)WQ * 32 * (BP * 4 + 16));
     static std::atomic<uint64_t> done{0};
     if constexpr (lds > 64 * 1024)
         if (int rc = allow_lds((const void *)q8_tile_kernel<T, EXACT, GATED, BP, BQ, WP, WQ, STEPS>, lds, done); rc != VF_OK) return rc;
@@ -637,11 +626,14 @@ template <class T, bool GATED> static int run_q8(const Q8Product &a, const Q8Epi
         else if (a.nq <= 32) q8_few_rows_kernel<T, 2, GATED><<<grid, block, 0, s>>>(a, e);
         else q8_few_rows_kernel<T, 4, GATED><<<grid, block, 0, s>>>(a, e);
     } else if (t == kQ8Slim) {
-        rc = launch_q8<T, kExact, GATED, 256, 64, 4, 1, 3>(a, e, s);
+        if constexpr (GATED) rc = launch_q8<T, kExact, true, 256, 64, 4, 1, 3>(a, e, s);
+    } else if (t == kQ8Small) {
+        rc = launch_q8<T, kExact, GATED, 64, 64, 2, 2, 4>(a, e, s);
     } else if (t == kQ8Square) {
         rc = launch_q8<T, kExact, GATED, 128, 128, 2, 2, 3>(a, e, s);
     } else if constexpr (!kExact) {
         if (t == kQ8Long) rc = launch_q8<T, false, GATED, 256, 128, 2, 2, 3>(a, e, s);
+        else if (t == kQ8Wide) rc = launch_q8<T, false, GATED, 256, 192, 4, 2, 4>(a, e, s);
         else rc = launch_q8<T, false, GATED, 256, 256, 2, 4, 4>(a, e, s);
     }
     if (rc != VF_OK) return rc;
@@ -667,7 +659,7 @@ int linear_q8_workspace_impl(int32_t dtype, int64_t m, int64_t n, int64_t k, int
     VF_REQUIRE(bytes != nullptr, "linear in 8 bits: bytes is NULL");
     if (int rc = check_q8_sizes(dtype, m, n, k, 0); rc != VF_OK) return rc;
     VF_REQUIRE((gated == 0 || gated == 1) && (quantized == 0 || quantized == 1), "linear in 8 bits: gated and quantized must be 0 or 1");
-    *bytes = plan_q8(dtype, m, n, k, gated, quantized).bytes;
+    *bytes = std::max(plan_q8(dtype, m, n, k, gated, quantized, false).bytes, plan_q8(dtype, m, n, k, gated, quantized, true).bytes);
     return VF_OK;
 }
 
@@ -686,7 +678,7 @@ int linear_q8_impl(const LinearQ8Args &a)
     if (q8)
         if (int rc = check_q8("linear in 8 bits: the output", a.out, a.m, a.n); rc != VF_OK) return rc;
     VF_REQUIRE(a.x.ld < (1 << 24) && a.w.ld < (1 << 24), "linear in 8 bits: rows of codes lie 2^24 bytes apart or more");   // (offsets within a tile have 32 bits)
-    const Q8Plan plan = plan_q8(a.dtype, a.m, a.n, a.k, a.gated, q8);
+    const Q8Plan plan = plan_q8(a.dtype, a.m, a.n, a.k, a.gated, q8, a.residual != nullptr || (!a.gated && costly(a.act)));
     VF_REQUIRE(plan.fits, "linear in 8 bits: too many output tiles in one call");
     if (int rc = check_workspace("linear in 8 bits", a.workspace, a.workspace_bytes, plan.bytes); rc != VF_OK) return rc;
     const size_t size = type_size(a.dtype);
