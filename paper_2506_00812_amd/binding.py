@@ -30,7 +30,7 @@ EXPORTED_SYMBOLS = ("vf_build_index", "vf_search", "vf_search_exact", "vf_index_
                     "vf_layer_norm_workspace", "vf_log_probs", "vf_log_probs_backward", "vf_log_probs_workspace",
                     "vf_adamw_step", "vf_adamw_moments",
                     "vf_gated_linear", "vf_gated_linear_backward", "vf_gated_linear_workspace", "vf_quantize", "vf_dequantize", "vf_linear_quantized",
-                    "vf_linear_quantized_workspace", "vf_rms_norm", "vf_rms_norm_backward", "vf_rms_norm_workspace", "vf_distill", "vf_distill_backward",
+                    "vf_linear_quantized_workspace", "vf_debug_linear_quantized", "vf_rms_norm", "vf_rms_norm_backward", "vf_rms_norm_workspace", "vf_distill", "vf_distill_backward",
                     "vf_distill_workspace")
 
 ALLOC_FN = C.CFUNCTYPE(C.c_void_p, C.c_size_t, C.c_void_p)
@@ -155,6 +155,7 @@ def load_library():
                 vf_dequantize=[i32, i64, i64, p, i64, p, i64, p, i64, p],
                 vf_linear_quantized=[i32, i64, i64, i64, p, i64, p, i64, p, i64, p, i64, p, i32, i32, p, i64, p, i64, p, i64, p, i64, p, sz, p],
                 vf_linear_quantized_workspace=[i32, i64, i64, i64, i32, i32, C.POINTER(sz)],
+                vf_debug_linear_quantized=[i32, i64, i64, i64, i32, i32, i32, C.POINTER(i32), C.POINTER(i32)],
                 vf_rms_norm=[i32, i64, i64, p, i64, p, i64, p, C.c_double, p, i64, p, i64, p, i64, p, i64, p, p],
                 vf_rms_norm_backward=[i32, i64, i64, p, i64, p, i64, p, p, p, i64, p, i64, p, p, sz, p],
                 vf_rms_norm_workspace=[i32, i64, i64, C.POINTER(sz)],
@@ -1018,6 +1019,13 @@ def linear_q8(x, weight, bias=None, residual=None, activation="none", gated=Fals
     _check(L.vf_linear_quantized(code, m, n, k, *px, *pw8, pb, act, int(gated), None if residual is None else residual.data_ptr(), ldr, py, ldy, *po, pw, nw,
                           handle))
     return y
+
+
+def debug_linear_q8(dtype, m, n, k, gated=False, quantize=False, heavy=False):
+    """(tiling, splits) of a product in 8 bits (vf_debug_linear_quantized); dtype: VF_F32, VF_BF16 or VF_F16."""
+    tiling, splits = C.c_int32(), C.c_int32()
+    _check(load_library().vf_debug_linear_quantized(dtype, m, n, k, int(gated), int(quantize), int(heavy), C.byref(tiling), C.byref(splits)))
+    return tiling.value, splits.value
 
 
 def rms_norm(x, weight=None, residual=None, eps=1e-6, save=False, quantize=False, out=None, out_total=None, stream=None):

@@ -408,6 +408,12 @@ extern "C" int vf_linear_quantized_workspace(int32_t dtype, int64_t m, int64_t n
     return guarded([&] { return linear_q8_workspace_impl(dtype, m, n, k, gated, quantized, bytes); });
 }
 
+extern "C" int vf_debug_linear_quantized(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t gated, int32_t quantized, int32_t heavy,
+                                         int32_t *tiling, int32_t *splits)
+{
+    return guarded([&] { return debug_linear_q8_impl(dtype, m, n, k, gated, quantized, heavy, tiling, splits); });
+}
+
 extern "C" int vf_rms_norm(int32_t dtype, int64_t m, int64_t d, const void *x, int64_t ldx, const void *residual, int64_t ldr,
                            const void *weight, double eps, void *y, int64_t ldy, uint8_t *y_codes, int64_t ldyc, uint8_t *y_scales,
                            int64_t ldys, void *total, int64_t ldt, float *rstd, void *hip_stream)

@@ -374,6 +374,7 @@ struct LinearQ8Args {
 };
 int linear_q8_impl(const LinearQ8Args &a);
 int linear_q8_workspace_impl(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t gated, int32_t quantized, size_t *bytes);
+int debug_linear_q8_impl(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t gated, int32_t quantized, int32_t heavy, int32_t *tiling, int32_t *splits);
 int quantize_impl(int32_t dtype, int64_t m, int64_t d, const void *x, int64_t ldx, const Q8Arg &out, hipStream_t s);
 int dequantize_impl(int32_t dtype, int64_t m, int64_t d, const Q8Arg &in, void *y, int64_t ldy, hipStream_t s);
 

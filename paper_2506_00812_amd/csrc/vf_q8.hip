@@ -649,7 +649,7 @@ template <class T, bool GATED> static int run_q8(const Q8Product &a, const Q8Epi
 static int check_q8_sizes(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t act)
 {
     VF_REQUIRE(is_float_type(dtype), "linear in 8 bits: dtype must be VF_F32, VF_BF16 or VF_F16");
-    VF_REQUIRE(m >= 0 && m <= kMaxExtent && n >= 0 && n <= (1 << 24) && k >= 0 && k <= (1 << 25), "linear in 8 bits: m, n or k out of range");
+    VF_REQUIRE(m >= 0 && m <= kMaxExtent && n >= 0 && n <= (1 << 24) && k >= 0 && k < (1 << 24), "linear in 8 bits: m, n or k out of range");
     VF_REQUIRE(act >= VF_ACT_NONE && act <= VF_ACT_SILU, "linear in 8 bits: unknown activation");
     return VF_OK;
 }
@@ -660,6 +660,17 @@ int linear_q8_workspace_impl(int32_t dtype, int64_t m, int64_t n, int64_t k, int
     if (int rc = check_q8_sizes(dtype, m, n, k, 0); rc != VF_OK) return rc;
     VF_REQUIRE((gated == 0 || gated == 1) && (quantized == 0 || quantized == 1), "linear in 8 bits: gated and quantized must be 0 or 1");
     *bytes = std::max(plan_q8(dtype, m, n, k, gated, quantized, false).bytes, plan_q8(dtype, m, n, k, gated, quantized, true).bytes);
+    return VF_OK;
+}
+
+int debug_linear_q8_impl(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t gated, int32_t quantized, int32_t heavy, int32_t *tiling, int32_t *splits)
+{
+    if (int rc = check_q8_sizes(dtype, m, n, k, 0); rc != VF_OK) return rc;
+    VF_REQUIRE(tiling && splits, "linear in 8 bits: tiling or splits is NULL");
+    const Q8Plan p = plan_q8(dtype, m, n, k, gated != 0, quantized != 0, heavy != 0);
+    VF_REQUIRE(p.fits, "linear in 8 bits: too many output tiles in one call");
+    *tiling = p.tiling;
+    *splits = p.splits;
     return VF_OK;
 }
 
