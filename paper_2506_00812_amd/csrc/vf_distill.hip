@@ -263,8 +263,8 @@ __global__ __launch_bounds__(256) void distill_backward_kernel(int64_t m, int64_
 #pragma unroll
                     for (int i = 0; i < R; ++i)
 #pragma unroll 1
-                        for (int j = 0; j < 64; ++j) {
-                            if (lane == j && at[i] >= 0) place[at[i]] += e.q[i];
+                        for (uint64_t left = __ballot(at[i] >= 0); left != 0; left &= left - 1) {
+                            if (lane == __ffsll((unsigned long long)left) - 1) place[at[i]] += e.q[i];
                             wave_sync<true>();
                         }
                 } else {
