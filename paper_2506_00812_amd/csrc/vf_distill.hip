@@ -116,7 +116,8 @@ template <class T, int R> __device__ __forceinline__ void load_entries(const Dis
 }
 
 // Segment `item % nseg` of a row: TPR threads take its vectors in turn, 16 elements a thread at a time.  nseg > 1: the segment's sums go to
-// part [row][nseg].
+// part [row][nseg].  Sixteen elements have one maximum and at most one change of origin, so that an element costs one exponential.  64 x 200,000 in bfloat16,
+// 13 segments a row: 26 MB in 8.0 us and 2.6 for the join; 10,000 x 10,000: 44 us (4.5 TB/s).  (Asking for the next vectors ahead gained nothing.)
 template <class T, int TPR, int R>
 __global__ __launch_bounds__(256) void distill_kernel(int64_t m, DistillRow<T> a, int nseg, int64_t seg, float2 *__restrict__ part)
 {
@@ -205,7 +206,8 @@ template <class T, int R> __global__ __launch_bounds__(64) void distill_join_ker
 
 // A wave has a segment of a row, 512 columns at a time, and all of the row's entries.  Those that fall into its columns leave their q in LDS at their place,
 // where the lanes that have these columns find it.  Two entries of the same label would overwrite each other: what is seen by writing
-// their numbers there first, and then they are added one after the other.
+// their numbers there first, and then they are added one after the other.  Bound by memory: 10,000 x 10,000 in bfloat16 with 32 entries a row 82 us (4.9 TB/s),
+// 2,000 x 10,000 with 200 19 us, 22 with random labels, some of them twice.
 template <class T, int R>
 __global__ __launch_bounds__(256) void distill_backward_kernel(int64_t m, int64_t v, const T *logits, int64_t ld, const float *__restrict__ lse,
                                                                const int32_t *__restrict__ ids, const float *__restrict__ teacher, int top,

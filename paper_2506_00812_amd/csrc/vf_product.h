@@ -139,7 +139,7 @@ constexpr int kRowBytes = 128;     // bytes of the contraction per step of the t
 // nothing waits for another wave until the end.  A workgroup has 16 rows of P; its waves share the contraction in whole fragments, loaded
 // from memory straight into the matrix instruction's layout, several in flight, and add up through LDS.
 // One row, 4096 x 1024 in bfloat16 (8 MB of weights): 4.4 us; 64 x 64 tiles over a split contraction and their join took 13.
-// Gated: sixteen rows of each half, 8 waves at most.
+// Gated: sixteen rows of each half, 8 waves at most; one row, 2 x 4,096 x 1,024 (17 MB) 6.0 us.
 template <class T, int FQ, bool GATED = false>
 __global__ __launch_bounds__(GATED ? 512 : 1024) void few_rows_kernel(Product<T> a, Epilogue<T> e)
 {
@@ -497,10 +497,11 @@ template <class T, bool ALONG_C, int ROWS> __device__ __forceinline__ Vec<T> dir
 }
 
 // BP x BQ outputs per workgroup of WP x WQ waves.  Bound by the matrix cores' clock under load and by how evenly the tiles fill 256
-// compute units.  bfloat16, bare products one after the other: 8,192 x 4,096 x 2,048 forward 114 us, dx 103, dw 134 with its join (the library 96, 104
-// and 131); 10,000 x 4,096 x 1,024 forward 95 us, dx 76, dw 84 with its join (880 - 1,100 TFLOP/s; the library 87 - 95, 82 and 114).  In such
-// a product with GELU and z the matrix cores are busy for a third of the cycles, in its dx and dw for half.  Rows 8,192 apart, along c on
-// both sides, are slow: 8,192^3 forward 1,225 us, dx 809 (the library 673 and 787).  A smaller tile reads more of its operands per product from L2: 128 x 128 takes 15 - 30 % longer where the tiles are many.
+// compute units.  bfloat16, bare products one after the other: 8,192 x 4,096 x 2,048 forward 115 us, dx 103, dw 130 with its join (the library 96, 105
+// and 131); 10,000 x 4,096 x 1,024 forward 95 us, dx 76, dw 85 with its join (880 - 1,100 TFLOP/s; the library 87 - 96, 83 and 116).  In such
+// a product with GELU and z the matrix cores are busy for a third of the cycles, in its dx and dw for half.  8,192^3 with rows 8,192 apart on both sides: forward
+// 831 us, dx 782 (the library 719 and 787); before the order of place_tile 1,225 and 809.  Gated, 10,000 x (2 x 4,096) x 1,024: 164 us, with z kept 174 (the library's
+// bare product of all 8,192 rows 161).  A smaller tile reads more of its operands per product from L2: 128 x 128 takes 15 - 30 % longer where the tiles are many.
 template <class T, bool PC, bool QC, int BP, int BQ, int WP, int WQ, int STEPS, bool GATED = false>
 __global__ __launch_bounds__(WP *WQ * 64, 2) void direct_kernel(Product<T> a, Epilogue<T> e)
 {

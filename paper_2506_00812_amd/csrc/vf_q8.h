@@ -19,7 +19,7 @@ __device__ __forceinline__ int scale_byte(float most)
 __device__ __forceinline__ float inverse_scale(int byte) { return __uint_as_float((uint32_t)(254 - byte) << 23); }   // byte <= 247: a normal number
 __device__ __forceinline__ float scale_value(int byte)
 {
-    return __uint_as_float(byte > 0 ? (uint32_t)byte << 23 : 0x400000u);   // 2^-127 is below the normal range
+    return __uint_as_float((uint32_t)byte << 23 | (((byte + 1) & 254) ? 0u : 0x400000u));   // 2^-127 is below the normal range, byte 255 NaN
 }
 
 // Eight values divided by their scale (exact: a power of two), to the nearest code, ties to even; what is not finite becomes NaN.
