@@ -541,8 +541,8 @@ struct Q8Plan {
 };
 
 // What a tiling costs, in microseconds: `step` per block of 128 of the contraction with a compute unit full of `together` workgroups, at least `alone` however few
-// there are; `fixed` per workgroup for its first loads and its outputs.  Fitted to 700 timings: 23 sizes from 65 x 1,024 x 1,024 to 8,192 x 4,096 x 2,048, each with
-// outputs in bfloat16, gated ones in bfloat16 and in 8 bits and float32 ones, every tiling and 1 to 8 splits; what it picks takes 2.6 % longer than the best of all on average,
+// there are; `fixed` per workgroup for its first loads and its outputs.  Fitted to 1,020 timings: 23 sizes from 65 x 1,024 x 1,024 to 8,192 x 4,096 x 2,048, each with
+// outputs in bfloat16, bare and with GELU and a residual, gated ones in bfloat16 and in 8 bits and float32 ones, every tiling and 1 to 8 splits; what it picks takes 2.6 % longer than the best of all on average,
 // 31 % at worst (100 x 300 -> 777).
 struct Q8Cost {
     int bp, bq, together;
