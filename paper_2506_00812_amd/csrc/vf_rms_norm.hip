@@ -18,6 +18,14 @@ template <class T> struct RmsOut {
     int64_t ldc, lds;
 };
 
+// What a row's last block is filled up with, also where rstd is not finite.
+__device__ __forceinline__ void zeros_behind(float (&v)[8], int n)
+{
+    if (n >= 8) return;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j < n ? v[j] : 0.f;
+}
+
 // Rows of up to TPR * NV eights: thread t of a row holds eights t, t + TPR, ...  A wave has a row of up to 1,024 by itself, four rows a workgroup and nothing to
 // wait for.  10,000 x 1,024 in bfloat16 with a residual, into 8 bits: 72 MB in 15 us (4.8 TB/s); one such row 3.1 us.
 template <class T, int TPR, int NV, bool Q8>
@@ -74,6 +82,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rms_forward_kernel(int6
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[i][j] = v[i][j] * rstd * w[j];
+            if constexpr (Q8) zeros_behind(v[i], d - c);
             if constexpr (Q8) keep_block(v[i], o.codes + row * o.ldc + c, o.scales + row * o.lds + c / kBlock);
             else store8(o.y + row * o.ldy + c, d - c, v[i]);
         }
@@ -114,6 +123,7 @@ __global__ __launch_bounds__(1024) void rms_forward_long_kernel(int64_t m, int64
             if (weight) load8(weight + c, n, w);
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = v[j] * rstd * (weight ? w[j] : 1.f);
+            if constexpr (Q8) zeros_behind(v, n);
             if constexpr (Q8) keep_block(v, o.codes + row * o.ldc + c, o.scales + row * o.lds + c / kBlock);
             else store8(o.y + row * o.ldy + c, n, v);
         }
