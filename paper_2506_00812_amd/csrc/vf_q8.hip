@@ -105,9 +105,9 @@ __device__ __forceinline__ float16v mma32(const int8v &p, int sp, const int8v &q
 
 // ---------------------------------------------------------------- few rows
 
-// At most 16 FQ rows of Q: one read of P, sixteen rows of it (of each half) a workgroup, whose waves share the contraction block by block, loaded from memory straight
+// Few rows, at most 16 FQ, of Q: one read of P, sixteen rows of it (of each half) a workgroup, whose waves share the contraction block by block, loaded from memory straight
 // into the matrix instruction's layout, and add up through LDS.  Bound by memory and latency; the codes are multiplied as bfloat16, which costs nothing
-// here and keeps every digit.  One row, 4,096 x 1,024 (4.3 MB): 4.0 us.
+// here and keeps every digit.  One row, 4,096 x 1,024 (4.3 MB): 4.0 us.  Each block of 128 costs a wave's loads in full, 1.5 us and more.
 template <class T, int FQ, bool GATED>
 __global__ __launch_bounds__(GATED ? 512 : 1024) void q8_few_rows_kernel(Q8Product a, Q8Epilogue<T> e)
 {
@@ -561,6 +561,22 @@ static Q8Cost q8_cost(Q8Tiling t, bool exact, bool gated)
     }
 }
 
+constexpr double kJoinCost = 6;   // of one more launch: small products come one after the other as fast as the host can launch them
+
+static int few_waves(int64_t blocks, bool gated) { return (int)std::max<int64_t>(1, std::min<int64_t>(gated ? 8 : 16, blocks)); }
+
+// What the few rows' kernel takes, in microseconds: the longer of a wave's way through its blocks, one after the other, and of all workgroups' loads, Q's in each of
+// them.  Fitted to timings of 1,200 products of 1 to 64 rows, 64 to 200,000 outputs and 100 to 16,384 of the contraction.  A few blocks and some thousand outputs go to it
+// (4,096 x 1,024: 3.6 us for one row, 4.6 for 32, in tiles of 64 x 64 5.8 and 6.1); long contractions and many outputs go to tiles, which read Q once for
+// 64 outputs (16 rows, 200,000 x 1,024: 35 us, here 51; 64 rows, 16,384 x 4,096: 18, here 61; 64 x 16,384: 12, here 55).
+static double few_cost(int64_t m, int64_t n, int64_t blocks, bool gated)
+{
+    const int waves = few_waves(blocks, gated);
+    const double groups = (double)ceil_div(n, 16), loads = (gated ? 8.8 : 4.4) + 0.1 * m;
+    const double chain = (double)ceil_div(blocks, waves) * (1.5 + 0.005 * m * waves);
+    return 1.6 + std::max(chain, groups * 1e-4 * (blocks * loads + (m <= 16 ? 2 : m <= 32 ? 13 : 40)));
+}
+
 // quantized: the output is in 8 bits.  heavy: its epilogue has a residual, or GELU or SiLU without a gate.
 static Q8Plan plan_q8(int32_t dtype, int64_t m, int64_t n, int64_t k, bool gated, bool quantized, bool heavy)
 {
@@ -568,14 +584,13 @@ static Q8Plan plan_q8(int32_t dtype, int64_t m, int64_t n, int64_t k, bool gated
     const bool exact = dtype == VF_F32;
     const int64_t blocks = ceil_div(k, kBlock), rows = gated ? 2 * n : n;
     const size_t sums = (size_t)m * rows * 4;
-    if (m <= 64) {
+    double least = 0;
+    if (m <= 64 && ceil_div(n, 16) < kMaxTiles) {
+        least = few_cost(m, n, blocks, gated) + (quantized ? kJoinCost + sums * 2 / 7.5e6 : 0);
         best.splits = quantized ? 1 : 0;
         best.chunk = blocks;
         best.bytes = quantized ? sums : 0;
-        best.fits = ceil_div(n, 16) < kMaxTiles;
-        return best;
     }
-    double least = 0;
     for (Q8Tiling t : {kQ8Slim, kQ8Small, kQ8Square, kQ8Long, kQ8Wide, kQ8Large}) {
         if (t == kQ8Slim && !(gated && quantized)) continue;
         if ((t == kQ8Small && quantized) || (t == kQ8Square && gated && quantized)) continue;   // (half a block of outputs)
@@ -593,7 +608,8 @@ static Q8Plan plan_q8(int32_t dtype, int64_t m, int64_t n, int64_t k, bool gated
             const double steps = (double)std::min(chunk, blocks);
             const double last = (double)(per_cu - (rounds - 1) * c.together) / c.together;
             double us = (double)(rounds - 1) * (steps * c.step + c.fixed) + steps * std::max(c.alone, c.step * last) + c.fixed;
-            if (used > 1) us += 6 + (double)used * sums * 2 / 7.5e6;
+            us = std::max(us, 4.0);   // (nothing was quicker)
+            if (used > 1) us += kJoinCost + (double)used * sums * 2 / 7.5e6;
             if (least == 0 || us < least) {
                 least = us;
                 best.tiling = t;
@@ -624,8 +640,7 @@ template <class T, bool GATED> static int run_q8(const Q8Product &a, const Q8Epi
     constexpr bool kExact = std::is_same_v<T, float>;
     int rc = VF_OK;
     if (t == kQ8Few) {
-        const int waves = (int)std::max<int64_t>(1, std::min<int64_t>(GATED ? 8 : 16, a.blocks));
-        const dim3 grid((unsigned)ceil_div(a.np, 16)), block(waves * 64);
+        const dim3 grid((unsigned)ceil_div(a.np, 16)), block(few_waves(a.blocks, GATED) * 64);
         if (a.nq <= 16) q8_few_rows_kernel<T, 1, GATED><<<grid, block, 0, s>>>(a, e);
         else if (a.nq <= 32) q8_few_rows_kernel<T, 2, GATED><<<grid, block, 0, s>>>(a, e);
         else q8_few_rows_kernel<T, 4, GATED><<<grid, block, 0, s>>>(a, e);
