@@ -92,7 +92,7 @@ int gated_linear_workspace_impl(int32_t dtype, int64_t m, int64_t n, int64_t k, 
     VF_REQUIRE(bytes != nullptr, "gated linear: bytes is NULL");
     if (int rc = check_gated(dtype, m, n, k, act); rc != VF_OK) return rc;
     if (!backward) {
-        *bytes = most_bytes(dtype, 2 * n, m, k, true, true, costly(act));
+        *bytes = most_bytes(dtype, 2 * n, m, k, true, true, costly(act), true);
         return VF_OK;
     }
     GatedBackward b;
@@ -109,7 +109,7 @@ int gated_linear_impl(const LinearArgs &a)
     VF_REQUIRE(a.y != nullptr, "gated linear: y is NULL");
     VF_REQUIRE(a.ldx >= a.k && a.ldw >= a.k, "gated linear: ldx or ldw is less than k");
     VF_REQUIRE(a.ldy >= a.n && (!a.z || a.ldz >= 2 * a.n), "gated linear: ldy is less than n or ldz less than 2 n");
-    const ProductPlan plan = plan_product(a.dtype, 2 * a.n, a.m, a.k, {true, true, costly(a.act), direct_rows(a.dtype, a.x, a.ldx) && direct_rows(a.dtype, a.w, a.ldw)});
+    const ProductPlan plan = plan_product(a.dtype, 2 * a.n, a.m, a.k, {true, true, costly(a.act), direct_rows(a.dtype, a.x, a.ldx) && direct_rows(a.dtype, a.w, a.ldw), true});
     VF_REQUIRE(plan.fits, kTooManyGatedTiles);
     if (int rc = check_workspace("gated linear", a.workspace, a.workspace_bytes, plan.bytes); rc != VF_OK) return rc;
     const size_t size = type_size(a.dtype);

@@ -720,6 +720,7 @@ struct Operands {
     bool p_along, q_along;   // contiguous along the contraction
     bool costly_act;         // an epilogue with GELU or SiLU
     bool direct;             // 2-byte types; rows start on 16 bytes, and an operand contiguous along its rows has whole vectors of them
+    bool gated = false;
 };
 
 constexpr int64_t kMaxTiles = 1 << 22;   // and more are not launched: a launch holds fewer than 2^32 threads
@@ -739,6 +740,8 @@ inline ProductPlan plan_product(int32_t dtype, int64_t np, int64_t nq, int64_t n
         best.tiling = kFewRows;
         best.chunk = nc;
         least = few_rows_us(np, nq, nc * (int64_t)type_size(dtype));
+        // what a workgroup costs by itself, which counts where the contraction is short (2 x 65,536 x 100 in bfloat16, 33 rows: 38 us, 14 in tiles of 64 x 64)
+        if (o.gated) least = std::max(least, 3 + (double)ceil_div(np, 16) * 1e-4 * (nq <= 16 ? 2 : nq <= 32 ? 13 : 40));
         // (the quickest that any tile could be: one split, or one step of many; a call of few rows should not wait for its plan)
         if (least <= std::min(3.4 + 0.4 * (double)ceil_div(nc, step), 9.3)) return best;
     }
@@ -852,10 +855,10 @@ inline bool direct_rows(int32_t dtype, const void *p, int64_t ld)
 }
 
 // Workspace of a product whose operands' alignment is not known yet.
-inline size_t most_bytes(int32_t dtype, int64_t np, int64_t nq, int64_t nc, bool p_along, bool q_along, bool costly)
+inline size_t most_bytes(int32_t dtype, int64_t np, int64_t nq, int64_t nc, bool p_along, bool q_along, bool costly, bool gated = false)
 {
-    return std::max(plan_product(dtype, np, nq, nc, {p_along, q_along, costly, false}).bytes,
-                    dtype == VF_F32 ? 0 : plan_product(dtype, np, nq, nc, {p_along, q_along, costly, true}).bytes);
+    return std::max(plan_product(dtype, np, nq, nc, {p_along, q_along, costly, false, gated}).bytes,
+                    dtype == VF_F32 ? 0 : plan_product(dtype, np, nq, nc, {p_along, q_along, costly, true, gated}).bytes);
 }
 
 }  // namespace vf
