@@ -134,7 +134,7 @@ __global__ __launch_bounds__(1024) void rms_forward_long_kernel(int64_t m, int64
 // the workgroup leaves one row of them in part [gridDim.x][d], or (part NULL: it is the only one) the sums themselves in dweight.
 // 100,000 x 1,024 in bfloat16 with d_s: 820 MB in 145 us (5.65 TB/s), the partial rows' join 5.
 template <class T, int TPR, int NV, bool PARTS>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rms_backward_kernel(int64_t m, int d, const T *dy, int64_t lddy, const T *__restrict__ s,
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR, 4) void rms_backward_kernel(int64_t m, int d, const T *dy, int64_t lddy, const T *__restrict__ s,
                                                                               int64_t lds_, const float *__restrict__ rstd, const T *__restrict__ weight,
                                                                               const T *d_total, int64_t ldt, T *dx, int64_t lddx, float *__restrict__ part,
                                                                               T *dweight)
@@ -291,14 +291,30 @@ constexpr int64_t kMaxRow = 1 << 24;   // elements of a row
 
 static int64_t eights_of(int64_t d) { return ceil_div(d, 8); }
 
-// Workgroups (and so partial rows) of the backward pass, as the layer norm has them.
+// Calls fn with the threads of a row and the eights of a thread; false: no kernel holds a row of so many.  Two eights a thread at most: four take so many registers
+// that two waves share a SIMD (50,000 x 2,048 in bfloat16 backward: 223 us so, 159 this way; 10,000 x 8,192: 192 and 133).
+template <class F> static bool by_eights(int64_t nv, F &&fn)
+{
+    if (nv <= 16) fn(std::integral_constant<int, 16>(), std::integral_constant<int, 1>());
+    else if (nv <= 32) fn(std::integral_constant<int, 16>(), std::integral_constant<int, 2>());
+    else if (nv <= 64) fn(std::integral_constant<int, 64>(), std::integral_constant<int, 1>());
+    else if (nv <= 128) fn(std::integral_constant<int, 64>(), std::integral_constant<int, 2>());
+    else if (nv <= 256) fn(std::integral_constant<int, 256>(), std::integral_constant<int, 1>());
+    else if (nv <= 512) fn(std::integral_constant<int, 256>(), std::integral_constant<int, 2>());
+    else if (nv <= 1024) fn(std::integral_constant<int, 512>(), std::integral_constant<int, 2>());
+    else if (nv <= 2048) fn(std::integral_constant<int, 1024>(), std::integral_constant<int, 2>());
+    else return false;
+    return true;
+}
+
+// Workgroups (and so partial rows) of the backward pass: as many as are in work at the same time, or fewer rows than that need.
 static int64_t parts_of(int64_t m, int64_t d)
 {
     const int64_t nv = eights_of(d);
-    if (m <= (nv <= 32 ? 32 : nv <= 256 ? 8 : 0)) return 1;   // two rows a wave, or two times four: less than one more launch
-    const int64_t most = std::max<int64_t>(512, std::min<int64_t>(1024, m / 16));
+    if (m <= (nv <= 32 ? 32 : nv <= 128 ? 8 : nv <= 256 ? 2 : 0)) return 1;   // two rows a wave, or two times four: less than one more launch
+    const int64_t most = nv > 512 ? 512 : std::max<int64_t>(512, std::min<int64_t>(1024, m / 16));
     if (nv <= 32) return std::min(ceil_div(m, 16), most);
-    if (nv <= 256) return std::min(ceil_div(m, 4), most);
+    if (nv <= 128) return std::min(ceil_div(m, 4), most);
     if (nv <= 2048) return std::min(m, most);
     return std::min<int64_t>(ceil_div(m, 4), 64);
 }
@@ -343,7 +359,7 @@ int rms_norm_impl(const RmsArgs &a)
         const RmsOut<T> o{(T *)a.y, a.ldy, (T *)a.total, a.ldt, a.rstd, a.codes, a.scales, a.ldc, a.lds};
         auto run = [&](auto in8) {
             constexpr bool Q8 = in8.value;
-            const bool short_row = by_row(eights_of(Q8 ? q8_width(a.d) : a.d), [&](auto tpr, auto nv) {
+            const bool short_row = by_eights(eights_of(Q8 ? q8_width(a.d) : a.d), [&](auto tpr, auto nv) {
                 constexpr int TPR = tpr.value, NV = nv.value;
                 const int64_t blocks = TPR < 256 ? ceil_div(a.m, 256 / TPR) : a.m;
                 rms_forward_kernel<T, TPR, NV, Q8><<<dim3(grid_of(blocks)), dim3(TPR < 256 ? 256 : TPR), 0, a.stream>>>(
@@ -396,7 +412,7 @@ int rms_norm_backward_impl(const RmsArgs &a)
             if (sums) launch_join_parts<T>(0, a.d, 1, part, (T *)a.dweight, nullptr, a.stream);
             return;
         }
-        const bool short_row = by_row(eights_of(a.d), [&](auto tpr, auto nv) {
+        const bool short_row = by_eights(eights_of(a.d), [&](auto tpr, auto nv) {
             constexpr int TPR = tpr.value, NV = nv.value;
             const dim3 block(TPR < 256 ? 256 : TPR), grid((unsigned)parts);
             if (sums)
