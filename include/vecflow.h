@@ -561,15 +561,15 @@ int vf_rms_norm_workspace(int32_t dtype, int64_t m, int64_t d, size_t *bytes);
  *   loss     float [m]; 0 for a row without entries, NaN for one with an id that is neither a label nor -1
  *   lse      float [m] or NULL: log sum exp(logits / temperature), which the gradient reads
  * temperature: 1e-6 .. 1e6.  A logit of -inf is a masked label: an entry at it whose q is not 0 makes the loss +inf.  NaN or +inf in a row's logits or
- * teacher makes its loss NaN.
+ * teacher makes its loss NaN.  Both over temperature are float32: what lies below its range then is -inf, above it +inf.
  */
 #define VF_DISTILL_MAX_TOP 256
 int vf_distill(int32_t dtype, int64_t m, int64_t v, const void *logits, int64_t ld, const int32_t *ids, const float *teacher,
                int32_t top, double temperature, float *loss, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream);
 /*
  * dlogits_i = d_loss / temperature (p_i - sum of q at i), [m][v] of dtype; lse as vf_distill left it for these logits and temperature (p as in
- * vf_log_probs_backward: lse's own rounding is a relative error that a row's p share).  Zeros for rows without entries, without a label left,
- * or with an id that is neither a label nor -1.  dlogits may be the logits' own memory (same ld).
+ * vf_log_probs_backward: lse's own rounding is a relative error that a row's p share).  Zeros for rows without entries, without a label left
+ * (masked by -inf, or by VF_F32's or VF_BF16's lowest numbers: an lse below -2^100), or with an id that is neither a label nor -1.  dlogits may be the logits' own memory (same ld).
  */
 int vf_distill_backward(int32_t dtype, int64_t m, int64_t v, const void *logits, int64_t ld, const float *lse, const int32_t *ids,
                         const float *teacher, int32_t top, double temperature, const float *d_loss, void *dlogits, int64_t ldd,

@@ -227,7 +227,7 @@ __global__ __launch_bounds__(256) void distill_backward_kernel(int64_t m, int64_
         e.load(ids, teacher, row, v, top, inv_t);
         e.soften();
         const float l = lse[row], g = d_loss[row] * inv_t;
-        const bool none = l == -kInf || e.bad || !e.any;   // no gradient
+        const bool none = l < -0x1p100f || e.bad || !e.any;   // no gradient (so low, l says nothing of how many labels share p)
         for (int64_t base = c0; base < c1; base += kTile) {
             float x[8];
 #pragma unroll
