@@ -1,4 +1,5 @@
-"""Encoding captured into a graph: every replay says what the eager call says of the same queries, bit for bit, with eager work in between."""
+"""Encoding captured into a graph: every replay says what the eager call says of the same queries, bit for bit, with eager work in between.  Among the last files
+by its name, as test_zz_ops_streams.py: it makes streams."""
 import pytest
 import torch
 
