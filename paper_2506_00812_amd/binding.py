@@ -933,12 +933,17 @@ def _q8(q, what, dev, rows=None, cols=None):
     if not isinstance(q, Q8):
         raise VecflowError(f"{what} must be a Q8")
     codes, scales, d = q
-    n = codes.shape[0]
+    shape = codes.shape
+    n = shape[0]
     if d < 0 or (rows is not None and n != rows) or (cols is not None and d != cols):
         raise VecflowError(f"{what} must have shape [{n if rows is None else rows}, {d if cols is None else cols}], not [{n}, {d}]")
     blocks = -(-d // Q8_BLOCK)
-    ld = _matrix(codes, f"{what}: codes", _torch.float8_e4m3fn, dev, n, blocks * Q8_BLOCK)
-    lds = _matrix(scales, f"{what}: scales", _torch.uint8, dev, n, -(-blocks // 4) * 4)
+    width, words = blocks * Q8_BLOCK, -(-blocks // 4) * 4
+    if (codes.dtype == _torch.float8_e4m3fn and scales.dtype == _torch.uint8 and codes.get_device() == dev and scales.get_device() == dev
+            and shape == (n, width) and scales.shape == (n, words) and codes.is_contiguous() and scales.is_contiguous()):
+        return codes.data_ptr(), width, scales.data_ptr(), words     # (as the library makes them: half of the time of what follows)
+    ld = _matrix(codes, f"{what}: codes", _torch.float8_e4m3fn, dev, n, width)
+    lds = _matrix(scales, f"{what}: scales", _torch.uint8, dev, n, words)
     return codes.data_ptr(), ld, scales.data_ptr(), lds
 
 
