@@ -636,6 +636,46 @@ __global__ __launch_bounds__(WP *WQ * 64, 2) void direct_kernel(Product<T> a, Ep
     store_tile<T, FP, FQ, FP * 16, FQ * 16, GATED>(a, e, acc, tiles, wave, lane, p0 + (GATED ? wp / 2 : wp), q0 + wq);
 }
 
+// a += the splits' sums of n (0 .. N) neighbours, in order; split: elements from one's to the next, half: to the other half's.  Four splits are on their way at a
+// time: outputs of few rows have many splits and too few threads to wait for each by itself.
+template <int G, int N>
+__device__ __forceinline__ void join_splits(const float *__restrict__ part, int64_t split, int64_t half, int splits, int n, float (&a)[G][N])
+{
+    using V = float __attribute__((ext_vector_type(N)));
+    if (n <= 0) return;
+    if (n >= N) {
+        for (int s = 0; s < splits; s += 4) {
+            V u[4][G];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int g = 0; g < G; ++g) u[k][g] = load_vec<V>(part + min(s + k, splits - 1) * split + g * half);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int g = 0; g < G; ++g)
+#pragma unroll
+                    for (int j = 0; j < N; ++j) a[g][j] += s + k < splits ? u[k][g][j] : 0.f;
+        }
+        return;
+    }
+    for (int s = 0; s < splits; s += 4) {   // (the same element by element)
+        float u[4][G][N];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+                for (int j = 0; j < N; ++j) u[k][g][j] = part[min(s + k, splits - 1) * split + g * half + min(j, n - 1)];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+                for (int j = 0; j < N; ++j) a[g][j] += s + k < splits && j < n ? u[k][g][j] : 0.f;
+    }
+}
+
 // The splits' sums, in order, and the epilogue: 4 x 4,096 x 1,024 in 12 us, 6 TB/s.
 template <class T, bool GATED = false>
 __global__ __launch_bounds__(256) void product_join_kernel(int64_t np, int64_t nq, int splits, const float *__restrict__ part, Epilogue<T> e)
@@ -645,14 +685,8 @@ __global__ __launch_bounds__(256) void product_join_kernel(int64_t np, int64_t n
         const int64_t q = i / quads, p = (i - q * quads) * 4;
         const int n = (int)min((int64_t)4, np - p);
         constexpr int G = GATED ? 2 : 1;
-        float a[G][4] = {}, u[4];
-        for (int s = 0; s < splits; ++s)
-#pragma unroll
-            for (int g = 0; g < G; ++g) {
-                load_row(part + ((int64_t)s * nq + q) * (G * np) + g * np + p, n, u);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) a[g][j] += u[j];
-            }
+        float a[G][4] = {};
+        join_splits<G, 4>(part + q * (G * np) + p, nq * (G * np), np, splits, n, a);
         float bias[G][4];
 #pragma unroll
         for (int g = 0; g < G; ++g) load_bias(e, g * np + p, n, bias[g]);

@@ -447,21 +447,17 @@ __global__ __launch_bounds__(256) void q8_join_kernel(Q8Product a, Q8Epilogue<T>
         const int64_t q = i / blocks, b = i - q * blocks, p = b * kBlock + (threadIdx.x & 15) * 8;
         const int n = (int)max((int64_t)0, min((int64_t)8, a.np - p));
         if (!Q8 && n == 0) continue;
-        float v[G][8], u[8];
+        float v[G][8] = {}, bias[G][8] = {}, r[8];
+        if (e.bias) {
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
-            load8(a.part + q * a.np * G + g * a.np + p, n, v[g]);
-            for (int s = 1; s < a.splits; ++s) {
-                load8(a.part + ((int64_t)s * a.nq + q) * a.np * G + g * a.np + p, n, u);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[g][j] += u[j];
-            }
-            if (e.bias) {
-                load8(e.bias + g * a.np + p, n, u);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[g][j] += u[j];
-            }
+            for (int g = 0; g < G; ++g) load8(e.bias + g * a.np + p, n, bias[g]);
         }
+        if (e.residual) load8(e.residual + q * e.ldr + p, n, r);
+        join_splits<G, 8>(a.part + q * (a.np * G) + p, a.nq * (a.np * G), a.np, a.splits, n, v);
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[g][j] += bias[g][j];
         by_act(e.act, [&](auto act) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -470,9 +466,8 @@ __global__ __launch_bounds__(256) void q8_join_kernel(Q8Product a, Q8Epilogue<T>
             }
         });
         if (e.residual) {
-            load8(e.residual + q * e.ldr + p, n, u);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[0][j] += u[j];
+            for (int j = 0; j < 8; ++j) v[0][j] += r[j];
         }
         if constexpr (Q8) keep_block(v[0], e.codes + q * e.ldc + p, e.scales + q * e.lds + b);
         else store8(e.y + q * e.ldy + p, n, v[0]);
