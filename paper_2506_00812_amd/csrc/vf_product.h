@@ -637,7 +637,7 @@ __global__ __launch_bounds__(WP *WQ * 64, 2) void direct_kernel(Product<T> a, Ep
 }
 
 // a += the splits' sums of n (0 .. N) neighbours, in order; split: elements from one's to the next, half: to the other half's.  Four splits are on their way at a
-// time: outputs of few rows have many splits and too few threads to wait for each by itself.
+// time: outputs of few rows have many splits and too few threads to wait for each by itself (288 x 2 x 181 in 8 bits, six splits: 7.5 us, 12 one by one).
 template <int G, int N>
 __device__ __forceinline__ void join_splits(const float *__restrict__ part, int64_t split, int64_t half, int splits, int n, float (&a)[G][N])
 {
