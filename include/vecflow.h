@@ -535,7 +535,7 @@ int vf_debug_linear_quantized(int32_t dtype, int64_t m, int64_t n, int64_t k, in
 
 /*
  * total = x + residual (rounded to dtype; total = x without a residual), y = total rstd weight, rstd = 1 / sqrt(avg(total^2) + eps), per row of
- * 1 <= d <= 2^24 elements.  Squares and their sum are float32: a row with values of 2^63 and more has rstd 0, one below 2^-75 everywhere rstd 1 / sqrt(eps).
+ * 1 <= d <= 2^24 elements.  Squares and their sum are float32: a row with values of 2^63 and more may have rstd 0, and y 0.
  *   weight [d] or NULL (1); residual, total [m][d]: both or neither; rstd float [m] or NULL.  The output is either y [m][d] or (y NULL) y_codes and
  *   y_scales, 8 bits straight from float32.  total may be x's or the residual's own memory (same ld); y may be x's own where there is no residual.
  */
