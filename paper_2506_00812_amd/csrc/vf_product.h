@@ -741,6 +741,15 @@ inline double few_rows_us(int64_t np, int64_t nq, int64_t row_bytes)
     return std::max(latency, (double)np * row_bytes / 5.3e6 + groups * nq * row_bytes / 10e6);
 }
 
+// The same of a gated layer, np rows of both halves: half as many waves, each with twice the loads, and Q's rows once for both.  The last term is what workgroups cost by
+// themselves, which counts where the contraction is short (2 x 65,536 x 100 in bfloat16, 33 rows: 38 us, 14 in tiles of 64 x 64).
+inline double few_rows_gated_us(int64_t np, int64_t nq, int64_t row_bytes)
+{
+    const double groups = (double)ceil_div(np, 16), rows = nq <= 16 ? 16 : nq <= 32 ? 32 : 64;
+    const double latency = 3 + 0.6 * (double)row_bytes / 1024 * (nq <= 16 ? 2 : nq <= 32 ? 3 : 5);
+    return std::max({latency, 3 + (double)np * row_bytes / 5.3e6 + groups * rows * row_bytes / 25e6, 3 + groups * 1e-4 * (nq <= 16 ? 2 : nq <= 32 ? 13 : 40)});
+}
+
 struct ProductPlan {
     bool fits = true;     // false: no tiling has few enough tiles
     Tiling tiling = kSmall;
@@ -774,8 +783,7 @@ inline ProductPlan plan_product(int32_t dtype, int64_t np, int64_t nq, int64_t n
         best.tiling = kFewRows;
         best.chunk = nc;
         least = few_rows_us(np, nq, nc * (int64_t)type_size(dtype));
-        // what a workgroup costs by itself, which counts where the contraction is short (2 x 65,536 x 100 in bfloat16, 33 rows: 38 us, 14 in tiles of 64 x 64)
-        if (o.gated) least = std::max(least, 3 + (double)ceil_div(np, 16) * 1e-4 * (nq <= 16 ? 2 : nq <= 32 ? 13 : 40));
+        if (o.gated) least = few_rows_gated_us(np, nq, nc * (int64_t)type_size(dtype));
         // (the quickest that any tile could be: one split, or one step of many; a call of few rows should not wait for its plan)
         if (least <= std::min(3.4 + 0.4 * (double)ceil_div(nc, step), 9.3)) return best;
     }
