@@ -391,9 +391,10 @@ template <int H> __device__ __forceinline__ void place_tile(int64_t group, int64
 // BP x BQ outputs per workgroup of WP x WQ waves; two tiles of each operand in LDS, one being read while the other is filled through
 // registers, which takes any alignment.  128 x 128 outputs by eight waves, 10,000 x 4,096 x 1,024: float32 123 - 132 TFLOP/s (the library's
 // product 137 - 154), bfloat16 with rows that start anywhere 530 - 720; four waves reach half of that (one wave per SIMD waits
-// for LDS), 64 x 64 outputs are for products with too few tiles of 128.
+// for LDS), 64 x 64 outputs are for products with too few tiles of 128.  Two workgroups of eight waves share a compute unit, which takes at most 128 registers a
+// lane: dx in 2-byte types is told so (by itself it came to 140: 11,311 x 2,663 x 968 in bfloat16 158 us, 113 this way).
 template <class T, bool PC, bool QC, int BP, int BQ, int WP, int WQ, bool GATED = false>
-__global__ __launch_bounds__(WP *WQ * 64) void tile_kernel(Product<T> a, Epilogue<T> e)
+__global__ __launch_bounds__(WP *WQ * 64, WP *WQ == 8 && !PC && QC && sizeof(T) == 2 ? 4 : 1) void tile_kernel(Product<T> a, Epilogue<T> e)
 {
     constexpr int OUT = GATED ? BP / 2 : BP;   // outputs of a row that the tile has
     constexpr int THREADS = WP * WQ * 64, BC = kRowBytes / (int)sizeof(T), FP = BP / WP / 16, FQ = BQ / WQ / 16;
