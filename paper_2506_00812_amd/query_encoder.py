@@ -97,8 +97,10 @@ class QueryEncoder(_Encoder):
         if gated:
             del start["n1b"], start["n2b"]
         gone = torch.as_tensor(() if absent is None else absent, device=device)
+        self._absent = None     # which labels, where there are any
         if gone.numel():     # (an empty list makes a tensor of floats, which is no index)
             start["bl"][gone] = -torch.inf
+            self._absent = torch.isneginf(start["bl"])
         self.params = {k: v.to(dtype) for k, v in start.items()}
         self.names = list(start)
         self._masters = [start[k] for k in self.names] if dtype != torch.float32 else None
@@ -146,8 +148,16 @@ class QueryEncoder(_Encoder):
         """(loss, {name: gradient}) of mean |vector - target|^2 - label_weight mean log p(label) - entropy_weight mean
         entropy.  vectors [m, dim]; labels int32 [m], -1 for a query without one.  Of no queries at all everything is 0.  Gradients
         are of the encoder's dtype, for float16 in float32.  teacher: (ids, log probabilities or logits) of a teacher's most probable labels, as encode(x, top)
-        of another encoder gives them; adds teacher_weight times the mean divergence from it at `temperature` (binding.distill)."""
+        of another encoder gives them; adds teacher_weight times the mean divergence from it at `temperature` (binding.distill).  What it says of this encoder's
+        `absent` labels is left out: the other entries' probabilities are taken among themselves, and a query without any other has no share in it."""
         return self._gradients(x, vectors, labels, label_weight, entropy_weight, teacher, teacher_weight, temperature)[:2]
+
+    def _given(self, ids, values):
+        """A teacher's entries, -1 for those at labels that are never predicted (an infinite divergence otherwise, with gradients that belong to none)."""
+        if self._absent is None or ids.dtype != torch.int32 or ids.device != self._absent.device:     # (other ids are refused)
+            return ids, values
+        at = ids.clamp(0, len(self._absent) - 1)
+        return ids.masked_fill(self._absent[at.long()] & (at == ids), -1), values
 
     def _gradients(self, x, vectors, labels, label_weight=1.0, entropy_weight=0.0, teacher=None, teacher_weight=1.0, temperature=1.0):
         """The same, and for float16 the one tensor that holds all gradients."""
@@ -167,6 +177,7 @@ class QueryEncoder(_Encoder):
                 d.mul_(self.scale)
         taught = None
         if teacher is not None:
+            teacher = self._given(*teacher)
             apart, lse_t = vf.distill(logits, *teacher, temperature=temperature)
             loss = loss + teacher_weight * apart.mean() if len(x) else loss
             d_apart = torch.full_like(apart, teacher_weight / m)
