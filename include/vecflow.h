@@ -492,6 +492,9 @@ int vf_gated_linear_backward(int32_t dtype, int64_t m, int64_t n, int64_t k, con
                              void *hip_stream);
 int vf_gated_linear_workspace(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t activation, int32_t backward,
                               size_t *bytes);
+/* Test support, host only: the tiling and splits of the forward product, as vf_debug_linear says them. */
+int vf_debug_gated_linear(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t activation, int32_t direct, int32_t *tiling,
+                          int32_t *splits);
 
 /*
  * Matrices in 8 bits: codes in OCP e4m3 (4 bits of exponent, 3 of significand, no infinity), and for each 128 columns of a row, its last ones

@@ -29,7 +29,7 @@ EXPORTED_SYMBOLS = ("vf_build_index", "vf_search", "vf_search_exact", "vf_index_
                     "vf_linear", "vf_linear_backward", "vf_linear_workspace", "vf_debug_linear", "vf_layer_norm", "vf_layer_norm_backward",
                     "vf_layer_norm_workspace", "vf_log_probs", "vf_log_probs_backward", "vf_log_probs_workspace",
                     "vf_adamw_step", "vf_adamw_moments",
-                    "vf_gated_linear", "vf_gated_linear_backward", "vf_gated_linear_workspace", "vf_quantize", "vf_dequantize", "vf_linear_quantized",
+                    "vf_gated_linear", "vf_gated_linear_backward", "vf_gated_linear_workspace", "vf_debug_gated_linear", "vf_quantize", "vf_dequantize", "vf_linear_quantized",
                     "vf_linear_quantized_workspace", "vf_debug_linear_quantized", "vf_rms_norm", "vf_rms_norm_backward", "vf_rms_norm_workspace", "vf_distill", "vf_distill_backward",
                     "vf_distill_workspace")
 
@@ -151,6 +151,7 @@ def load_library():
                 vf_gated_linear=[i32, i64, i64, i64, p, i64, p, i64, p, i32, p, i64, p, i64, p, sz, p],
                 vf_gated_linear_backward=[i32, i64, i64, i64, p, i64, p, i64, p, i64, p, i64, i32, p, i64, p, i64, p, p, sz, p],
                 vf_gated_linear_workspace=[i32, i64, i64, i64, i32, i32, C.POINTER(sz)],
+                vf_debug_gated_linear=[i32, i64, i64, i64, i32, i32, C.POINTER(i32), C.POINTER(i32)],
                 vf_quantize=[i32, i64, i64, p, i64, p, i64, p, i64, p],
                 vf_dequantize=[i32, i64, i64, p, i64, p, i64, p, i64, p],
                 vf_linear_quantized=[i32, i64, i64, i64, p, i64, p, i64, p, i64, p, i64, p, i32, i32, p, i64, p, i64, p, i64, p, i64, p, sz, p],
@@ -910,6 +911,13 @@ def gated_linear_backward(dy, x, weight, z, activation="silu", bias=True, dx=Tru
                                       gx.data_ptr() if dx else None, k, gw.data_ptr() if dweight else None, k,
                                       gb.data_ptr() if bias else None, pw, nw, handle))
     return gx, gw, gb
+
+
+def debug_gated_linear(dtype, m, n, k, activation="silu", direct=True):
+    """(tiling, splits) of gated_linear's product (vf_debug_gated_linear); dtype: VF_F32, VF_BF16 or VF_F16."""
+    tiling, splits = C.c_int32(), C.c_int32()
+    _check(load_library().vf_debug_gated_linear(dtype, m, n, k, _activation(activation), int(direct), C.byref(tiling), C.byref(splits)))
+    return tiling.value, splits.value
 
 
 class Q8(NamedTuple):

@@ -376,6 +376,12 @@ extern "C" int vf_gated_linear_workspace(int32_t dtype, int64_t m, int64_t n, in
     return guarded([&] { return gated_linear_workspace_impl(dtype, m, n, k, activation, backward, bytes); });
 }
 
+extern "C" int vf_debug_gated_linear(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t activation, int32_t direct, int32_t *tiling,
+                                     int32_t *splits)
+{
+    return guarded([&] { return debug_gated_linear_impl(dtype, m, n, k, activation, direct, tiling, splits); });
+}
+
 extern "C" int vf_quantize(int32_t dtype, int64_t m, int64_t d, const void *x, int64_t ldx, uint8_t *codes, int64_t ld, uint8_t *scales,
                            int64_t lds, void *hip_stream)
 {

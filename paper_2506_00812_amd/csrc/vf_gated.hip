@@ -101,6 +101,23 @@ int gated_linear_workspace_impl(int32_t dtype, int64_t m, int64_t n, int64_t k, 
     return VF_OK;
 }
 
+// The forward product's plan; direct: whether both operands' rows can go to LDS directly.
+static ProductPlan plan_gated(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t act, bool direct)
+{
+    return plan_product(dtype, 2 * n, m, k, {true, true, costly(act), direct, true});
+}
+
+int debug_gated_linear_impl(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t act, int32_t direct, int32_t *tiling, int32_t *splits)
+{
+    if (int rc = check_gated(dtype, m, n, k, act); rc != VF_OK) return rc;
+    VF_REQUIRE(tiling && splits, "gated linear: tiling or splits is NULL");
+    const ProductPlan p = plan_gated(dtype, m, n, k, act, direct != 0 && dtype != VF_F32);
+    VF_REQUIRE(p.fits, kTooManyGatedTiles);
+    *tiling = p.tiling;
+    *splits = p.splits;
+    return VF_OK;
+}
+
 int gated_linear_impl(const LinearArgs &a)
 {
     if (int rc = check_gated(a.dtype, a.m, a.n, a.k, a.act); rc != VF_OK) return rc;
@@ -109,7 +126,7 @@ int gated_linear_impl(const LinearArgs &a)
     VF_REQUIRE(a.y != nullptr, "gated linear: y is NULL");
     VF_REQUIRE(a.ldx >= a.k && a.ldw >= a.k, "gated linear: ldx or ldw is less than k");
     VF_REQUIRE(a.ldy >= a.n && (!a.z || a.ldz >= 2 * a.n), "gated linear: ldy is less than n or ldz less than 2 n");
-    const ProductPlan plan = plan_product(a.dtype, 2 * a.n, a.m, a.k, {true, true, costly(a.act), direct_rows(a.dtype, a.x, a.ldx) && direct_rows(a.dtype, a.w, a.ldw), true});
+    const ProductPlan plan = plan_gated(a.dtype, a.m, a.n, a.k, a.act, direct_rows(a.dtype, a.x, a.ldx) && direct_rows(a.dtype, a.w, a.ldw));
     VF_REQUIRE(plan.fits, kTooManyGatedTiles);
     if (int rc = check_workspace("gated linear", a.workspace, a.workspace_bytes, plan.bytes); rc != VF_OK) return rc;
     const size_t size = type_size(a.dtype);

@@ -318,6 +318,7 @@ int linear_backward_impl(const LinearArgs &a);
 bool linear_backward_fits(const LinearArgs &a);   // whether its products (activation none) have few enough tiles
 int gated_linear_impl(const LinearArgs &a);       // n outputs of 2 n rows of w
 int gated_linear_backward_impl(const LinearArgs &a);
+int debug_gated_linear_impl(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t act, int32_t direct, int32_t *tiling, int32_t *splits);
 int gated_linear_workspace_impl(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t act, int32_t backward, size_t *bytes);
 int debug_linear_impl(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t product, int32_t direct, int32_t *tiling, int32_t *splits);
 int linear_workspace_impl(int32_t dtype, int64_t m, int64_t n, int64_t k, int32_t act, int32_t backward, size_t *bytes);
