@@ -289,6 +289,23 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(int64_t m, int64_t d,
         part[((int64_t)blockIdx.y * 2 + sub) * d + c] = (comb[sub][0][t] + comb[sub][1][t]) + (comb[sub][2][t] + comb[sub][3][t]);
 }
 
+// Calls fn(threads per row, vectors per thread) as constants for rows of nv vectors; false: no such kernel, the row is too long.
+// A wave takes rows of up to four vectors a lane by itself; beyond that the row's sums would keep too many registers.  Rows of up to 32
+// vectors, the index's own dimensions among them, take sixteen lanes each: a wave's instructions then serve four rows.
+template <class F> static bool by_row(int64_t nv, F &&fn)
+{
+    if (nv <= 16) fn(std::integral_constant<int, 16>(), std::integral_constant<int, 1>());
+    else if (nv <= 32) fn(std::integral_constant<int, 16>(), std::integral_constant<int, 2>());
+    else if (nv <= 64) fn(std::integral_constant<int, 64>(), std::integral_constant<int, 1>());
+    else if (nv <= 128) fn(std::integral_constant<int, 64>(), std::integral_constant<int, 2>());
+    else if (nv <= 256) fn(std::integral_constant<int, 64>(), std::integral_constant<int, 4>());
+    else if (nv <= 512) fn(std::integral_constant<int, 256>(), std::integral_constant<int, 2>());
+    else if (nv <= 1024) fn(std::integral_constant<int, 256>(), std::integral_constant<int, 4>());
+    else if (nv <= 2048) fn(std::integral_constant<int, 512>(), std::integral_constant<int, 4>());
+    else return false;
+    return true;
+}
+
 constexpr int64_t kMaxRow = 1 << 24;   // elements of a row
 
 static int64_t vectors_of(int32_t dtype, int64_t d) { return ceil_div(d, 16 / (int64_t)type_size(dtype)); }

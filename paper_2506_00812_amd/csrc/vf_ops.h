@@ -280,23 +280,6 @@ template <class T> void launch_join_parts(int parts, int64_t d, int sums, const 
     join_parts_kernel<T><<<dim3((unsigned)ceil_div(d, 16), (unsigned)sums), dim3(1024), 0, s>>>(parts, d, part, out0, out1);
 }
 
-// Calls fn(threads per row, vectors per thread) as constants for rows of nv vectors; false: no such kernel, the row is too long.
-// A wave takes rows of up to four vectors a lane by itself; beyond that the row's sums would keep too many registers.  Rows of up to 32
-// vectors, the index's own dimensions among them, take sixteen lanes each: a wave's instructions then serve four rows.
-template <class F> bool by_row(int64_t nv, F &&fn)
-{
-    if (nv <= 16) fn(std::integral_constant<int, 16>(), std::integral_constant<int, 1>());
-    else if (nv <= 32) fn(std::integral_constant<int, 16>(), std::integral_constant<int, 2>());
-    else if (nv <= 64) fn(std::integral_constant<int, 64>(), std::integral_constant<int, 1>());
-    else if (nv <= 128) fn(std::integral_constant<int, 64>(), std::integral_constant<int, 2>());
-    else if (nv <= 256) fn(std::integral_constant<int, 64>(), std::integral_constant<int, 4>());
-    else if (nv <= 512) fn(std::integral_constant<int, 256>(), std::integral_constant<int, 2>());
-    else if (nv <= 1024) fn(std::integral_constant<int, 256>(), std::integral_constant<int, 4>());
-    else if (nv <= 2048) fn(std::integral_constant<int, 512>(), std::integral_constant<int, 4>());
-    else return false;
-    return true;
-}
-
 // A launch holds fewer than 2^32 threads: kernels loop over the rows beyond so many workgroups.
 inline unsigned grid_of(int64_t blocks) { return (unsigned)std::min<int64_t>(blocks, 1 << 20); }
 
