@@ -518,8 +518,9 @@ int vf_dequantize(int32_t dtype, int64_t m, int64_t d, const uint8_t *codes, int
  * y = act(z) + residual, or where `gated` is 1 act(z_gate) z_up + residual, z = x w^T + bias, of x [m][k] and w [n][k] (gated: [2 n][k], the gate's
  * rows first) in 8 bits.  dtype is that of bias [n] (gated: [2 n]; or NULL), residual [m][n] (or NULL) and y [m][n].  The output is either y, which may be
  * the residual's own memory (same ld), or (y NULL) y_codes and y_scales.  n <= 2^24, k < 2^24; rows of x and w lie less than 2^24 bytes apart.
- * dtype VF_F32: products to float32's accuracy, at half the rate.  Else they are as good as the matrix cores' sums of products of codes, which are added
- * eight neighbours at a time to 2^-13 of the largest of them: 1.4e-5 of the result where values are of like size, a hundredth of what bfloat16 rounds by.
+ * dtype VF_F32 and outputs in 8 bits: products to float32's accuracy, at half the rate.  Else they are as good as the matrix cores' sums of products of codes, which are
+ * added eight neighbours at a time to 2^-13 of the largest of them: 1.4e-5 of the result where values are of like size, a hundredth of what bfloat16 rounds by, but all of
+ * one that is left of large products' difference.  (Up to 64 rows may be computed to float32's accuracy all the same: a row's outputs depend on the batch that far.)
  * Values below 2^-126, which only scales of 2^-118 and less have, may count as 0.
  */
 int vf_linear_quantized(int32_t dtype, int64_t m, int64_t n, int64_t k, const uint8_t *x_codes, int64_t ldx, const uint8_t *x_scales,

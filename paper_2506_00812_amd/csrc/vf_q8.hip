@@ -71,12 +71,16 @@ template <class T> struct Q8Epilogue {
     int64_t ldc, lds;
 };
 
-// 32 rows of each operand and 64 of the contraction, 32 codes a lane.  EXACT (float32 outputs): the codes are turned into bfloat16, which holds them
-// exactly together with their scales.  The matrix cores add products of codes eight neighbours at a time, to 2^-13 of the largest of them
+// 32 rows of each operand and 64 of the contraction, 32 codes a lane.  EXACT (outputs in float32 and in 8 bits): the codes are turned into bfloat16, which holds
+// them exactly together with their scales.  The matrix cores add products of codes eight neighbours at a time, to 2^-13 of the largest of them
 // (measured: 2^16 + 2^3 is right, 2^16 + 2^2 is 2^16; nine places apart nothing is lost): 1.4e-5 of a result of values of like size, whatever their
-// number, where products of bfloat16 have 3e-8.  Outputs in bfloat16 and float16 round by far more.
-__device__ __forceinline__ void decode(const int8v &c, float scale, Vec<bf16> (&v)[4])
+// number, where products of bfloat16 have 3e-8.  Outputs in bfloat16 and float16 round by far more, 2^-9 of themselves on average and 2^-12, and take it.  Codes do not:
+// a sum that is off by so little is on the other side of the middle of two codes once in 2,500 outputs, and a code is 2^-3 of its value further: 0.0015 of the result
+// in norm, where float32 sums leave 0.0001.
+// (The conversion reads the exponent's bits of the scale alone, and takes 0 for 2^-127 and 255 for NaN, as a scale's byte has them.)
+__device__ __forceinline__ void decode(const int8v &c, int byte, Vec<bf16> (&v)[4])
 {
+    const float scale = __uint_as_float((uint32_t)byte << 23);
 #pragma unroll
     for (int g = 0; g < 4; ++g)
 #pragma unroll
@@ -88,19 +92,15 @@ __device__ __forceinline__ void decode(const int8v &c, float scale, Vec<bf16> (&
         }
 }
 
-template <bool EXACT>
+__device__ __forceinline__ float16v mma32(const Vec<bf16> (&p)[4], const Vec<bf16> (&q)[4], float16v acc)
+{
+#pragma unroll
+    for (int g = 0; g < 4; ++g) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(p[g], q[g], acc, 0, 0, 0);
+    return acc;
+}
 __device__ __forceinline__ float16v mma32(const int8v &p, int sp, const int8v &q, int sq, float16v acc)
 {
-    if constexpr (EXACT) {
-        Vec<bf16> vp[4], vq[4];
-        decode(p, scale_value(sp & 255), vp);
-        decode(q, scale_value(sq & 255), vq);
-#pragma unroll
-        for (int g = 0; g < 4; ++g) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vp[g], vq[g], acc, 0, 0, 0);
-        return acc;
-    } else {
-        return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(p, q, acc, 0, 0, 0, sp, 0, sq);
-    }
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(p, q, acc, 0, 0, 0, sp, 0, sq);
 }
 
 // ---------------------------------------------------------------- few rows
@@ -137,11 +137,11 @@ __global__ __launch_bounds__(GATED ? 512 : 1024) void q8_few_rows_kernel(Q8Produ
         }
         Vec<bf16> vp[G][4];
 #pragma unroll
-        for (int g = 0; g < G; ++g) decode(cp[g], scale_value(sp[g]), vp[g]);
+        for (int g = 0; g < G; ++g) decode(cp[g], sp[g], vp[g]);
 #pragma unroll
         for (int j = 0; j < FQ; ++j) {
             Vec<bf16> vq[4];
-            decode(cq[j], scale_value(sq[j]), vq);
+            decode(cq[j], sq[j], vq);
 #pragma unroll
             for (int u = 0; u < 4; ++u)
 #pragma unroll
@@ -222,8 +222,9 @@ __device__ __forceinline__ void request4(const void *from, uint32_t to)
 // scales of four blocks, eight steps, come a 32-bit word a row; a word's next byte is shifted down every other step.
 // Bound by the matrix cores' clock under load and by what a tile has beside its loop: 256 x 256 sums take 1.47 us per block of 128 of the contraction (1.26 without
 // any loads), and a tile some 2 us for its first loads and 5 - 8 for its outputs, which only a second workgroup on the compute unit hides.  10,000 x 1,024 x 4,096 with a
-// residual: 48 - 53 us in 212 tiles of 256 x 192 (1,600 - 1,740 TFLOP/s; the library's bare product 44.5); 10,000 x (2 x 4,096) x 1,024, gated into 8 bits: 103 - 115 us in tiles
-// of 256 x 128 (1,460 - 1,630); bare 10,000 x 4,096 x 1,024 68 us (the library 63); 1,777 x 333 x 777 into float32: 11 us.
+// residual: 48 - 53 us in 212 tiles of 256 x 192 (1,600 - 1,740 TFLOP/s; the library's bare product 44.5); 10,000 x (2 x 4,096) x 1,024, gated into bfloat16: 109 us in tiles
+// of 256 x 128 (1,540); bare 10,000 x 4,096 x 1,024 67 us (the library 63).  EXACT is bound by the rate of bfloat16 and has sixteen conversions for a fragment beside it: the gated
+// product into 8 bits 170 us (990 TFLOP/s), 10,000 x 1,024 x 4,096 into 8 bits 81, into float32 in tiles of 128 x 128 88; 1,777 x 333 x 777 into float32: 8 us.
 template <class T, bool EXACT, bool GATED, int BP, int BQ, int WP, int WQ, int STEPS>
 __global__ __launch_bounds__(WP *WQ * 64, BP *BQ == 16384 ? 3 : 2) void q8_tile_kernel(Q8Product a, Q8Epilogue<T> e)
 {
@@ -293,7 +294,7 @@ __global__ __launch_bounds__(WP *WQ * 64, BP *BQ == 16384 ? 3 : 2) void q8_tile_
     if (BP * BQ == 32768 && (blockIdx.x >> 8) == 1 && gridDim.x > 512)
         for (int i = 0; i < blocks; ++i) __builtin_amdgcn_s_sleep(32);
     float16v acc[FP][FQ] = {};
-    int8v fp[FP], fq[2][FQ];
+    int8v fp[FP], fq[EXACT ? 1 : 2][FQ];
     int sp[FP], sq[FQ];
     auto read_scales = [&](int group) {
         const int *w = (const int *)(words + (group & 1) * ((BP + BQ) * 4));
@@ -305,13 +306,18 @@ __global__ __launch_bounds__(WP *WQ * 64, BP *BQ == 16384 ? 3 : 2) void q8_tile_
     // A step in parts, one for each fragment of P: its matrix instructions, then the same fragment of the next step into the registers that they have read; Q's
     // fragments have two sets.  Step t + STEPS - 1 goes into the buffer of step t - 1, whose fragments everybody has used before this step's barrier: the last reads
     // of a step's own may still be on their way there.  MORE: step t + STEPS - 1 exists.
-    auto one_step = [&](auto more, int t, int set) {
+    auto one_step = [&](auto more, int t, int set) __attribute__((always_inline)) {   // (as a function of its own it would take addresses in vector registers)
         constexpr int kParts = FP;
         __builtin_amdgcn_sched_barrier(0);
         if (more.value || t + STEPS - 2 < steps) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((STEPS - 3) * LOADS) : "memory");
         else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
         const bool request_more = more.value || t + STEPS - 1 < steps;
         const unsigned char *at = tiles + buffer_of(t + 1) * kStep;   // (beyond the last step: a buffer's old contents, not used)
+        Vec<bf16> vq[EXACT ? FQ : 1][4];   // Q's fragments as they are multiplied: their codes' registers are free for the next step's
+        if constexpr (EXACT) {
+#pragma unroll
+            for (int j = 0; j < FQ; ++j) decode(fq[0][j], sq[j] & 255, vq[j]);
+        }
 #pragma unroll
         for (int g = 0; g < kParts; ++g) {
             __builtin_amdgcn_sched_barrier(0);
@@ -319,9 +325,16 @@ __global__ __launch_bounds__(WP *WQ * 64, BP *BQ == 16384 ? 3 : 2) void q8_tile_
             // (the next step begins with these: read early, they are there by then)
 #pragma unroll
             for (int f = 0; f < FQ; ++f)
-                if (min(f, kParts - 1) == g) fq[set ^ 1][f] = q8_fragment(at + BP * 64, wq + f * 32 + row, lane);
+                if (min(f, kParts - 1) == g) fq[EXACT ? 0 : set ^ 1][f] = q8_fragment(at + BP * 64, wq + f * 32 + row, lane);
+            if constexpr (EXACT) {
+                Vec<bf16> vp[4];
+                decode(fp[g], sp[g] & 255, vp);
 #pragma unroll
-            for (int j = 0; j < FQ; ++j) acc[g][j] = mma32<EXACT>(fp[g], sp[g], fq[set][j], sq[j], acc[g][j]);
+                for (int j = 0; j < FQ; ++j) acc[g][j] = mma32(vp, vq[j], acc[g][j]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < FQ; ++j) acc[g][j] = mma32(fp[g], sp[g], fq[set][j], sq[j], acc[g][j]);
+            }
             // (here, and the sums in their own registers: the compiler would gather the step's matrix instructions at its end, and keep all of its reads until then)
 #pragma unroll
             for (int j = 0; j < FQ; ++j) asm volatile("" : "+a"(acc[g][j])::"memory");
@@ -342,7 +355,7 @@ __global__ __launch_bounds__(WP *WQ * 64, BP *BQ == 16384 ? 3 : 2) void q8_tile_
     }
     // The words of the next four blocks are asked for at the first of four, into the half that the last four have left (their words were read before this
     // block's first barrier), and read at the fourth's end: eight steps' waits lie between.
-    auto one_block = [&](auto more, int b) {
+    auto one_block = [&](auto more, int b) __attribute__((always_inline)) {
         const bool next = (b & 3) == 0 && b + 4 < blocks;
         one_step(more, 2 * b, 0);
         if (next) request_scales(b / 4 + 1);
@@ -536,20 +549,29 @@ struct Q8Plan {
 };
 
 // What a tiling costs, in microseconds: `step` per block of 128 of the contraction with a compute unit full of `together` workgroups, at least `alone` however few
-// there are; `fixed` per workgroup for its first loads and its outputs.  Fitted to 1,020 timings: 23 sizes from 65 x 1,024 x 1,024 to 8,192 x 4,096 x 2,048, each with
-// outputs in bfloat16, bare and with GELU and a residual, gated ones in bfloat16 and in 8 bits and float32 ones, every tiling and 1 to 8 splits; what it picks takes 2.6 % longer than the best of all on average,
-// 31 % at worst (100 x 300 -> 777).
+// there are; `fixed` per workgroup for its first loads and its outputs.  Fitted: 23 sizes from 65 x 1,024 x 1,024 to 8,192 x 4,096 x 2,048, outputs in bfloat16 bare, gated and
+// with GELU and a residual, and in float32, every tiling and 1 to 8 splits; outputs in 8 bits: 113 sizes, 1 to 16 splits.  What it picks takes 1.1 % longer than the best of all on average,
+// 23 % at worst (65 x 1,024 x 1,024 into 8 bits).  `step` and `fixed` are not told apart well by contractions of 8 to 32 blocks: they are fits, not times of a loop.
 struct Q8Cost {
     int bp, bq, together;
     double step, alone, fixed;
 };
-static Q8Cost q8_cost(Q8Tiling t, bool exact, bool gated)
+static Q8Cost q8_cost(Q8Tiling t, bool f32, bool gated, bool quantized)
 {
+    if (quantized && !f32) {   // exact sums
+        switch (t) {
+        case kQ8Slim: return Q8Cost{256, 64, 2, 1.43, 1.08, 5.35};
+        case kQ8Square: return Q8Cost{128, 128, 3, 2.36, 1.31, 6.16};
+        case kQ8Long: return gated ? Q8Cost{256, 128, 2, 2.34, 0.865, 9.04} : Q8Cost{256, 128, 2, 3.6, 0.876, 9.48};
+        case kQ8Wide: return gated ? Q8Cost{256, 192, 1, 1.28, 0.383, 10.5} : Q8Cost{256, 192, 1, 1.92, 1.87, 8.93};
+        default: return gated ? Q8Cost{256, 256, 1, 1.98, 0.999, 12.6} : Q8Cost{256, 256, 1, 2.45, 0.546, 12.1};
+        }
+    }
     switch (t) {
-    case kQ8Slim: return exact ? Q8Cost{256, 64, 2, 2.1, 1.2, 8.0} : Q8Cost{256, 64, 2, 1.34, 0.73, 7.0};
-    case kQ8Small: return exact ? Q8Cost{64, 64, 4, 1.36, 0.47, 4.1} : Q8Cost{64, 64, 4, 1.07, 0.33, gated ? 2.5 : 3.0};
+    case kQ8Slim: return Q8Cost{256, 64, 2, 2.1, 1.2, 8.0};   // (float32: the others' outputs in 8 bits are above)
+    case kQ8Small: return f32 ? Q8Cost{64, 64, 4, 1.36, 0.47, 4.1} : Q8Cost{64, 64, 4, 1.07, 0.33, gated ? 2.5 : 3.0};
     case kQ8Square:
-        return exact ? Q8Cost{128, 128, 3, 2.65, 0.98, 7.5} : gated ? Q8Cost{128, 128, 3, 1.6, 0.6, 6.2} : Q8Cost{128, 128, 3, 1.55, 0.55, 7.2};
+        return f32 ? Q8Cost{128, 128, 3, 2.65, 0.98, 7.5} : gated ? Q8Cost{128, 128, 3, 1.6, 0.6, 6.2} : Q8Cost{128, 128, 3, 1.55, 0.55, 7.2};
     case kQ8Long: return gated ? Q8Cost{256, 128, 2, 1.6, 1.2, 9.0} : Q8Cost{256, 128, 2, 1.64, 1.2, 9.1};
     case kQ8Wide: return gated ? Q8Cost{256, 192, 1, 1.08, 0.3, 10.0} : Q8Cost{256, 192, 1, 0.87, 0.12, 10.0};
     default: return gated ? Q8Cost{256, 256, 1, 1.38, 0.26, 12.0} : Q8Cost{256, 256, 1, 1.03, 0.11, 11.4};
@@ -576,7 +598,7 @@ static double few_cost(int64_t m, int64_t n, int64_t blocks, bool gated)
 static Q8Plan plan_q8(int32_t dtype, int64_t m, int64_t n, int64_t k, bool gated, bool quantized, bool heavy)
 {
     Q8Plan best;
-    const bool exact = dtype == VF_F32;
+    const bool f32 = dtype == VF_F32;
     const int64_t blocks = ceil_div(k, kBlock), rows = gated ? 2 * n : n;
     const size_t sums = (size_t)m * rows * 4;
     double least = 0;
@@ -589,8 +611,8 @@ static Q8Plan plan_q8(int32_t dtype, int64_t m, int64_t n, int64_t k, bool gated
     for (Q8Tiling t : {kQ8Slim, kQ8Small, kQ8Square, kQ8Long, kQ8Wide, kQ8Large}) {
         if (t == kQ8Slim && !(gated && quantized)) continue;
         if ((t == kQ8Small && quantized) || (t == kQ8Square && gated && quantized)) continue;   // (half a block of outputs)
-        if (exact && t > kQ8Square) continue;
-        Q8Cost c = q8_cost(t, exact, gated);
+        if (f32 && t > kQ8Square) continue;
+        Q8Cost c = q8_cost(t, f32, gated, quantized);
         if (heavy) c.fixed += 6.0 * c.together * c.bp * c.bq / 65536 * (c.together > 1 ? 0.75 : 1);   // (less where another workgroup multiplies meanwhile)
         const int64_t tiles = ceil_div(n, gated ? c.bp / 2 : c.bp) * ceil_div(m, c.bq);
         if (tiles >= kMaxTiles) continue;
@@ -630,9 +652,10 @@ static int launch_q8(const Q8Product &a, const Q8Epilogue<T> &e, hipStream_t s)
     return VF_OK;
 }
 
-template <class T, bool GATED> static int run_q8(const Q8Product &a, const Q8Epilogue<T> &e, Q8Tiling t, hipStream_t s)
+// EXACT: outputs in float32 or in 8 bits.
+template <class T, bool EXACT, bool GATED> static int run_q8(const Q8Product &a, const Q8Epilogue<T> &e, Q8Tiling t, hipStream_t s)
 {
-    constexpr bool kExact = std::is_same_v<T, float>;
+    constexpr bool kWide = std::is_same_v<T, float> || !EXACT, kEight = EXACT;   // outputs that the call may have
     int rc = VF_OK;
     if (t == kQ8Few) {
         const dim3 grid((unsigned)ceil_div(a.np, 16)), block(few_waves(a.blocks, GATED) * 64);
@@ -640,15 +663,15 @@ template <class T, bool GATED> static int run_q8(const Q8Product &a, const Q8Epi
         else if (a.nq <= 32) q8_few_rows_kernel<T, 2, GATED><<<grid, block, 0, s>>>(a, e);
         else q8_few_rows_kernel<T, 4, GATED><<<grid, block, 0, s>>>(a, e);
     } else if (t == kQ8Slim) {
-        if constexpr (GATED) rc = launch_q8<T, kExact, true, 256, 64, 4, 1, 3>(a, e, s);
+        if constexpr (GATED && kEight) rc = launch_q8<T, EXACT, true, 256, 64, 4, 1, 3>(a, e, s);
     } else if (t == kQ8Small) {
-        rc = launch_q8<T, kExact, GATED, 64, 64, 2, 2, 4>(a, e, s);
+        if constexpr (kWide) rc = launch_q8<T, EXACT, GATED, 64, 64, 2, 2, 4>(a, e, s);
     } else if (t == kQ8Square) {
-        rc = launch_q8<T, kExact, GATED, 128, 128, 2, 2, 3>(a, e, s);
-    } else if constexpr (!kExact) {
-        if (t == kQ8Long) rc = launch_q8<T, false, GATED, 256, 128, 2, 2, 3>(a, e, s);
-        else if (t == kQ8Wide) rc = launch_q8<T, false, GATED, 256, 192, 4, 2, 4>(a, e, s);
-        else rc = launch_q8<T, false, GATED, 256, 256, 2, 4, 4>(a, e, s);
+        if constexpr (kWide || !GATED) rc = launch_q8<T, EXACT, GATED, 128, 128, 2, 2, 3>(a, e, s);
+    } else if constexpr (!std::is_same_v<T, float>) {
+        if (t == kQ8Long) rc = launch_q8<T, EXACT, GATED, 256, 128, 2, 2, 3>(a, e, s);
+        else if (t == kQ8Wide) rc = launch_q8<T, EXACT, GATED, 256, 192, 4, 2, 4>(a, e, s);
+        else rc = launch_q8<T, EXACT, GATED, 256, 256, 2, 4, 4>(a, e, s);
     }
     if (rc != VF_OK) return rc;
     if (a.splits > 0) {
@@ -718,7 +741,12 @@ int linear_q8_impl(const LinearQ8Args &a)
     by_type(a.dtype, [&](auto *t) {
         using T = std::remove_pointer_t<decltype(t)>;
         const Q8Epilogue<T> e{(const T *)a.bias, a.act, (const T *)a.residual, a.ldr, (T *)a.y, a.ldy, (uint8_t *)a.out.codes, (uint8_t *)a.out.scales, a.out.ld, a.out.lds};
-        rc = a.gated ? run_q8<T, true>(p, e, plan.tiling, a.stream) : run_q8<T, false>(p, e, plan.tiling, a.stream);
+        auto run = [&](auto exact) {
+            rc = a.gated ? run_q8<T, exact.value, true>(p, e, plan.tiling, a.stream) : run_q8<T, exact.value, false>(p, e, plan.tiling, a.stream);
+        };
+        if constexpr (std::is_same_v<T, float>) run(std::true_type());
+        else if (q8) run(std::true_type());
+        else run(std::false_type());
     });
     return rc;
 }
