@@ -74,7 +74,7 @@ template <class T> struct Q8Epilogue {
 // 32 rows of each operand and 64 of the contraction, 32 codes a lane.  EXACT (outputs in float32 and in 8 bits): the codes are turned into bfloat16, which holds
 // them exactly together with their scales.  The matrix cores add products of codes eight neighbours at a time, to 2^-13 of the largest of them
 // (measured: 2^16 + 2^3 is right, 2^16 + 2^2 is 2^16; nine places apart nothing is lost): 1.4e-5 of a result of values of like size, whatever their
-// number, where products of bfloat16 have 3e-8.  Outputs in bfloat16 and float16 round by far more, 2^-9 of themselves on average and 2^-12, and take it.  Codes do not:
+// number, where products of bfloat16 have 3e-8.  Outputs in bfloat16 and float16 round by far more (up to 2^-8 and 2^-11 of themselves) and take it.  Codes do not:
 // a sum that is off by so little is on the other side of the middle of two codes once in 2,500 outputs, and a code is 2^-3 of its value further: 0.0015 of the result
 // in norm, where float32 sums leave 0.0001.
 // (The conversion reads the exponent's bits of the scale alone, and takes 0 for 2^-127 and 255 for NaN, as a scale's byte has them.)
@@ -290,8 +290,8 @@ __global__ __launch_bounds__(WP *WQ * 64, BP *BQ == 16384 ? 3 : 2) void q8_tile_
     };
     const int wp = wave % WP * (FP * 32), wq = wave / WP * (FQ * 32), row = lane & 31;
     // Two workgroups share a compute unit: the second of each begins later, by some two thirds of a loop alone, so that one's matrix instructions have the time in
-    // which the other's outputs are computed and written (10,000 x 4,096 x 1,024, gated into 8 bits: 103 us, side by side 112).
-    if (BP * BQ == 32768 && (blockIdx.x >> 8) == 1 && gridDim.x > 512)
+    // which the other's outputs are computed and written (10,000 x 4,096 x 1,024, gated into bfloat16: 108 us, side by side 113; exact sums take longer and gain nothing).
+    if (!EXACT && BP * BQ == 32768 && (blockIdx.x >> 8) == 1 && gridDim.x > 512)
         for (int i = 0; i < blocks; ++i) __builtin_amdgcn_s_sleep(32);
     float16v acc[FP][FQ] = {};
     int8v fp[FP], fq[EXACT ? 1 : 2][FQ];
@@ -578,7 +578,7 @@ static Q8Cost q8_cost(Q8Tiling t, bool f32, bool gated, bool quantized)
     }
 }
 
-constexpr double kJoinCost = 6;   // of one more launch: small products come one after the other as fast as the host can launch them
+constexpr double kJoinCost = 6;   // of one more launch and its workspace, for a host that makes small calls as fast as it can: 4 us and more (in a graph 2)
 
 static int few_waves(int64_t blocks, bool gated) { return (int)std::max<int64_t>(1, std::min<int64_t>(gated ? 8 : 16, blocks)); }
 
