@@ -117,7 +117,7 @@ template <class T, int R> __device__ __forceinline__ void load_entries(const Dis
 
 // Segment `item % nseg` of a row: TPR threads take its vectors in turn, 16 elements a thread at a time.  nseg > 1: the segment's sums go to
 // part [row][nseg].  Sixteen elements have one maximum and at most one change of origin, so that an element costs one exponential.  64 x 200,000 in bfloat16,
-// 13 segments a row: 26 MB in 8.0 us and 2.6 for the join; 10,000 x 10,000: 44 us (4.5 TB/s).  (Asking for the next vectors ahead gained nothing.)
+// 13 segments a row: 26 MB in 8.0 us and 2.6 for the join; 10,000 x 10,000: 38 us (5.2 TB/s).  (Asking for the next vectors ahead gained nothing.)
 template <class T, int TPR, int R>
 __global__ __launch_bounds__(256) void distill_kernel(int64_t m, DistillRow<T> a, int nseg, int64_t seg, float2 *__restrict__ part)
 {

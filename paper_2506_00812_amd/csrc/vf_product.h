@@ -711,8 +711,9 @@ enum Tiling {
 
 // What a tiling costs, in microseconds: `step` per 128 bytes of the contraction with a compute unit full of `together` workgroups, at
 // least `alone` however few there are; `fixed` per workgroup for its first loads and its stores.  Fitted to 2,255 timings: 39 sizes
-// from 32 x 1,024 x 1,024 to 8,192 x 4,096 x 2,048, each product, every tiling and 1 to 32 splits; what it picks takes 3.4 % longer than the best of
-// all on average, more than 10 % for 16 of 117 products, 53 % at worst (64 x 4,096 -> 128: 16.3 us for 10.7).
+// from 32 x 1,024 x 1,024 to 8,192 x 4,096 x 2,048, each product, every tiling and 1 to 32 splits.  Timed again with tiles in place_tile's order and splits joined four at a
+// time, what it picks takes 2.9 % longer than the best of all on average, more than 10 % for 10 of 117 products, 31 % at worst (dx of 4,000 x 1,024 x 1,024 whose rows start
+// anywhere: 64 x 64 for 128 x 128).
 struct TilingCost {
     int bp, bq, together;
     double step, alone, fixed;

@@ -187,7 +187,7 @@ class QueryEncoder(_Encoder):
         d_logits = vf.log_probs_backward(logits, lse, labels, d_logp, entropy=entropy if entropy_weight else None,
                                          d_entropy=d_entropy, out=logits)
         if taught is not None:
-            d_logits.add_(taught)
+            d_logits.add_(taught)     # (each rounded to the type, and their sum: up to three halves of its steps)
         dg, grads["wl"], grads["bl"] = vf.linear_backward(d_logits, g, p["wl"])
         dg2, grads["wv"], grads["bv"] = vf.linear_backward(d_out.to(self.dtype), g, p["wv"])
         if self.gated:
