@@ -8,7 +8,8 @@ namespace vf {
 
 // dz and column sums of it: blockIdx.x has 64 vectors of columns of each half, blockIdx.y every gridDim.y-th group of four rows; one partial row
 // [2][n] each, or (dbias given: there is one) the sums themselves.  Bound by memory: dy and z read, dz written.  dz is rounded
-// to T, which the matrix cores take beside w and x (the linear layer's choice too); the sums take it before that.  10,000 x 4,096 in bfloat16: 410 MB in 70 us
+// to T, which the matrix cores take beside w and x (the linear layer's choice too; dx and dw are off by 0.0024 of their size in bfloat16, 0.0017 without it, and two
+// terms of dz would take both products twice as long); the sums take it before that.  10,000 x 4,096 in bfloat16: 410 MB in 70 us
 // (5.9 TB/s), the partial rows' join 5.  Kept apart from the products: dz is an operand of both, and each reads it many times over.
 template <class T, int ACT>
 __global__ __launch_bounds__(256) void gated_slope_kernel(int64_t m, int64_t n, const T *__restrict__ dy, int64_t lddy, const T *__restrict__ z,

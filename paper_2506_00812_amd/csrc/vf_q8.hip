@@ -379,7 +379,7 @@ __global__ __launch_bounds__(WP *WQ * 64, BP *BQ == 16384 ? 3 : 2) void q8_tile_
     constexpr int kRow = BP * 4 + 16, kLanes = OUT / 8, kRows = 32 / WP;   // 16 bytes more: rows start in other banks; rows of a wave
     static_assert(kLanes <= 64 && kRows % (64 / kLanes) == 0, "");
     unsigned char *turn = tiles + wave / WP * (32 * kRow);
-    const bool raw = a.splits > 0, q8 = e.y == nullptr;
+    const bool raw = a.splits > 0, q8 = EXACT && (!std::is_same_v<T, float> || e.y == nullptr);   // (2-byte types: exact sums are for outputs in 8 bits alone)
     const int64_t p = p0 + lane % kLanes * 8;
     const int m = (int)max((int64_t)0, min((int64_t)8, a.np - p));
     const int col = GATED ? (lane % kLanes >> 2) * 64 + (lane & 3) * 8 : lane % kLanes * 8;   // of the sums; the other half's are 32 further
