@@ -224,7 +224,7 @@ __device__ __forceinline__ void request4(const void *from, uint32_t to)
 // any loads), and a tile some 2 us for its first loads and 5 - 8 for its outputs, which only a second workgroup on the compute unit hides.  10,000 x 1,024 x 4,096 with a
 // residual: 48 - 53 us in 212 tiles of 256 x 192 (1,600 - 1,740 TFLOP/s; the library's bare product 44.5); 10,000 x (2 x 4,096) x 1,024, gated into bfloat16: 109 us in tiles
 // of 256 x 128 (1,540); bare 10,000 x 4,096 x 1,024 67 us (the library 63).  EXACT is bound by the rate of bfloat16 and has sixteen conversions for a fragment beside it: the gated
-// product into 8 bits 170 us (990 TFLOP/s), 10,000 x 1,024 x 4,096 into 8 bits 81, into float32 in tiles of 128 x 128 88; 1,777 x 333 x 777 into float32: 8 us.
+// product into 8 bits 157 - 171 us (980 - 1,070 TFLOP/s), 10,000 x 1,024 x 4,096 into 8 bits 78, into float32 in tiles of 128 x 128 88; 1,777 x 333 x 777 into float32: 8 us.
 template <class T, bool EXACT, bool GATED, int BP, int BQ, int WP, int WQ, int STEPS>
 __global__ __launch_bounds__(WP *WQ * 64, BP *BQ == 16384 ? 3 : 2) void q8_tile_kernel(Q8Product a, Q8Epilogue<T> e)
 {
@@ -550,8 +550,8 @@ struct Q8Plan {
 
 // What a tiling costs, in microseconds: `step` per block of 128 of the contraction with a compute unit full of `together` workgroups, at least `alone` however few
 // there are; `fixed` per workgroup for its first loads and its outputs.  Fitted: 23 sizes from 65 x 1,024 x 1,024 to 8,192 x 4,096 x 2,048, outputs in bfloat16 bare, gated and
-// with GELU and a residual, and in float32, every tiling and 1 to 8 splits; outputs in 8 bits: 113 sizes, 1 to 16 splits.  What it picks takes 1.1 % longer than the best of all on average,
-// 23 % at worst (65 x 1,024 x 1,024 into 8 bits).  `step` and `fixed` are not told apart well by contractions of 8 to 32 blocks: they are fits, not times of a loop.
+// with GELU and a residual, and in float32, every tiling and 1 to 8 splits; outputs in 8 bits: 113 sizes, 1 to 16 splits.  What it picks takes 0.9 % longer than the best of all on average,
+// 21 % at worst (65 x 1,024 x 1,024 into 8 bits).  `step` and `fixed` are not told apart well by contractions of 8 to 32 blocks: they are fits, not times of a loop.
 struct Q8Cost {
     int bp, bq, together;
     double step, alone, fixed;
