@@ -521,7 +521,7 @@ int vf_dequantize(int32_t dtype, int64_t m, int64_t d, const uint8_t *codes, int
  * dtype VF_F32 and outputs in 8 bits: products to float32's accuracy, at half the rate.  Else they are as good as the matrix cores' sums of products of codes, which are
  * added eight neighbours at a time to 2^-13 of the largest of them: 1.4e-5 of the result where values are of like size, a hundredth of what bfloat16 rounds by, but all of
  * one that is left of large products' difference.  (Up to 64 rows may be computed to float32's accuracy all the same: a row's outputs depend on the batch that far.)
- * Values below 2^-126, which only scales of 2^-118 and less have, may count as 0.
+ * Values below 2^-126, which only scales of 2^-118 and less have, may count as 0, and values of 2^128 and more, which nothing that the library writes has, as infinite.
  */
 int vf_linear_quantized(int32_t dtype, int64_t m, int64_t n, int64_t k, const uint8_t *x_codes, int64_t ldx, const uint8_t *x_scales,
                  int64_t ldxs, const uint8_t *w_codes, int64_t ldw, const uint8_t *w_scales, int64_t ldws, const void *bias,
