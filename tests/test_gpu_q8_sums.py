@@ -37,3 +37,31 @@ def test_small_products_beside_large_ones(T, m, n, k, gated, tiling, split):
         values, byte = held((z[:, :n].clamp_min(0) if act == "relu" else z[:, :n]) * z[:, n:] if gated else z.clamp_min(0) if act == "relu" else z)
         y = vf.linear_q8(vf.quantize(x), vf.quantize(w), activation=act, gated=bool(gated), dtype=T, quantize=True)
         assert torch.equal(vf.dequantize(y, F32).double(), values) and torch.equal(y.scales[:, :byte.shape[1]], byte)
+
+
+@pytest.mark.parametrize("T", [F32, BF, HF])
+@pytest.mark.parametrize("m,n,k,gated", [(5, 100, 300, 0), (130, 301, 700, 1), (1500, 1000, 256, 0), (2999, 2099, 640, 1), (9999, 777, 777, 0), (9999, 1499, 512, 0)])
+def test_scales_of_the_callers_own(T, m, n, k, gated):
+    """Scales whose powers cancel leave the outputs as they are; 255 is NaN for its row of x, or of w, and for no other one."""
+    x, w = (vf.quantize(torch.randn((r, k), generator=generator(r), device="cuda")) for r in (m, n * (1 + gated)))
+    x.scales.fill_(127)
+    w.scales.fill_(127)
+    call = lambda: vf.linear_q8(x, w, gated=bool(gated), dtype=T, quantize=True)   # noqa: E731
+    want = call()
+    for byte in (16, 238):
+        x.scales.fill_(byte)
+        w.scales.fill_(254 - byte)
+        got = call()
+        assert torch.equal(got.codes.view(torch.uint8), want.codes.view(torch.uint8)) and torch.equal(got.scales[:, :-(-n // 128)], want.scales[:, :-(-n // 128)]), byte
+    x.scales.fill_(127)
+    w.scales.fill_(127)
+    x.scales[m // 2, 1], w.scales[n - 3, 0] = 255, 255
+    got = call()
+    lost = torch.zeros((m, n), dtype=torch.bool, device="cuda")
+    lost[m // 2] = True
+    lost[:, n - 3] = True
+    values = vf.dequantize(got, F32)
+    assert torch.equal(values.isnan(), lost)
+    apart = torch.arange(n, device="cuda") // 128 != (n - 3) // 128     # blocks whose scale cannot have moved
+    keep = torch.arange(m, device="cuda") != m // 2
+    assert torch.equal(values[keep][:, apart], vf.dequantize(want, F32)[keep][:, apart])
